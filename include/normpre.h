@@ -430,6 +430,164 @@ int normpre_kernel_stats(normpre_ctx* ctx, int kclass, int64_t* launches,
 int normpre_stream_ceiling(int mix, int64_t n, const float* a, const float* b, const float* c,
                            float* out32, void* out16, void* stream);
 
+/* ---- training-step operators --------------------------------------------- */
+/*
+ * Operators that lie between a model's loss and the gradients normpre_step()
+ * takes: attention over packed sequences with its backward pass, and 8-bit
+ * activation checkpoints with the products of the backward pass that read
+ * them.
+ *   - No context: they keep no state and own no memory.  Workspaces are
+ *     arguments.  Any number of threads may call them at once.  They only
+ *     enqueue work on `stream` (a hipStream_t of the current device, to which
+ *     every pointer belongs); none of them allocates or synchronizes, so they
+ *     can be captured in a HIP graph.
+ *   - Arguments are checked on the host before anything is enqueued; the
+ *     message of an error is normpre_last_error(NULL) on the calling thread.
+ *   - Results do not depend on the order in which blocks run: the same
+ *     arguments give the same bits.
+ *   - Outputs must not overlap inputs or each other.
+ * Element types: NORMPRE_DTYPE_F32, NORMPRE_DTYPE_BF16.  Products of fp32
+ * operands keep fp32 accuracy, sums and softmax statistics are fp32 for both.
+ */
+#define NORMPRE_DTYPE_F32  0
+#define NORMPRE_DTYPE_BF16 1
+
+/*
+ * Plan of a packed batch: sequence i takes lens[i] >= 0 consecutive tokens,
+ * one sequence after the other.  The plan lists the blocks of 128 rows that
+ * the attention kernels work through, those with most work first.
+ * normpre_attention_plan_tiles() returns their number in *num_tiles;
+ * normpre_attention_plan() writes 8 int32 per tile to the host array `plan`
+ * (capacity in int32).  The caller copies it to the device once and passes it
+ * to every call on that batch; it depends on lens and causal only.  Host only.
+ * Errors: INVALID_ARG (null pointers, num_seqs < 0, a negative length,
+ * capacity too small), UNSUPPORTED (2^31 tokens or more), OOM.
+ */
+int normpre_attention_plan_tiles(int64_t num_seqs, const int64_t* lens, int64_t* num_tiles);
+int normpre_attention_plan(int64_t num_seqs, const int64_t* lens, int causal, int32_t* plan, int64_t capacity);
+
+/* One operand [tokens, heads, head_dim]: element (t, h, d) is
+ * data[t * token_stride + h * head_stride + d] (strides in elements, >= 0; a
+ * zero stride repeats an input).  Any strides and alignment of an element
+ * work; rows that start on 16 bytes (data, strides and head_dim multiples of
+ * 16 bytes) are read with 16-byte loads. */
+typedef struct normpre_heads {
+    void*   data;
+    int64_t token_stride;
+    int64_t head_stride;
+} normpre_heads;
+
+typedef struct normpre_attention {
+    int32_t dtype;              /* NORMPRE_DTYPE_*, of every operand             */
+    int32_t heads;              /* query heads                                   */
+    int32_t kv_heads;           /* key/value heads; divides heads: query head h  */
+                                /* reads key head h / (heads / kv_heads)         */
+    int32_t head_dim;           /* 1..128                                        */
+    int32_t causal;             /* 1: query i sees keys j <= i of its sequence   */
+    float   scale;              /* c, finite                                     */
+    int64_t tokens;             /* sum of the plan's lengths                     */
+    const int32_t* plan;        /* device copy of the plan (made with `causal`)  */
+    int64_t num_tiles;          /* of the plan                                   */
+    normpre_heads q, k, v;      /* read                                          */
+    normpre_heads out;          /* forward: written; backward: read              */
+    float*  lse;                /* [heads][tokens]: written / read               */
+    normpre_heads dout;         /* backward: read                                */
+    normpre_heads dq, dk, dv;   /* backward: written                             */
+    float*  workspace;          /* backward: heads * tokens floats               */
+} normpre_attention;
+
+/*
+ * out_i = sum_j p_ij v_j, p_ij = exp(c q_i . k_j - lse_i) over the keys j that
+ * query i sees, lse_i = log sum_j exp(c q_i . k_j).  A value that a query does
+ * not see never reaches its row, also where it is infinite or NaN; a row that
+ * sees one follows the formula.  tokens = 0 is a successful no-op.
+ * bf16 operands: p is rounded to bf16 for its product with v.
+ * The backward call takes q, k, v, out and lse of the forward call and
+ * d loss / d out, and writes d loss / d q, k, v (of a shared key head: summed
+ * over its query heads).  bf16 operands: p and ds are rounded to bf16 for
+ * their products.
+ * Errors: INVALID_ARG (null or misaligned pointers, unknown dtype, heads not
+ * a multiple of kv_heads, head_dim < 1, negative strides, an output whose
+ * rows overlap, a non-finite scale, num_tiles < 0, causal not 0 or 1, tokens
+ * and num_tiles that contradict each other), UNSUPPORTED (head_dim > 128,
+ * 2^31 tokens, strides above 2^40, more than 2^31 - 1 blocks), HIP.
+ */
+int normpre_attention_forward(const normpre_attention* a, void* stream);
+int normpre_attention_backward(const normpre_attention* a, void* stream);
+
+/*
+ * 8-bit checkpoints.  The checkpoint of x [rows, cols] has groups of 64
+ * consecutive features of a row (the last one of a row may be shorter).  With
+ * amax the largest magnitude of a group, e is the smallest integer in
+ * [-126, 121] with rint(amax 2^-e) <= 127 (-126 for a group of zeros), and a
+ * code is rint(x 2^-e), ties to even, within +-127; it stands for code * 2^e,
+ * which bf16 holds exactly.  A group with a NaN or an infinity has codes 0 and
+ * exponent -128, and stands for NaN.
+ *   codes: int8 [rows][pitch], pitch = cols rounded up to 64; 16-byte aligned
+ *   exps : int8 [rows][pitch / 64]
+ * The padding of a row is written as codes 0.
+ * ld_*: row strides in elements, >= cols; rows on 16 bytes are accessed in
+ * 16-byte pieces.  rows = 0 is a successful no-op.
+ */
+#define NORMPRE_CHECKPOINT_GROUP 64
+#define NORMPRE_ACT_NONE   0    /* checkpoint of u alone                        */
+#define NORMPRE_ACT_GELU   1    /* h = u s(2 sqrt(2/pi) (u + 0.044715 u^3))     */
+#define NORMPRE_ACT_SWIGLU 2    /* h = u s(u) up                                */
+/* (s: logistic function) */
+
+/*
+ * The activation of an MLP with the checkpoints its backward pass needs, in
+ * one pass: h (dtype) from u (and up), the checkpoint of u (and of up), and
+ * that of h as rounded to dtype, which the next layer reads.
+ * NORMPRE_ACT_NONE only packs u; up, h and their checkpoints are ignored, as
+ * is up with NORMPRE_ACT_GELU.
+ * Errors: INVALID_ARG (unknown act or dtype, null or misaligned pointers,
+ * rows < 0, cols < 1, ld < cols), UNSUPPORTED (more than 2^40 elements), HIP.
+ */
+int normpre_checkpoint_pack(int act, int dtype, int64_t rows, int64_t cols,
+                            const void* u, int64_t ld_u, const void* up, int64_t ld_up,
+                            void* h, int64_t ld_h,
+                            int8_t* u_codes, int8_t* u_exps, int8_t* up_codes, int8_t* up_exps,
+                            int8_t* h_codes, int8_t* h_exps, void* stream);
+
+/* The values a checkpoint stands for, in dtype (exact in both).  Errors as above. */
+int normpre_checkpoint_unpack(int dtype, int64_t rows, int64_t cols, const int8_t* codes, const int8_t* exps,
+                              void* out, int64_t ld_out, void* stream);
+
+/*
+ * Backward pass of the activation, from the checkpoints of its inputs:
+ *   GELU   du = dh (s + u s (1 - s) z'), z = 2 sqrt(2/pi) (u + 0.044715 u^3), s = s(z)
+ *   SWIGLU du = dh up s (1 + u (1 - s)), dup = dh u s, s = s(u)
+ * up_codes, up_exps and dup are ignored with NORMPRE_ACT_GELU.
+ * Errors as above, and INVALID_ARG for NORMPRE_ACT_NONE.
+ */
+int normpre_checkpoint_act_grad(int act, int dtype, int64_t rows, int64_t cols, const void* dh, int64_t ld_dh,
+                                const int8_t* u_codes, const int8_t* u_exps,
+                                const int8_t* up_codes, const int8_t* up_exps,
+                                void* du, int64_t ld_du, void* dup, int64_t ld_dup, void* stream);
+
+#define NORMPRE_WEIGHT_INNER_OUTER 0   /* dw[inner][outer]: y = x W              */
+#define NORMPRE_WEIGHT_OUTER_INNER 1   /* dw[outer][inner]: y = x W^T            */
+/*
+ * Weight gradient of a linear layer from the checkpoint of its input x
+ * [tokens, inner] and the gradient dy [tokens, outer] (dtype) of its output:
+ * dw[i, o] = sum_t x(t, i) dy(t, o), fp32, added to what dw holds if
+ * accumulate is 1.  Every product is exact (checkpoint values are exact in
+ * bf16, fp32 dy is split into three bf16 terms) and summed in fp32.  With
+ * tokens = 0 the gradient is zero.
+ * workspace: normpre_checkpoint_weight_grad_workspace() bytes, 16-byte aligned
+ * (null where that is 0).
+ * Errors: INVALID_ARG (as above, unknown layout, accumulate not 0 or 1, too
+ * small a workspace), UNSUPPORTED (a dimension above 2^31 - 1, more than 2^40
+ * elements), HIP.
+ */
+int normpre_checkpoint_weight_grad_workspace(int dtype, int64_t tokens, int64_t inner, int64_t outer,
+                                             int64_t* bytes);
+int normpre_checkpoint_weight_grad(int dtype, int layout, int accumulate, int64_t tokens, int64_t inner,
+                                   int64_t outer, const int8_t* codes, const int8_t* exps,
+                                   const void* dy, int64_t ld_dy, float* dw, int64_t ld_dw,
+                                   void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Library version string (static storage). */
 const char* normpre_version(void);
 

@@ -2,6 +2,8 @@
 
 The compute path is libnormpre.so (hand-written HIP kernels behind the C ABI of
 include/normpre.h); ``normpre`` is its ctypes binding and ``workloads`` draws
-seeded synthetic inputs.  Importing the package does not load the library.
+seeded synthetic inputs.  ``train_ops`` holds the training-step operators around
+the optimizer step (packed attention, 8-bit activation checkpoints).  Importing
+the package does not load the library.
 """
-__all__ = ["normpre", "workloads"]
+__all__ = ["normpre", "train_ops", "workloads"]

@@ -2354,6 +2354,8 @@ int step_prologue(normpre_ctx* ctx, int variant, int num_mats, float* const* par
 }  // namespace
 
 // =========================================================== C ABI ========
+int np::set_thread_error(int code, const char* msg) { return set_err(nullptr, code, msg); }
+
 extern "C" {
 
 const char* normpre_version(void) { return "normpre-mi355x 0.1 (gfx950, fp16 MFMA, fp32 accumulate)"; }

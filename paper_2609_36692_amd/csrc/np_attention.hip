@@ -1,0 +1,697 @@
+// Attention over packed sequences with grouped heads, forward and backward,
+// on the matrix instructions of gfx950 (32x32x16 bf16, 32x32x2 fp32).
+//
+// For query i and the keys j of its sequence that it sees (j <= i if causal),
+//   s_ij = c q_i . k_j,  p_ij = exp(s_ij - lse_i),  o_i = sum_j p_ij v_j,
+//   lse_i = log sum_j exp(s_ij),
+//   delta_i = do_i . o_i,  ds_ij = p_ij (do_i . v_j - delta_i),
+//   dq_i = c sum_j ds_ij k_j,  dk_j = c sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i,
+// the last two also over the query heads that share the key's head.
+//
+// All three passes have one form.  A wave owns 32 rows (queries, or keys in
+// the dk/dv pass) as the columns of its matrix products and keeps their
+// operands in registers; the other side streams through LDS in tiles that
+// all four waves of the block read.  A 32 x 32 block of scores then comes
+// out with one owned row per lane (both halves of the wave share it), so a
+// softmax row needs one exchange between the halves, and the block is
+// already in the layout of the second product's right operand: the k slots
+// of a matrix instruction may hold the streamed rows in any order as long as
+// both operands agree, and the transposing LDS reads of the left operand
+// fetch exactly the rows a lane's score registers hold.
+#include "np_train.h"
+
+#include <type_traits>
+
+namespace np {
+namespace {
+
+typedef __bf16 bf16_t;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr int kThreads = 256;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Block barrier that orders LDS only, so prefetches from global memory stay
+// in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+    return v;
+}
+
+// One 16-byte chunk of a row of `dim` elements, zero past the row's end.
+// VEC: rows are 16-byte aligned and dim is a whole number of chunks.
+template <class T, bool VEC>
+__device__ __forceinline__ u32x4 load_chunk(const T* row, int chunk, int dim, bool live) {
+    constexpr int E = 16 / sizeof(T);
+    u32x4 r = {0, 0, 0, 0};
+    const int d = chunk * E;
+    if constexpr (VEC) {
+        if (live && d < dim) r = *reinterpret_cast<const u32x4*>(row + d);
+    } else {
+        T e[E];
+#pragma unroll
+        for (int i = 0; i < E; ++i) e[i] = live && d + i < dim ? row[d + i] : T(0.f);
+        __builtin_memcpy(&r, e, 16);
+    }
+    return r;
+}
+
+// ------------------------------------------------------------ LDS tiles ---
+// ROWS x DP elements, rows of CH 16-byte chunks; chunk c of row r is kept at
+// c ^ swz(r).  Row reads take one chunk of 32 consecutive rows, transposing
+// reads 32 bytes of each of four consecutive rows: swz sends any eight
+// consecutive rows to eight different chunks and any four to four different
+// pairs of chunks, so neither kind meets itself in a bank.
+__device__ __forceinline__ int swz(int r) { return ((r & 3) << 1) | ((r >> 2) & 1); }
+
+template <class T, int DP>
+struct Tile {
+    static constexpr int E = 16 / sizeof(T);     // elements of a chunk
+    static constexpr int CH = DP / E;            // chunks of a row
+    static __device__ __forceinline__ int idx(int r, int c) { return (r * CH + (c ^ swz(r))) * E; }
+};
+
+// Staging of ROWS x DP from rows [row0, row0 + ROWS) of one operand, rows at
+// `rows` and past it zero.
+template <class T, int DP, int ROWS, bool VEC>
+struct Stage {
+    using TL = Tile<T, DP>;
+    static constexpr int N = ROWS * TL::CH / kThreads;
+    static_assert(N >= 1 && ROWS * TL::CH % kThreads == 0, "tile does not fill the block");
+    static __device__ __forceinline__ void load(u32x4 (&r)[N], const T* base, int64_t tok, int row0, int rows,
+                                                int dim, int tid) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int e = tid + i * kThreads, row = row0 + e / TL::CH;
+            r[i] = load_chunk<T, VEC>(base + (int64_t)row * tok, e % TL::CH, dim, row < rows);
+        }
+    }
+    static __device__ __forceinline__ void store(const u32x4 (&r)[N], T* lds, int tid) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int e = tid + i * kThreads;
+            *reinterpret_cast<u32x4*>(lds + TL::idx(e / TL::CH, e % TL::CH)) = r[i];
+        }
+    }
+};
+
+// Owned operand of one wave: chunk 2 s + half of row lane % 32, for every s.
+template <class T, int DP>
+struct Owned {
+    static constexpr int S = Tile<T, DP>::CH / 2;
+    u32x4 c[S];
+    template <bool VEC>
+    __device__ __forceinline__ void load(const T* row, int dim, bool live, int half) {
+#pragma unroll
+        for (int s = 0; s < S; ++s) c[s] = load_chunk<T, VEC>(row, 2 * s + half, dim, live);
+    }
+};
+
+// 32 x 32 scores: streamed rows [base, base + 32) of the tile against the
+// wave's owned rows.  Lane l gets owned row l % 32, register r streamed row
+// base + 8 (r / 4) + 4 (l / 32) + r % 4.
+template <class T, int DP>
+__device__ __forceinline__ f32x16 scores(const T* lds, int base, const Owned<T, DP>& b, int lane) {
+    using TL = Tile<T, DP>;
+    f32x16 acc = {};
+    const int row = base + (lane & 31), half = lane >> 5;
+#pragma unroll
+    for (int s = 0; s < Owned<T, DP>::S; ++s) {
+        const u32x4 a = *reinterpret_cast<const u32x4*>(lds + TL::idx(row, 2 * s + half));
+        if constexpr (std::is_same_v<T, bf16_t>) {
+            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                          __builtin_bit_cast(bf16x8, b.c[s]), acc, 0, 0, 0);
+        } else {
+            const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b.c[s]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], acc, 0, 0, 0);
+        }
+    }
+    return acc;
+}
+
+// acc[t] (features 32 t .. of the result, by owned row) += tile^T weights,
+// over streamed rows [base, base + 32); w in the layout of scores().  The
+// weights of bf16 operands are rounded to bf16, as matrix instructions take
+// them: relative error 2^-9 each, below the rounding of the bf16 result.
+template <class T, int DP>
+__device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* lds, int base, const f32x16& w,
+                                           int lane) {
+    using TL = Tile<T, DP>;
+    if constexpr (std::is_same_v<T, bf16_t>) {
+        typedef short s16x4 __attribute__((ext_vector_type(4)));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+        // Within each 16-lane group the transposing read returns to lane j
+        // the j-th column of the 4 x 16 block the group addresses (lane p
+        // supplies row p / 4, elements 4 (p % 4) ..).
+        const int g = lane >> 4, p = lane & 15;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            bf16x8 b;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] = (bf16_t)w[8 * s + i];
+            const int r0 = base + 16 * s + 4 * (g >> 1) + (p >> 2), r1 = r0 + 8;
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t) {
+                const int c = 4 * t + 2 * (g & 1) + ((p & 3) >> 1), in = 4 * (p & 1);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + TL::idx(r0, c) + in));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + TL::idx(r1, c) + in));
+                const s16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b, acc[t], 0, 0, 0);
+            }
+        }
+    } else {
+        const int half = lane >> 5, n = lane & 31;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = base + 8 * (r / 4) + 4 * half + r % 4;
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t) {
+                const float a = lds[TL::idx(row, 8 * t + n / 4) + n % 4];
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], acc[t], 0, 0, 0);
+            }
+        }
+    }
+}
+
+// Writes f * acc of the lane's owned row.
+template <class T, int DP, bool VEC>
+__device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], float f, int dim, int half) {
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int d = 32 * t + 8 * j + 4 * half;
+            if constexpr (VEC) {
+                if (d < dim) {
+                    T e[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) e[i] = (T)(f * acc[t][4 * j + i]);
+                    typedef uint32_t V __attribute__((ext_vector_type(sizeof(T))));
+                    V v;
+                    __builtin_memcpy(&v, e, sizeof v);
+                    *reinterpret_cast<V*>(row + d) = v;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (d + i < dim) row[d + i] = (T)(f * acc[t][4 * j + i]);
+            }
+        }
+}
+
+template <int NT>
+__device__ __forceinline__ bool any_nonfinite(const f32x16 (&acc)[NT]) {
+    float t = 0.f;                               // x * 0 is NaN for what is not finite
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) t = __builtin_fmaf(acc[i][r], 0.f, t);
+    return !(t == 0.f);
+}
+
+// ----------------------------------------------------- rows one by one ---
+// A matrix product multiplies the zero weight of a masked place with the
+// value there, and 0 * inf is NaN: where a tile on the diagonal holds values
+// that are not finite, rows that must not see them come out as NaN.  Rows of
+// the tiled passes that are not finite are therefore done again here, by one
+// wave each, over the places that they see and no others: lanes first along
+// the other side (64 scores at a time), then along the features.
+template <class T>
+__device__ __forceinline__ float dot(const T* a, const T* b, int dim) {
+    float s = 0.f;
+    for (int d = 0; d < dim; ++d) s = __builtin_fmaf((float)a[d], (float)b[d], s);
+    return s;
+}
+
+struct Where {                                   // one sequence, one head
+    int start, len, head, kv;
+};
+
+template <class T>
+__device__ __forceinline__ T* row_of(const AttnOperand& o, const Where& w, int row, int head) {
+    return static_cast<T*>(o.p) + (int64_t)(w.start + row) * o.tok + (int64_t)head * o.head;
+}
+
+template <class T>
+__device__ void forward_row(const AttnArgs& a, const Where& w, int qi, int lane) {
+    const T* q = row_of<T>(a.q, w, qi, w.head);
+    const int end = a.causal ? qi + 1 : w.len;
+    const float c2 = a.scale * kLog2e;
+    float m = -INFINITY, l = 0.f, o[2] = {0.f, 0.f};
+    for (int k0 = 0; k0 < end; k0 += 64) {
+        const int n = min(64, end - k0);
+        const float t = lane < n ? dot(q, row_of<T>(a.k, w, k0 + lane, w.kv), a.dim) * c2 : -INFINITY;
+        const float mn = fmaxf(m, wave_max(t)), mu = mn == -INFINITY ? 0.f : mn;
+        const float p = exp2_fast(t - mu), f = exp2_fast(m - mu);
+        l = l * f + wave_sum(p);
+        m = mn;
+        o[0] *= f;
+        o[1] *= f;
+        for (int j = 0; j < n; ++j) {
+            const float pj = __shfl(p, j, 64);
+            const T* v = row_of<T>(a.v, w, k0 + j, w.kv);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                if (lane + 64 * x < a.dim) o[x] = __builtin_fmaf(pj, (float)v[lane + 64 * x], o[x]);
+        }
+    }
+    T* out = row_of<T>(a.out, w, qi, w.head);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        if (lane + 64 * x < a.dim) out[lane + 64 * x] = (T)(o[x] / l);
+    if (lane == 0) a.lse[w.head * a.tokens + w.start + qi] = m * kLn2 + logf(l);
+}
+
+template <class T>
+__device__ void dq_row(const AttnArgs& a, const Where& w, int qi, float delta, int lane) {
+    const T *q = row_of<T>(a.q, w, qi, w.head), *dout = row_of<T>(a.dout, w, qi, w.head);
+    const int end = a.causal ? qi + 1 : w.len;
+    const float c2 = a.scale * kLog2e, lse2 = a.lse[w.head * a.tokens + w.start + qi] * kLog2e;
+    float g[2] = {0.f, 0.f};
+    for (int k0 = 0; k0 < end; k0 += 64) {
+        const int n = min(64, end - k0);
+        float ds = 0.f;
+        if (lane < n) {
+            const float p = exp2_fast(dot(q, row_of<T>(a.k, w, k0 + lane, w.kv), a.dim) * c2 - lse2);
+            ds = p * (dot(dout, row_of<T>(a.v, w, k0 + lane, w.kv), a.dim) - delta);
+        }
+        for (int j = 0; j < n; ++j) {
+            const float dj = __shfl(ds, j, 64);
+            const T* k = row_of<T>(a.k, w, k0 + j, w.kv);
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                if (lane + 64 * x < a.dim) g[x] = __builtin_fmaf(dj, (float)k[lane + 64 * x], g[x]);
+        }
+    }
+    T* dq = row_of<T>(a.dq, w, qi, w.head);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        if (lane + 64 * x < a.dim) dq[lane + 64 * x] = (T)(a.scale * g[x]);
+}
+
+template <class T>
+__device__ void dkv_row(const AttnArgs& a, const Where& w, int ki, int lane) {
+    const T *k = row_of<T>(a.k, w, ki, w.kv), *v = row_of<T>(a.v, w, ki, w.kv);
+    const int beg = a.causal ? ki : 0, group = a.heads / a.kv_heads;
+    const float c2 = a.scale * kLog2e;
+    float gk[2] = {0.f, 0.f}, gv[2] = {0.f, 0.f};
+    for (int h = w.kv * group; h < (w.kv + 1) * group; ++h)
+        for (int q0 = beg; q0 < w.len; q0 += 64) {
+            const int n = min(64, w.len - q0);
+            float p = 0.f, ds = 0.f;
+            if (lane < n) {
+                const int64_t at = h * a.tokens + w.start + q0 + lane;
+                p = exp2_fast(dot(row_of<T>(a.q, w, q0 + lane, h), k, a.dim) * c2 - a.lse[at] * kLog2e);
+                ds = p * (dot(row_of<T>(a.dout, w, q0 + lane, h), v, a.dim) - a.delta[at]);
+            }
+            for (int j = 0; j < n; ++j) {
+                const float pj = __shfl(p, j, 64), dj = __shfl(ds, j, 64);
+                const T *q = row_of<T>(a.q, w, q0 + j, h), *dout = row_of<T>(a.dout, w, q0 + j, h);
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (lane + 64 * x < a.dim) {
+                        gk[x] = __builtin_fmaf(dj, (float)q[lane + 64 * x], gk[x]);
+                        gv[x] = __builtin_fmaf(pj, (float)dout[lane + 64 * x], gv[x]);
+                    }
+            }
+        }
+    T *dk = row_of<T>(a.dk, w, ki, w.kv), *dv = row_of<T>(a.dv, w, ki, w.kv);
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+        if (lane + 64 * x < a.dim) {
+            dk[lane + 64 * x] = (T)(a.scale * gk[x]);
+            dv[lane + 64 * x] = (T)gv[x];
+        }
+}
+
+// Owned rows (bit r: row r of the wave's 32) that any lane calls bad.
+__device__ __forceinline__ uint32_t bad_rows(bool bad) {
+    const uint64_t b = __ballot(bad);
+    return (uint32_t)b | (uint32_t)(b >> 32);
+}
+
+// ---------------------------------------------------------------- passes ---
+// Rows of a streamed tile.
+template <class T> constexpr int kStream = std::is_same_v<T, bf16_t> ? 64 : 32;
+
+// Block order: key heads fastest, so the blocks of one key head (consecutive
+// workgroups go to the 8 XCDs in turn) stay with one XCD's L2 where the
+// number of key heads is a multiple of 8; the plan's tiles, longest first,
+// slowest.
+__device__ __forceinline__ bool locate(const AttnArgs& a, const AttnTile& t, int rows_per_tile, int& row0) {
+    row0 = t.tile * rows_per_tile;
+    return t.start >= 0 && t.len > 0 && t.tile >= 0 && row0 < t.len && (int64_t)t.start + t.len <= a.tokens;
+}
+
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__(kThreads, 1) attn_fwd_kernel(AttnArgs a) {
+    constexpr int BN = kStream<T>, NB = BN / 32, DT = DP / 32;
+    using ST = Stage<T, DP, BN, VEC>;
+    __shared__ __attribute__((aligned(16))) T smem[2][2][BN * DP];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int group = a.heads / a.kv_heads;
+    const AttnTile tile = a.tiles[blockIdx.x / a.heads];
+    const int kv = blockIdx.x % a.kv_heads, head = kv * group + (blockIdx.x / a.kv_heads) % group;
+    int q0;
+    if (!locate(a, tile, kAttnRows, q0)) return;    // the whole block
+    const Where w{tile.start, tile.len, head, kv};
+    const int qw = q0 + wave * 32, qi = qw + (lane & 31);
+    const bool live = qi < w.len;
+
+    Owned<T, DP> q;
+    q.template load<VEC>(row_of<T>(a.q, w, live ? qi : 0, head), a.dim, live, half);
+    const T *kb = row_of<T>(a.k, w, 0, kv), *vb = row_of<T>(a.v, w, 0, kv);
+    const int end = a.causal ? min(w.len, q0 + kAttnRows) : w.len, steps = (end + BN - 1) / BN;
+    const float c2 = a.scale * kLog2e;
+
+    f32x16 o[DT] = {};
+    float m = -INFINITY, l = 0.f;
+    u32x4 rk[ST::N], rv[ST::N];
+    ST::load(rk, kb, a.k.tok, 0, w.len, a.dim, tid);
+    ST::load(rv, vb, a.v.tok, 0, w.len, a.dim, tid);
+    ST::store(rk, smem[0][0], tid);
+    ST::store(rv, smem[0][1], tid);
+    for (int it = 0; it < steps; ++it) {
+        const int k0 = it * BN;
+        const bool more = it + 1 < steps;
+        if (more) {
+            ST::load(rk, kb, a.k.tok, k0 + BN, w.len, a.dim, tid);
+            ST::load(rv, vb, a.v.tok, k0 + BN, w.len, a.dim, tid);
+        }
+        lds_barrier();
+        const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
+        if (!a.causal || k0 <= qw + 31) {            // same for the whole wave
+            f32x16 s[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                s[b] = scores<T, DP>(ks, 32 * b, q, lane);
+                s[b] *= c2;
+            }
+            if (k0 + BN > w.len || (a.causal && k0 + BN - 1 > qw)) {
+                const int last = a.causal ? min(qi, w.len - 1) : w.len - 1;
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (k0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4 > last) s[b][r] = -INFINITY;
+            }
+            float mx = m;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float mu = mx == -INFINITY ? 0.f : mx, f = exp2_fast(m - mu);
+            m = mx;
+            l *= f;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[b][r] = exp2_fast(s[b][r] - mu);
+                    l += s[b][r];
+                }
+            if (__any(f != 1.f)) {
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[t] *= f;
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) accumulate<T, DP>(o, vs, 32 * b, s[b], lane);
+        }
+        if (more) {
+            ST::store(rk, smem[(it + 1) & 1][0], tid);
+            ST::store(rv, smem[(it + 1) & 1][1], tid);
+        }
+    }
+    l += __shfl_xor(l, 32, 64);
+    uint32_t bad = bad_rows(live && (any_nonfinite(o) || !(l < INFINITY)));
+    if (live && !(bad >> (lane & 31) & 1)) {
+        store_row<T, DP, VEC>(row_of<T>(a.out, w, qi, head), o, 1.f / l, a.dim, half);
+        if (half == 0) a.lse[head * a.tokens + w.start + qi] = m * kLn2 + logf(l);
+    }
+    for (; bad; bad &= bad - 1) forward_row<T>(a, w, qw + __builtin_ctz(bad), lane);
+}
+
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__(kThreads, 1) attn_dq_kernel(AttnArgs a) {
+    constexpr int BN = kStream<T>, NB = BN / 32, DT = DP / 32;
+    using ST = Stage<T, DP, BN, VEC>;
+    __shared__ __attribute__((aligned(16))) T smem[2][2][BN * DP];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int group = a.heads / a.kv_heads;
+    const AttnTile tile = a.tiles[blockIdx.x / a.heads];
+    const int kv = blockIdx.x % a.kv_heads, head = kv * group + (blockIdx.x / a.kv_heads) % group;
+    int q0;
+    if (!locate(a, tile, kAttnRows, q0)) return;    // the whole block
+    const Where w{tile.start, tile.len, head, kv};
+    const int qw = q0 + wave * 32, qi = qw + (lane & 31);
+    const bool live = qi < w.len;
+
+    Owned<T, DP> q, dout;
+    q.template load<VEC>(row_of<T>(a.q, w, live ? qi : 0, head), a.dim, live, half);
+    dout.template load<VEC>(row_of<T>(a.dout, w, live ? qi : 0, head), a.dim, live, half);
+    // delta of the lane's row: its half of the chunks, then the other half's.
+    float delta = 0.f;
+    {
+        const T* orow = row_of<T>(a.out, w, live ? qi : 0, head);
+#pragma unroll
+        for (int s = 0; s < Owned<T, DP>::S; ++s) {
+            const u32x4 oc = load_chunk<T, VEC>(orow, 2 * s + half, a.dim, live);
+            T x[16 / sizeof(T)], y[16 / sizeof(T)];
+            __builtin_memcpy(x, &oc, 16);
+            __builtin_memcpy(y, &dout.c[s], 16);
+#pragma unroll
+            for (int i = 0; i < (int)(16 / sizeof(T)); ++i) delta = __builtin_fmaf((float)x[i], (float)y[i], delta);
+        }
+        delta += __shfl_xor(delta, 32, 64);
+    }
+    const int64_t at = head * a.tokens + w.start + (live ? qi : 0);
+    const float lse2 = live ? a.lse[at] * kLog2e : INFINITY;
+    const T *kb = row_of<T>(a.k, w, 0, kv), *vb = row_of<T>(a.v, w, 0, kv);
+    const int end = a.causal ? min(w.len, q0 + kAttnRows) : w.len, steps = (end + BN - 1) / BN;
+    const float c2 = a.scale * kLog2e;
+
+    f32x16 g[DT] = {};
+    u32x4 rk[ST::N], rv[ST::N];
+    // delta = do . o carries the rounding of o.  Where a row sees few keys, o
+    // is as large as a value and that error as large as the other ones, so
+    // blocks with up to kAttnRows keys first sum delta = sum_j p dp from the
+    // scores; with more keys o averages out (error under a fifth of a
+    // rounding of ds) and a second pass over them would cost 2/3 of the first.
+    const bool twice = end <= kAttnRows;
+    float sum = 0.f;
+    for (int it = twice ? -steps : 0; it < steps; ++it) {
+        const int k0 = (it < 0 ? it + steps : it) * BN;
+        const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
+        if (it == 0 || it == -steps) {
+            if (it == 0 && twice) {
+                sum += __shfl_xor(sum, 32, 64);
+                delta = sum;
+                lds_barrier();                       // the first pass has read its tiles
+            }
+            ST::load(rk, kb, a.k.tok, 0, w.len, a.dim, tid);
+            ST::load(rv, vb, a.v.tok, 0, w.len, a.dim, tid);
+            ST::store(rk, smem[it & 1][0], tid);
+            ST::store(rv, smem[it & 1][1], tid);
+        }
+        const bool more = it + 1 < steps && it != -1;
+        if (more) {
+            ST::load(rk, kb, a.k.tok, k0 + BN, w.len, a.dim, tid);
+            ST::load(rv, vb, a.v.tok, k0 + BN, w.len, a.dim, tid);
+        }
+        lds_barrier();
+        if (!a.causal || k0 <= qw + 31) {            // same for the whole wave
+            const bool edge = k0 + BN > w.len || (a.causal && k0 + BN - 1 > qw);
+            const int last = a.causal ? min(qi, w.len - 1) : w.len - 1;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                f32x16 s = scores<T, DP>(ks, 32 * b, q, lane);
+                const f32x16 dp = scores<T, DP>(vs, 32 * b, dout, lane);
+                const float de = it < 0 ? 0.f : delta;
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    s[r] = exp2_fast(__builtin_fmaf(s[r], c2, -lse2)) * (dp[r] - de);
+                if (edge) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (k0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4 > last) s[r] = 0.f;
+                }
+                if (it < 0) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) sum += s[r];
+                } else {
+                    accumulate<T, DP>(g, ks, 32 * b, s, lane);
+                }
+            }
+        }
+        if (more) {
+            ST::store(rk, smem[(it + 1) & 1][0], tid);
+            ST::store(rv, smem[(it + 1) & 1][1], tid);
+        }
+    }
+    if (live && half == 0) a.delta[at] = delta;
+    uint32_t bad = bad_rows(live && any_nonfinite(g));
+    if (live && !(bad >> (lane & 31) & 1))
+        store_row<T, DP, VEC>(row_of<T>(a.dq, w, qi, head), g, a.scale, a.dim, half);
+    for (; bad; bad &= bad - 1) {
+        const int r = __builtin_ctz(bad);
+        dq_row<T>(a, w, qw + r, __shfl(delta, r, 64), lane);
+    }
+}
+
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__(kThreads, 1) attn_dkv_kernel(AttnArgs a) {
+    constexpr int BM = kStream<T>, NB = BM / 32, DT = DP / 32;
+    using ST = Stage<T, DP, BM, VEC>;
+    __shared__ __attribute__((aligned(16))) T smem[2][2][BM * DP];
+    __shared__ __attribute__((aligned(16))) float stat[2][2][BM];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int group = a.heads / a.kv_heads;
+    const AttnTile tile = a.tiles[a.num_tiles + blockIdx.x / a.kv_heads];
+    const int kv = blockIdx.x % a.kv_heads;
+    int kt;
+    if (!locate(a, tile, kAttnRows, kt)) return;    // the whole block
+    const Where w{tile.start, tile.len, kv * group, kv};
+    const int kw = kt + wave * 32, ki = kw + (lane & 31);
+    const bool live = ki < w.len;
+
+    Owned<T, DP> k, v;
+    k.template load<VEC>(row_of<T>(a.k, w, live ? ki : 0, kv), a.dim, live, half);
+    v.template load<VEC>(row_of<T>(a.v, w, live ? ki : 0, kv), a.dim, live, half);
+    const int first = a.causal ? kt / BM : 0, per = (w.len + BM - 1) / BM - first, steps = per * group;
+    const float c2 = a.scale * kLog2e;
+
+    f32x16 gk[DT] = {}, gv[DT] = {};
+    u32x4 rq[ST::N], rd[ST::N];
+    float rs = 0.f;
+    // Step i: queries of tile first + i % per, head kv * group + i / per.
+    auto fetch = [&](int i) {
+        const int h = w.head + i / per, row0 = (first + i % per) * BM;
+        ST::load(rq, row_of<T>(a.q, w, 0, h), a.q.tok, row0, w.len, a.dim, tid);
+        ST::load(rd, row_of<T>(a.dout, w, 0, h), a.dout.tok, row0, w.len, a.dim, tid);
+        if (tid < 2 * BM) {
+            const int row = row0 + tid % BM;
+            const float* src = tid < BM ? a.lse : a.delta;
+            // Queries past the end get lse = inf: their weights are zero.
+            rs = row < w.len ? src[h * a.tokens + w.start + row] * (tid < BM ? kLog2e : 1.f)
+                             : (tid < BM ? INFINITY : 0.f);
+        }
+    };
+    auto put = [&](int buf) {
+        ST::store(rq, smem[buf][0], tid);
+        ST::store(rd, smem[buf][1], tid);
+        if (tid < 2 * BM) stat[buf][tid / BM][tid % BM] = rs;
+    };
+    fetch(0);
+    put(0);
+    for (int it = 0; it < steps; ++it) {
+        const int q0 = (first + it % per) * BM;
+        const bool more = it + 1 < steps;
+        if (more) fetch(it + 1);
+        lds_barrier();
+        const T *qs = smem[it & 1][0], *ds = smem[it & 1][1];
+        const float *lse2 = stat[it & 1][0], *delta = stat[it & 1][1];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int qb = q0 + 32 * b;
+            if (qb >= w.len || (a.causal && qb + 31 < kw)) continue;   // same for the whole wave
+            f32x16 p = scores<T, DP>(qs, 32 * b, k, lane);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 ls = *reinterpret_cast<const f32x4*>(lse2 + 32 * b + 8 * j + 4 * half);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) p[4 * j + i] = exp2_fast(__builtin_fmaf(p[4 * j + i], c2, -ls[i]));
+            }
+            const bool edge = a.causal && qb < kw + 31;
+            if (edge) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (qb + 8 * (r / 4) + 4 * half + r % 4 < ki) p[r] = 0.f;
+            }
+            accumulate<T, DP>(gv, ds, 32 * b, p, lane);
+            f32x16 dp = scores<T, DP>(ds, 32 * b, v, lane);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 de = *reinterpret_cast<const f32x4*>(delta + 32 * b + 8 * j + 4 * half);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) dp[4 * j + i] = p[4 * j + i] * (dp[4 * j + i] - de[i]);
+            }
+            if (edge) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (qb + 8 * (r / 4) + 4 * half + r % 4 < ki) dp[r] = 0.f;
+            }
+            accumulate<T, DP>(gk, qs, 32 * b, dp, lane);
+        }
+        if (more) put((it + 1) & 1);
+    }
+    uint32_t bad = bad_rows(live && (any_nonfinite(gk) || any_nonfinite(gv)));
+    if (live && !(bad >> (lane & 31) & 1)) {
+        store_row<T, DP, VEC>(row_of<T>(a.dk, w, ki, kv), gk, a.scale, a.dim, half);
+        store_row<T, DP, VEC>(row_of<T>(a.dv, w, ki, kv), gv, 1.f, a.dim, half);
+    }
+    for (; bad; bad &= bad - 1) dkv_row<T>(a, w, kw + __builtin_ctz(bad), lane);
+}
+
+// -------------------------------------------------------------- launches ---
+template <class T>
+bool aligned(const AttnOperand& o) {
+    constexpr int E = 16 / sizeof(T);
+    return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.tok % E == 0 && o.head % E == 0;
+}
+
+template <class T, int DP, bool VEC>
+hipError_t run(const AttnArgs& a, bool backward, hipStream_t s) {
+    const unsigned n = (unsigned)a.num_tiles;
+    if (!backward) {
+        attn_fwd_kernel<T, DP, VEC><<<n * a.heads, kThreads, 0, s>>>(a);
+    } else {
+        attn_dq_kernel<T, DP, VEC><<<n * a.heads, kThreads, 0, s>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        attn_dkv_kernel<T, DP, VEC><<<n * a.kv_heads, kThreads, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+template <class T>
+hipError_t dispatch(const AttnArgs& a, bool backward, hipStream_t s) {
+    bool vec = a.dim % (16 / (int)sizeof(T)) == 0 && aligned<T>(a.q) && aligned<T>(a.k) && aligned<T>(a.v) &&
+               aligned<T>(a.out);
+    if (backward) vec = vec && aligned<T>(a.dout) && aligned<T>(a.dq) && aligned<T>(a.dk) && aligned<T>(a.dv);
+    if (a.dim <= 64) return vec ? run<T, 64, true>(a, backward, s) : run<T, 64, false>(a, backward, s);
+    return vec ? run<T, 128, true>(a, backward, s) : run<T, 128, false>(a, backward, s);
+}
+
+}  // namespace
+
+hipError_t launch_attention_forward(DType t, const AttnArgs& a, hipStream_t s) {
+    return t == DType::BF16 ? dispatch<bf16_t>(a, false, s) : dispatch<float>(a, false, s);
+}
+
+hipError_t launch_attention_backward(DType t, const AttnArgs& a, hipStream_t s) {
+    return t == DType::BF16 ? dispatch<bf16_t>(a, true, s) : dispatch<float>(a, true, s);
+}
+
+}  // namespace np

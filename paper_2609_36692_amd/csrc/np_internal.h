@@ -519,4 +519,8 @@ hipError_t launch_eig_select_dense(const EigArgs& a, const TriWork& w, double* l
 hipError_t launch_gemm_gram_f32(int layout, Operand A, Operand B, GemmShape sh, int batch, const EpiPartial& e,
                                 hipStream_t s);
 
+// Sets the calling thread's error message for entry points without a context
+// (normpre_last_error(NULL)); returns code.
+int set_thread_error(int code, const char* msg);
+
 }  // namespace np

@@ -68,6 +68,15 @@ NORMPRE_KCLASS_COUNT = 10
 KCLASS_NAMES = ["normalize", "ns_gram", "ns_poly", "ns_combine", "g_update",
                 "sk_stream", "sk_small", "l_apply", "eigen", "normalize_col"]
 
+NORMPRE_DTYPE_F32 = 0
+NORMPRE_DTYPE_BF16 = 1
+NORMPRE_CHECKPOINT_GROUP = 64
+NORMPRE_ACT_NONE = 0
+NORMPRE_ACT_GELU = 1
+NORMPRE_ACT_SWIGLU = 2
+NORMPRE_WEIGHT_INNER_OUTER = 0
+NORMPRE_WEIGHT_OUTER_INNER = 1
+
 
 class NormPreError(RuntimeError):
     def __init__(self, code: int, msg: str):
@@ -92,6 +101,30 @@ class normpre_hparams(ctypes.Structure):
         ("step", ctypes.c_int64),
         ("norm_eps", ctypes.c_float),
         ("flags", ctypes.c_uint32),
+    ]
+
+
+class normpre_heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class normpre_attention(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("causal", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("tokens", ctypes.c_int64),
+        ("plan", ctypes.c_void_p),
+        ("num_tiles", ctypes.c_int64),
+        ("q", normpre_heads), ("k", normpre_heads), ("v", normpre_heads),
+        ("out", normpre_heads),
+        ("lse", ctypes.c_void_p),
+        ("dout", normpre_heads),
+        ("dq", normpre_heads), ("dk", normpre_heads), ("dv", normpre_heads),
+        ("workspace", ctypes.c_void_p),
     ]
 
 
@@ -139,6 +172,23 @@ def load_library(path: str = LIB_PATH):
         "normpre_workspace_bytes": (ctypes.c_int, [P, i64p]),
         "normpre_step_noalloc": (ctypes.c_int, [P, ctypes.c_int, ctypes.c_int, ctypes.POINTER(P), ctypes.POINTER(P),
                                                 ctypes.POINTER(P), i64p, hpp, P]),
+        "normpre_attention_plan_tiles": (ctypes.c_int, [ctypes.c_int64, i64p, i64p]),
+        "normpre_attention_plan": (ctypes.c_int, [ctypes.c_int64, i64p, ctypes.c_int, P, ctypes.c_int64]),
+        "normpre_attention_forward": (ctypes.c_int, [ctypes.POINTER(normpre_attention), P]),
+        "normpre_attention_backward": (ctypes.c_int, [ctypes.POINTER(normpre_attention), P]),
+        "normpre_checkpoint_pack": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
+                                                   P, ctypes.c_int64, P, ctypes.c_int64, P, ctypes.c_int64,
+                                                   P, P, P, P, P, P, P]),
+        "normpre_checkpoint_unpack": (ctypes.c_int, [ctypes.c_int, ctypes.c_int64, ctypes.c_int64, P, P,
+                                                     P, ctypes.c_int64, P]),
+        "normpre_checkpoint_act_grad": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
+                                                       P, ctypes.c_int64, P, P, P, P, P, ctypes.c_int64,
+                                                       P, ctypes.c_int64, P]),
+        "normpre_checkpoint_weight_grad_workspace": (ctypes.c_int, [ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
+                                                                    ctypes.c_int64, i64p]),
+        "normpre_checkpoint_weight_grad": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64,
+                                                          ctypes.c_int64, ctypes.c_int64, P, P, P, ctypes.c_int64,
+                                                          P, ctypes.c_int64, P, ctypes.c_int64, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -350,6 +400,61 @@ def normpre_energy_split(eigs, count: int, rank: int) -> np.ndarray:
                                                int(rank), out.ctypes.data_as(ctypes.POINTER(ctypes.c_double)))
     _check(code)
     return out
+
+
+# ------------------------------------------------- training-step operators ---
+# The same names and argument order as the C ABI, on raw device pointers; the
+# tensor-level front end is ``train_ops``.
+def normpre_attention_plan(lens, causal: bool) -> np.ndarray:
+    """Plan of a packed batch as a host array int32 [2, tiles, 4]."""
+    n = len(lens)
+    arr = (ctypes.c_int64 * max(1, n))(*[int(v) for v in lens])
+    tiles = ctypes.c_int64()
+    lib = load_library()
+    _check(lib.normpre_attention_plan_tiles(n, arr, ctypes.byref(tiles)))
+    plan = np.zeros((2, tiles.value, 4), dtype=np.int32)
+    _check(lib.normpre_attention_plan(n, arr, int(bool(causal)), plan.ctypes.data_as(ctypes.c_void_p), plan.size))
+    return plan
+
+
+def normpre_attention_forward(args: normpre_attention, stream=None) -> None:
+    _check(load_library().normpre_attention_forward(ctypes.byref(args), _stream_handle(stream)))
+
+
+def normpre_attention_backward(args: normpre_attention, stream=None) -> None:
+    _check(load_library().normpre_attention_backward(ctypes.byref(args), _stream_handle(stream)))
+
+
+def normpre_checkpoint_pack(act: int, dtype: int, rows: int, cols: int, u, ld_u, up, ld_up, h, ld_h, u_codes, u_exps,
+                            up_codes, up_exps, h_codes, h_exps, stream=None) -> None:
+    _check(load_library().normpre_checkpoint_pack(act, dtype, rows, cols, u, ld_u, up, ld_up, h, ld_h, u_codes,
+                                                  u_exps, up_codes, up_exps, h_codes, h_exps,
+                                                  _stream_handle(stream)))
+
+
+def normpre_checkpoint_unpack(dtype: int, rows: int, cols: int, codes, exps, out, ld_out, stream=None) -> None:
+    _check(load_library().normpre_checkpoint_unpack(dtype, rows, cols, codes, exps, out, ld_out,
+                                                    _stream_handle(stream)))
+
+
+def normpre_checkpoint_act_grad(act: int, dtype: int, rows: int, cols: int, dh, ld_dh, u_codes, u_exps, up_codes,
+                                up_exps, du, ld_du, dup, ld_dup, stream=None) -> None:
+    _check(load_library().normpre_checkpoint_act_grad(act, dtype, rows, cols, dh, ld_dh, u_codes, u_exps, up_codes,
+                                                      up_exps, du, ld_du, dup, ld_dup, _stream_handle(stream)))
+
+
+def normpre_checkpoint_weight_grad_workspace(dtype: int, tokens: int, inner: int, outer: int) -> int:
+    out = ctypes.c_int64()
+    _check(load_library().normpre_checkpoint_weight_grad_workspace(dtype, tokens, inner, outer, ctypes.byref(out)))
+    return out.value
+
+
+def normpre_checkpoint_weight_grad(dtype: int, layout: int, accumulate: bool, tokens: int, inner: int, outer: int,
+                                   codes, exps, dy, ld_dy, dw, ld_dw, workspace, workspace_bytes,
+                                   stream=None) -> None:
+    _check(load_library().normpre_checkpoint_weight_grad(dtype, layout, int(bool(accumulate)), tokens, inner, outer,
+                                                         codes, exps, dy, ld_dy, dw, ld_dw, workspace,
+                                                         workspace_bytes, _stream_handle(stream)))
 
 
 class NormPre:

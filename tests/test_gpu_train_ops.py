@@ -1,0 +1,628 @@
+"""Training-step operators on the GPU against 64-bit references: packed
+attention and its backward pass, 8-bit activation checkpoints and the gradients
+that read them.  Bounds: tests/train_ops_util.py."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2609_36692_amd import normpre as N  # noqa: E402
+from paper_2609_36692_amd import train_ops as T  # noqa: E402
+from train_ops_util import (H, U, act_grad_reference, act_reference, assert_within, attention_reference,  # noqa: E402
+                            decode_reference, encode_reference)
+
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def dev():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch.device("cuda:0")
+
+
+def _gen(dev, seed):
+    g = torch.Generator(device=dev)
+    g.manual_seed(seed)
+    return g
+
+
+def _qkv(dev, seed, t, hq, hk, d, dtype):
+    g = _gen(dev, seed)
+    return [torch.randn(t, h, d, generator=g, device=dev).to(dtype) for h in (hq, hk, hk, hq)]
+
+
+def _check(q, k, v, dout, lens, causal, scale=None):
+    c = 1.0 / math.sqrt(q.shape[2]) if scale is None else scale
+    plan = T.AttentionPlan(lens, causal, q.device)
+    out, lse = T.attention_forward(q, k, v, plan, scale)
+    dq, dk, dv = T.attention_backward(dout, q, k, v, out, lse, plan, scale)
+    want, tol = attention_reference(q, k, v, lens, causal, c, dout)
+    r = 1 if q.dtype == BF16 else 0
+    for name, got in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        assert got.dtype == (F32 if name == "lse" else q.dtype)
+        assert_within(name, got, want[name], tol[name][r])
+    return out, lse, dq, dk, dv
+
+
+# ------------------------------------------------------------- attention ---
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("lens,hq,hk,d,causal", [
+    ([1], 1, 1, 64, True),
+    ([1, 2, 3, 31, 32, 33], 2, 1, 64, True),
+    ([63, 64, 65, 0, 1], 3, 3, 64, True),
+    ([127, 128, 129], 4, 2, 128, True),
+    ([257], 2, 1, 128, True),
+    ([100, 130], 2, 2, 128, False),
+    ([5, 300], 1, 1, 64, False),
+    ([40, 70], 8, 2, 40, True),
+    ([150], 3, 1, 7, True),
+    ([33, 66], 2, 1, 96, True),
+    ([50], 5, 1, 1, True),
+    ([90], 2, 2, 127, False),
+])
+def test_attention_matches_reference(dev, dtype, lens, hq, hk, d, causal):
+    print(f"attention {dtype} {lens} {hq}/{hk}x{d} causal={causal}", flush=True)
+    q, k, v, dout = _qkv(dev, 1 + sum(lens), sum(lens), hq, hk, d, dtype)
+    _check(q, k, v, dout, lens, causal)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
+def test_attention_scales(dev, dtype, scale):
+    q, k, v, dout = _qkv(dev, 5, 97, 2, 1, 64, dtype)
+    _check(q, k, v, dout, [60, 37], True, scale)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["fused", "head_major", "odd_stride", "misaligned", "expanded", "feature_major"])
+def test_attention_strides(dev, dtype, layout):
+    lens, hq, hk, d = [70, 1, 60], 4, 2, 64
+    t = sum(lens)
+    q, k, v, dout = _qkv(dev, 11, t, hq, hk, d, dtype)
+    if layout == "fused":
+        buf = torch.cat([x.flatten(1) for x in (q, k, v)], 1)
+        q, k, v = (x.unflatten(1, (-1, d)) for x in buf.split([hq * d, hk * d, hk * d], 1))
+    elif layout == "head_major":
+        q, k, v, dout = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v, dout))
+    elif layout == "odd_stride":
+        q, k, v, dout = (torch.nn.functional.pad(x, (0, 3))[:, :, :d] for x in (q, k, v, dout))
+    elif layout == "misaligned":
+        q, k, v, dout = (torch.nn.functional.pad(x.flatten(), (1, 0))[1:].view(x.shape) for x in (q, k, v, dout))
+    elif layout == "expanded":
+        k, v = (x[:, :1].expand(t, hk, d) for x in (k, v))
+    else:
+        q, k, v, dout = (x.transpose(1, 2).contiguous().transpose(1, 2) for x in (q, k, v, dout))
+    _check(q, k, v, dout, lens, True)
+
+
+def test_attention_extreme_scores(dev):
+    # Scores of hundreds: a row's weights fall on one or two keys.
+    q, k, v, dout = _qkv(dev, 21, 140, 2, 2, 64, F32)
+    _check(8 * q, 8 * k, v, dout, [140], True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention_long_rows(dev, dtype):
+    # A sequence of many tiles.
+    lens, hq, hk, d = [1500, 37], 2, 1, 64
+    q, k, v, dout = _qkv(dev, 31, sum(lens), hq, hk, d, dtype)
+    _check(q, k, v, dout, lens, True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("where", ["q", "k", "v", "dout"])
+def test_attention_nonfinite_stays_with_rows_that_see_it(dev, dtype, d, value, where):
+    # In the middle of a diagonal tile of the second sequence, one head.
+    lens, hq, hk = [50, 150, 40], 2, 1
+    x = dict(zip(("q", "k", "v", "dout"), _qkv(dev, 41, sum(lens), hq, hk, d, dtype)))
+    at = 50 + 77
+    x[where][at, 0, 3] = value
+    out, lse, dq, dk, dv = _check(**x, lens=lens, causal=True)
+    # No row before it in its sequence and no other sequence is touched.
+    others = torch.tensor([i for i in range(sum(lens)) if i < 50 or i >= 200], device=dev)
+    before = torch.arange(50, at, device=dev)
+    for y in (out, dq):
+        assert torch.isfinite(y[others]).all() and torch.isfinite(y[before]).all()
+    for y in (dk, dv):
+        assert torch.isfinite(y[others]).all()
+
+
+def test_attention_all_scores_minus_infinity(dev):
+    # Formula of a row whose scores are all -inf: 0 / 0.
+    q = torch.ones(4, 1, 64, device=dev)
+    k = torch.full((4, 1, 64), float("-inf"), device=dev)
+    v = torch.ones(4, 1, 64, device=dev)
+    out, _ = T.attention_forward(q, k, v, T.AttentionPlan([4], True, dev))
+    assert torch.isnan(out).all()
+
+
+def test_attention_empty_batch(dev):
+    for lens in ([], [0], [0, 0, 0]):
+        plan = T.AttentionPlan(lens, True, dev)
+        q = torch.empty(0, 4, 64, device=dev, dtype=BF16, requires_grad=True)
+        k = torch.empty(0, 2, 64, device=dev, dtype=BF16, requires_grad=True)
+        out = T.attention(q, k, k, plan)
+        assert out.shape == q.shape
+        out.sum().backward()
+        assert q.grad.shape == q.shape
+
+
+def test_attention_offsets_past_32_bits(dev):
+    # Rows 24 MB apart: element offsets reach 2.5e9.
+    lens, hq, hk, d, pitch = [130, 70], 2, 1, 64, 12_500_000
+    t = sum(lens)
+    q, k, v, dout = _qkv(dev, 51, t, hq, hk, d, BF16)
+    want = _check(q, k, v, dout, lens, True)
+    buf = torch.empty(t * pitch, dtype=BF16, device=dev)
+    far, at = [], 0
+    for x in (q, k, v, dout):
+        y = buf.as_strided(x.shape, (pitch, d, 1), at)
+        y.copy_(x)
+        far.append(y)
+        at += x.shape[1] * d
+    plan = T.AttentionPlan(lens, True, dev)
+    out, lse = T.attention_forward(*far[:3], plan)
+    got = (out, lse, *T.attention_backward(far[3], *far[:3], out, lse, plan))
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_attention_is_reproducible(dev):
+    lens = [300, 17, 211]
+    q, k, v, dout = _qkv(dev, 61, sum(lens), 8, 2, 128, BF16)
+    plan = T.AttentionPlan(lens, True, dev)
+    runs = []
+    for _ in range(3):
+        out, lse = T.attention_forward(q, k, v, plan)
+        runs.append((out, lse, *T.attention_backward(dout, q, k, v, out, lse, plan)))
+    for r in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(r, runs[0]))
+
+
+def test_attention_of_a_packed_batch_equals_its_sequences(dev):
+    lens = [40, 129, 7]
+    q, k, v, _ = _qkv(dev, 71, sum(lens), 4, 4, 64, BF16)
+    out, lse = T.attention_forward(q, k, v, T.AttentionPlan(lens, True, dev))
+    at = 0
+    for n in lens:
+        s = slice(at, at + n)
+        o, l = T.attention_forward(q[s], k[s], v[s], T.AttentionPlan([n], True, dev))
+        assert torch.equal(o, out[s]) and torch.equal(l, lse[:, s])
+        at += n
+
+
+def test_attention_gradient_against_differences(dev):
+    # d/dt of sum(w * out) along random directions, by central differences of the
+    # fp32 forward kernel (the loss summed in fp64).  Step 2^-7: the third
+    # derivative's term is below step^2 * |direction|^3-ish = 1e-3 of the slope
+    # here, the rounding of the outputs (1e-6 of them) over the step 2e-4.
+    lens = [37, 70]
+    q, k, v, w = _qkv(dev, 81, sum(lens), 4, 2, 64, F32)
+    plan = T.AttentionPlan(lens, True, dev)
+    xs = [x.requires_grad_() for x in (q, k, v)]
+    (w * T.attention(*xs, plan)).sum().backward()
+    g = _gen(dev, 82)
+    step = 2.0 ** -7
+    for i in range(3):
+        r = torch.randn(xs[i].shape, generator=g, device=dev)
+        ends = []
+        for sign in (1, -1):
+            moved = [x.detach() + (sign * step * r if j == i else 0) for j, x in enumerate(xs)]
+            ends.append((w.double() * T.attention_forward(*moved, plan)[0].double()).sum().item())
+        slope = (ends[0] - ends[1]) / (2 * step)
+        want = (xs[i].grad.double() * r.double()).sum().item()
+        scale = (xs[i].grad.double().norm() * r.double().norm()).item() / math.sqrt(r.numel())
+        assert abs(slope - want) <= 3e-3 * max(abs(want), scale), (i, slope, want)
+
+
+def test_attention_autograd_matches_calls(dev):
+    lens = [90, 45]
+    q, k, v, dout = _qkv(dev, 91, sum(lens), 4, 2, 64, BF16)
+    plan = T.AttentionPlan(lens, True, dev)
+    out, lse = T.attention_forward(q, k, v, plan)
+    want = T.attention_backward(dout, q, k, v, out, lse, plan)
+    xs = [x.clone().requires_grad_() for x in (q, k, v)]
+    y = T.attention(*xs, plan)
+    assert torch.equal(y, out)
+    y.backward(dout)
+    for x, g in zip(xs, want):
+        assert torch.equal(x.grad, g)
+
+
+# ----------------------------------------------------------- checkpoints ---
+def _activations(dev, seed, rows, cols, dtype):
+    g = _gen(dev, seed)
+    x = torch.randn(rows, cols, generator=g, device=dev) * torch.exp(torch.randn(cols, generator=g, device=dev))
+    return x.to(dtype)
+
+
+def _special(dev, dtype):
+    """Rows of one group each, and one of two groups of which the second is short."""
+    rows = [[0.0], [1e-45], [2.0 ** -126], [2.0 ** -140, -(2.0 ** -127)], [127.0, 63.5, 0.5, -0.5, 1.5, 2.5],
+            [127.5, 1.0], [127.49999, -127.4], [1.0, 2.0 ** -8, 2.0 ** -9], [3.3895314e38, 1.0],
+            [-3.3895314e38, 3.0e38], [float("nan"), 1.0], [float("inf"), 1.0], [-float("inf"), float("nan")],
+            [255.0, 1.0, 3.0, 5.0], [-128.0, 64.0]]
+    x = torch.zeros(len(rows), 70)
+    for i, r in enumerate(rows):
+        x[i, :len(r)] = torch.tensor(r)
+        x[i, 66] = i - 7.25
+    return x.to(device=dev, dtype=dtype)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 64), (3, 65), (7, 127), (5, 128), (130, 200), (33, 1000)])
+def test_pack_matches_definition(dev, dtype, rows, cols):
+    x = _activations(dev, 3 + rows + cols, rows, cols, dtype)
+    c = T.checkpoint_pack(x)
+    codes, exps = encode_reference(x)
+    assert np.array_equal(c.codes.cpu().numpy(), codes)
+    assert np.array_equal(c.exps.cpu().numpy(), exps)
+    want = decode_reference(codes, exps, cols)
+    for out in (BF16, F32):
+        y = T.checkpoint_unpack(c, out)
+        assert y.dtype == out and np.array_equal(y.double().cpu().numpy(), want)
+    # Half a step at most, and a step is at most amax / 63.
+    top = np.repeat(np.abs(np.pad(x.double().cpu().numpy(), ((0, 0), (0, -cols % 64)))).reshape(rows, -1, 64)
+                    .max(2), 64, axis=1)[:, :cols]
+    assert (np.abs(x.double().cpu().numpy() - want) <= top / 126).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_pack_special_groups(dev, dtype):
+    x = _special(dev, dtype)
+    c = T.checkpoint_pack(x)
+    codes, exps = encode_reference(x)
+    assert np.array_equal(c.codes.cpu().numpy(), codes)
+    assert np.array_equal(c.exps.cpu().numpy(), exps)
+    for out in (BF16, F32):
+        y = T.checkpoint_unpack(c, out).double().cpu().numpy()
+        want = decode_reference(codes, exps, x.shape[1])
+        assert np.array_equal(np.isnan(y), np.isnan(want)) and np.array_equal(y[~np.isnan(y)], want[~np.isnan(want)])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("how", ["strided", "odd_stride", "misaligned", "transposed", "expanded"])
+def test_pack_strides(dev, dtype, how):
+    x = _activations(dev, 9, 50, 150, dtype)
+    if how == "strided":
+        y = torch.zeros(50, 400, dtype=dtype, device=dev)[:, 40:190]
+    elif how == "odd_stride":
+        y = torch.zeros(50, 153, dtype=dtype, device=dev)[:, :150]
+    elif how == "misaligned":
+        y = torch.zeros(50 * 150 + 1, dtype=dtype, device=dev)[1:].view(50, 150)
+    elif how == "transposed":
+        y = torch.zeros(150, 50, dtype=dtype, device=dev).t()
+    else:
+        x = x[:1].expand(50, 150)
+        y = x
+    if how != "expanded":
+        y.copy_(x)
+    a, b = T.checkpoint_pack(x.contiguous()), T.checkpoint_pack(y)
+    assert torch.equal(a.codes, b.codes) and torch.equal(a.exps, b.exps)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("rows,cols", [(1, 3), (4, 64), (37, 130), (64, 777)])
+def test_act_and_its_checkpoints(dev, dtype, act, rows, cols):
+    u = _activations(dev, 17, rows, cols, dtype)
+    up = _activations(dev, 18, rows, cols, dtype) if act == "swiglu" else None
+    h, cu, cup, ch = T.checkpoint_act(act, u, up)
+    ud = u.double().cpu().numpy()
+    want = act_reference(act, ud, None if up is None else up.double().cpu().numpy())
+    # The logistic function's argument is off by 4 u relative, so the result by
+    # |z| 4 u + 8 u relative; then the rounding to the type.
+    z = np.abs(1.6 * (np.abs(ud) + 0.045 * np.abs(ud) ** 3)) if act == "gelu" else np.abs(ud)
+    half = H if dtype == BF16 else 0.0
+    assert_within("h", h, want, np.abs(want) * ((4 * z + 8) * U + half) + 1e-38)
+    for c, x in ((cu, u), (cup, up), (ch, h)):
+        if x is None:
+            assert c is None
+            continue
+        codes, exps = encode_reference(x)
+        assert np.array_equal(c.codes.cpu().numpy(), codes) and np.array_equal(c.exps.cpu().numpy(), exps)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("rows,cols", [(1, 3), (4, 64), (37, 130), (64, 777)])
+def test_act_grad(dev, dtype, act, rows, cols):
+    cu = T.checkpoint_pack(_activations(dev, 27, rows, cols, dtype))
+    cup = T.checkpoint_pack(_activations(dev, 28, rows, cols, dtype)) if act == "swiglu" else None
+    dh = _activations(dev, 29, rows, cols, dtype)
+    u = decode_reference(cu.codes, cu.exps, cols)
+    up = None if cup is None else decode_reference(cup.codes, cup.exps, cols)
+    d = dh.double().cpu().numpy()
+    du, dup = T.checkpoint_act_grad(act, dh, cu, cup)
+    want, want_up = act_grad_reference(act, d, u, up)
+    half = H if dtype == BF16 else 0.0
+    # Terms of the sum in the derivative, each off by (4 |z| + 16) u relative; the
+    # second factor |u z'| is at most |z| of a cubic, 3 times it.
+    z = np.abs(1.6 * (np.abs(u) + 0.045 * np.abs(u) ** 3)) if act == "gelu" else np.abs(u)
+    mag = np.abs(d) * (1 + 3 * z) * (1.0 if up is None else np.abs(up))
+    assert_within("du", du, want, (4 * z + 16) * U * mag + half * np.abs(want) + 1e-38)
+    if cup is not None:
+        assert_within("dup", dup, want_up, (4 * z + 16) * U * np.abs(d * u) + half * np.abs(want_up) + 1e-38)
+
+
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+def test_act_grad_against_differences(dev, act):
+    # Central differences of the activation at the held values, in 64 bits: step
+    # 2^-12, third derivatives below 4 here, so the error is below 4 2^-24 / 6,
+    # plus that of the kernel's fp32 result.
+    cu = T.checkpoint_pack(torch.linspace(-6, 6, 320, device=dev).view(5, 64))
+    cup = T.checkpoint_pack(torch.linspace(3, -2, 320, device=dev).view(5, 64)) if act == "swiglu" else None
+    u = decode_reference(cu.codes, cu.exps, 64)
+    up = None if cup is None else decode_reference(cup.codes, cup.exps, 64)
+    dh = torch.ones(5, 64, device=dev)
+    du, dup = T.checkpoint_act_grad(act, dh, cu, cup)
+    s = 2.0 ** -12
+    slope = (act_reference(act, u + s, up) - act_reference(act, u - s, up)) / (2 * s)
+    assert np.abs(du.double().cpu().numpy() - slope).max() <= 4e-6
+    if dup is not None:
+        slope = (act_reference(act, u, up + s) - act_reference(act, u, up - s)) / (2 * s)
+        assert np.abs(dup.double().cpu().numpy() - slope).max() <= 4e-6
+
+
+def _weight_bound(x, d, tokens):
+    """Every product is exact: only the sums round."""
+    return (tokens + 8) * U * (np.abs(x).T @ np.abs(d)) + 1e-38
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["io", "oi"])
+@pytest.mark.parametrize("tokens,inner,outer", [
+    (1, 1, 1), (2, 64, 64), (31, 65, 129), (64, 128, 128), (100, 257, 100), (700, 130, 300), (1100, 70, 33),
+    (4099, 200, 136),
+])
+def test_weight_grad(dev, dtype, layout, tokens, inner, outer):
+    print(f"weight_grad {dtype} {layout} {tokens} {inner} {outer}", flush=True)
+    c = T.checkpoint_pack(_activations(dev, 37, tokens, inner, dtype))
+    dy = _activations(dev, 38, tokens, outer, dtype)
+    x, d = decode_reference(c.codes, c.exps, inner), dy.double().cpu().numpy()
+    want, tol = x.T @ d, _weight_bound(x, d, tokens)
+    if layout == "oi":
+        want, tol = want.T, tol.T
+    got = T.checkpoint_weight_grad(c, dy, layout)
+    assert_within("dw", got, want, tol)
+    assert torch.equal(got, T.checkpoint_weight_grad(c, dy, layout))
+    # Into a part of a larger matrix, added to what is there.
+    big = torch.full((got.shape[0] + 2, got.shape[1] + 5), 3.0, device=dev)
+    part = big[1:-1, 2:-3]
+    T.checkpoint_weight_grad(c, dy, layout, out=part, accumulate=True)
+    assert_within("accumulated", part, want + 3.0, tol + U * (np.abs(want) + 3.0) * 2)
+    big[1:-1, 2:-3] = 3.0
+    assert (big == 3.0).all()
+
+
+@pytest.mark.parametrize("how", ["strided", "odd_stride", "misaligned", "transposed"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_weight_grad_strides(dev, dtype, how):
+    c = T.checkpoint_pack(_activations(dev, 47, 90, 70, dtype))
+    dy = _activations(dev, 48, 90, 150, dtype)
+    y = {"strided": lambda: torch.zeros(90, 400, dtype=dtype, device=dev)[:, 40:190],
+         "odd_stride": lambda: torch.zeros(90, 153, dtype=dtype, device=dev)[:, :150],
+         "misaligned": lambda: torch.zeros(90 * 150 + 1, dtype=dtype, device=dev)[1:].view(90, 150),
+         "transposed": lambda: torch.zeros(150, 90, dtype=dtype, device=dev).t()}[how]()
+    y.copy_(dy)
+    assert torch.equal(T.checkpoint_weight_grad(c, y), T.checkpoint_weight_grad(c, dy))
+
+
+def test_weight_grad_of_no_tokens(dev):
+    c = T.checkpoint_pack(torch.empty(0, 70, device=dev))
+    dy = torch.empty(0, 30, device=dev)
+    assert (T.checkpoint_weight_grad(c, dy, "io") == 0).all()
+    out = torch.ones(30, 70, device=dev)
+    T.checkpoint_weight_grad(c, dy, "oi", out=out, accumulate=True)
+    assert (out == 1).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_weight_grad_nonfinite(dev, dtype):
+    # A NaN in x reaches the 64 features of its group, an infinity in dy its column.
+    x, dy = _activations(dev, 57, 40, 200, dtype), _activations(dev, 58, 40, 90, dtype)
+    x[7, 70] = float("nan")
+    dy[9, 5] = float("inf")
+    c = T.checkpoint_pack(x)
+    got = T.checkpoint_weight_grad(c, dy, "io").cpu()
+    bad = torch.zeros(200, 90, dtype=torch.bool)
+    bad[64:128] = True
+    bad[:, 5] = True
+    assert torch.equal(~torch.isfinite(got), bad)
+    # Past the infinity only the sign of the code counts.
+    held = torch.from_numpy(decode_reference(c.codes, c.exps, 200)[9])
+    col = got[:, 5]
+    keep = torch.ones(200, dtype=torch.bool)
+    keep[64:128] = False
+    assert torch.equal(col[keep & (held > 0)], torch.full_like(col[keep & (held > 0)], float("inf")))
+    assert torch.equal(col[keep & (held < 0)], torch.full_like(col[keep & (held < 0)], float("-inf")))
+
+
+def test_weight_grad_fp32_terms(dev):
+    # One token: every product of a code and an fp32 value with all 24 bits set,
+    # over the whole range of exponents, is within one rounding.
+    g = _gen(dev, 67)
+    x = torch.zeros(1, 64, device=dev)
+    x[0, 0], x[0, 1] = 127.0, 1.0
+    dy = torch.randn(1, 500, generator=g, device=dev) * 2.0 ** torch.linspace(-90, 110, 500, device=dev)
+    got = T.checkpoint_weight_grad(T.checkpoint_pack(x), dy, "io").double()
+    for i, c in ((0, 127.0), (1, 1.0)):
+        want = c * dy[0].double()
+        assert ((got[i] - want).abs() <= 3 * U * want.abs()).all()
+
+
+# ------------------------------------------------------------------ layers ---
+@pytest.mark.parametrize("layout", ["io", "oi"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_checkpointed_linear(dev, dtype, layout):
+    g = _gen(dev, 77)
+    x = torch.randn(130, 96, generator=g, device=dev).to(dtype).requires_grad_()
+    w = (torch.randn(*((96, 200) if layout == "io" else (200, 96)), generator=g, device=dev) * 0.1).requires_grad_()
+    b = torch.randn(200, generator=g, device=dev).requires_grad_()
+    dy = torch.randn(130, 200, generator=g, device=dev).to(dtype)
+    y = T.checkpointed_linear(x, w, b, layout)
+    y.backward(dy)
+    c = T.checkpoint_pack(x.detach())
+    wt = w.detach().to(dtype)
+    assert torch.equal(y, (x.detach() @ (wt if layout == "io" else wt.t())) + b.detach().to(dtype))
+    assert torch.equal(w.grad, T.checkpoint_weight_grad(c, dy, layout))
+    assert torch.equal(x.grad, dy @ (wt.t() if layout == "io" else wt))
+    assert torch.equal(b.grad, dy.sum(0, dtype=F32))
+
+
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
+@pytest.mark.parametrize("layout", ["io", "oi"])
+def test_checkpointed_mlp_against_formula(dev, act, layout):
+    # fp32, against the formula in 64 bits with the held values in place of the
+    # activations (that of h and the checkpoints come from the kernels' own h).
+    g = _gen(dev, 87)
+    t, n, m = 70, 64, 160
+    shape = lambda a, b: (a, b) if layout == "io" else (b, a)  # noqa: E731
+    x = torch.randn(t, n, generator=g, device=dev).requires_grad_()
+    w1, w3 = ((torch.randn(*shape(n, m), generator=g, device=dev) * 0.1).requires_grad_() for _ in range(2))
+    w2 = (torch.randn(*shape(m, n), generator=g, device=dev) * 0.1).requires_grad_()
+    gated = act == "swiglu"
+    b1, b2 = (None, None) if gated else (torch.randn(k, generator=g, device=dev).requires_grad_() for k in (m, n))
+    dy = torch.randn(t, n, generator=g, device=dev)
+    y = T.checkpointed_mlp(x, w1, w2, act=act, w_up=w3 if gated else None, b_in=b1, b_out=b2, layout=layout)
+    y.backward(dy)
+    D = lambda z: z.detach().double().cpu().numpy()  # noqa: E731
+    W = lambda z: D(z) if layout == "io" else D(z).T  # noqa: E731
+    u = D(x) @ W(w1) + (0 if gated else D(b1))
+    up = D(x) @ W(w3) if gated else None
+    h = act_reference(act, u, up)
+    held = lambda z: decode_reference(*encode_reference(torch.from_numpy(z)), z.shape[1])  # noqa: E731
+    dh = D(dy) @ W(w2).T
+    du, dup = act_grad_reference(act, dh, held(u), held(up) if gated else None)
+    want = {"dx": du @ W(w1).T + (dup @ W(w3).T if gated else 0), "w1": held(D(x)).T @ du, "w2": held(h).T @ D(dy)}
+    got = {"dx": D(x.grad), "w1": W(w1.grad), "w2": W(w2.grad)}
+    if gated:
+        want["w3"], got["w3"] = held(D(x)).T @ dup, W(w3.grad)
+    else:
+        want |= {"b1": du.sum(0), "b2": D(dy).sum(0)}
+        got |= {"b1": D(b1.grad), "b2": D(b2.grad)}
+    np.testing.assert_allclose(D(y), h @ W(w2) + (0 if gated else D(b2)), rtol=0, atol=1e-5)
+    for name in want:
+        # A value beside a tie may round to the next code: at most a step of
+        # amax / 63 at a few places; fp32 elsewhere.
+        err = np.linalg.norm(got[name] - want[name]) / np.linalg.norm(want[name])
+        assert err <= 1e-3, (name, err)
+
+
+def test_checkpointed_layers_keep_8_bits(dev):
+    x = torch.randn(256, 128, device=dev).requires_grad_()
+    w = torch.randn(512, 128, device=dev).requires_grad_()
+    kept = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(t) or t, lambda t: t):
+        T.checkpointed_linear(x, w)
+    kept = [t for t in kept if t.data_ptr() != w.data_ptr()]
+    assert sum(t.numel() * t.element_size() for t in kept) == 256 * (128 + 2)
+
+
+# ---------------------------------------------------- streams and graphs ---
+def test_operators_on_a_side_stream(dev):
+    s = torch.cuda.Stream()
+    lens = [200, 56]
+    with torch.cuda.stream(s):
+        # Inputs made on the stream, used on it without a wait.
+        torch.cuda._sleep(20_000_000)
+        q, k, v, dout = _qkv(dev, 97, sum(lens), 4, 2, 64, BF16)
+        plan = T.AttentionPlan(lens, True, dev)
+        out, lse = T.attention_forward(q, k, v, plan)
+        grads = T.attention_backward(dout, q, k, v, out, lse, plan)
+        h, cu, _, ch = T.checkpoint_act("gelu", q.flatten(1))
+        du, _ = T.checkpoint_act_grad("gelu", dout.flatten(1), cu)
+        dw = T.checkpoint_weight_grad(ch, dout.flatten(1))
+    s.synchronize()
+    out2, lse2 = T.attention_forward(q, k, v, plan)
+    assert torch.equal(out, out2)
+    for a, b in zip(grads, T.attention_backward(dout, q, k, v, out2, lse2, plan)):
+        assert torch.equal(a, b)
+    h2, cu2, _, ch2 = T.checkpoint_act("gelu", q.flatten(1))
+    assert torch.equal(h, h2)
+    assert torch.equal(du, T.checkpoint_act_grad("gelu", dout.flatten(1), cu2)[0])
+    assert torch.equal(dw, T.checkpoint_weight_grad(ch2, dout.flatten(1)))
+
+
+def test_operators_in_a_graph(dev):
+    lens = [200, 56, 700]
+    q, k, v, dout = _qkv(dev, 107, sum(lens), 4, 2, 64, BF16)
+    plan = T.AttentionPlan(lens, True, dev)
+
+    def step():
+        out, lse = T.attention_forward(q, k, v, plan)
+        grads = T.attention_backward(dout, q, k, v, out, lse, plan)
+        h, cu, cup, ch = T.checkpoint_act("swiglu", q.flatten(1), dout.flatten(1))
+        du, dup = T.checkpoint_act_grad("swiglu", dout.flatten(1), cu, cup)
+        return (out, *grads, h, du, dup, T.checkpoint_weight_grad(ch, out.flatten(1)))
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        got = step()
+    for r in range(3):
+        q.mul_(-0.7).add_(0.01)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b), r
+
+
+# ---------------------------------------------------------------- refusals ---
+def test_refusals(dev):
+    q, k, v, dout = _qkv(dev, 117, 20, 4, 2, 64, BF16)
+    plan = T.AttentionPlan([20], True, dev)
+    out, lse = T.attention_forward(q, k, v, plan)
+    with pytest.raises(ValueError):
+        T.attention_forward(q, k, v, T.AttentionPlan([19], True, dev))
+    with pytest.raises(ValueError):
+        T.attention_forward(q, k.float(), v, plan)
+    with pytest.raises(ValueError):
+        T.attention_forward(q, k[:, :, :32], v, plan)
+    with pytest.raises(TypeError):
+        T.attention_forward(q.half(), k.half(), v.half(), plan)
+    with pytest.raises(N.NormPreError) as e:
+        T.attention_forward(q[:, :3], k, v, plan)
+    assert e.value.code == N.NORMPRE_ERR_INVALID_ARG
+    with pytest.raises(N.NormPreError) as e:
+        T.attention_forward(*(x.repeat(1, 1, 3) for x in (q, k, v)), plan)
+    assert e.value.code == N.NORMPRE_ERR_UNSUPPORTED
+    with pytest.raises(N.NormPreError):
+        T.attention_forward(q, k, v, plan, float("nan"))
+    with pytest.raises(ValueError):
+        T.attention_backward(dout[:10], q, k, v, out, lse, plan)
+    with pytest.raises(ValueError):
+        T.attention_backward(dout, q, k, v, out, lse[:, :10], plan)
+    with pytest.raises(N.NormPreError) as e:
+        T.AttentionPlan([3, -1], True, dev)
+    assert e.value.code == N.NORMPRE_ERR_INVALID_ARG
+    with pytest.raises(ValueError):
+        T.checkpoint_act("relu", q.flatten(1))
+    c = T.checkpoint_pack(q.flatten(1))
+    with pytest.raises(ValueError):
+        T.checkpoint_weight_grad(c, dout.flatten(1)[:10])
+    with pytest.raises(ValueError):
+        T.checkpoint_weight_grad(c, dout.flatten(1), "xy")
+    with pytest.raises(ValueError):
+        T.checkpoint_weight_grad(c, dout.flatten(1), out=torch.empty(3, 3, device=dev))
+    with pytest.raises(ValueError):
+        T.checkpoint_act_grad("gelu", dout.flatten(1)[:, :100], c)
+    with pytest.raises(ValueError):
+        T.checkpoint_act_grad("swiglu", dout.flatten(1), c)
+    with pytest.raises(ValueError):
+        T.checkpoint_pack(q)
+    with pytest.raises(TypeError):
+        T.checkpoint_pack(q.flatten(1).half())
+    with pytest.raises(TypeError):
+        T.checkpoint_unpack(c, torch.float16)

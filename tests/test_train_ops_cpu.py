@@ -1,0 +1,168 @@
+"""Training-step operators without a GPU: the plan of a packed batch, and the
+refusals of the C ABI, which come before anything is launched."""
+import ctypes
+import os
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2609_36692_amd import normpre as N  # noqa: E402
+
+INVALID, UNSUPPORTED = N.NORMPRE_ERR_INVALID_ARG, N.NORMPRE_ERR_UNSUPPORTED
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    if not os.path.exists(N.LIB_PATH):
+        from paper_2609_36692_amd import _build
+        _build.build_library()
+    return N.load_library()
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("lens", [[], [0], [1], [128], [129], [300, 0, 1, 128, 1000], [5] * 40])
+def test_plan_covers_every_row_once_by_falling_work(lens, causal):
+    plan = N.normpre_attention_plan(lens, causal)
+    starts = np.cumsum([0] + lens)
+    for side in range(2):
+        rows = np.zeros(sum(lens), int)
+        work = []
+        for start, n, tile, zero in plan[side].tolist():
+            i = [j for j, s in enumerate(starts[:-1]) if s == start and lens[j] == n][0]
+            assert zero == 0 and n > 0 and 0 <= 128 * tile < n
+            end = min(n, 128 * (tile + 1))
+            rows[starts[i] + 128 * tile:starts[i] + end] += 1
+            work.append(n if not causal else end if side == 0 else n - 128 * tile)
+        assert (rows == 1).all()
+        assert work == sorted(work, reverse=True)
+
+
+def test_plan_refusals(lib):
+    tiles = ctypes.c_int64()
+    one = (ctypes.c_int64 * 2)(1, -1)
+    assert lib.normpre_attention_plan_tiles(2, one, ctypes.byref(tiles)) == INVALID
+    assert "negative" in N.normpre_last_error()
+    assert lib.normpre_attention_plan_tiles(1, None, ctypes.byref(tiles)) == INVALID
+    assert lib.normpre_attention_plan_tiles(-1, one, ctypes.byref(tiles)) == INVALID
+    assert lib.normpre_attention_plan_tiles(1, one, None) == INVALID
+    big = (ctypes.c_int64 * 2)(2 ** 31 - 1, 1)
+    assert lib.normpre_attention_plan_tiles(2, big, ctypes.byref(tiles)) == UNSUPPORTED
+    assert lib.normpre_attention_plan_tiles(1, (ctypes.c_int64 * 1)(2 ** 62), ctypes.byref(tiles)) == UNSUPPORTED
+    buf = (ctypes.c_int32 * 8)()
+    ok = (ctypes.c_int64 * 1)(100)
+    assert lib.normpre_attention_plan(1, ok, 1, buf, 7) == INVALID
+    assert lib.normpre_attention_plan(1, ok, 2, buf, 8) == INVALID
+    assert lib.normpre_attention_plan(1, ok, 1, None, 8) == INVALID
+    assert lib.normpre_attention_plan(1, ok, 1, buf, 8) == 0
+
+
+def _block(**over):
+    """A valid argument block on pointers that nothing may touch."""
+    at = 1 << 40
+    rows = lambda i, h: N.normpre_heads(at + (i << 30), h * 64, 64)  # noqa: E731
+    a = N.normpre_attention(dtype=1, heads=4, kv_heads=2, head_dim=64, causal=1, scale=0.125, tokens=100, plan=at,
+                            num_tiles=1, q=rows(1, 4), k=rows(2, 2), v=rows(3, 2), out=rows(4, 4), lse=at + (5 << 30),
+                            dout=rows(6, 4), dq=rows(7, 4), dk=rows(8, 2), dv=rows(9, 2), workspace=at + (10 << 30))
+    for k, v in over.items():
+        setattr(a, k, v)
+    return a
+
+
+H = N.normpre_heads
+P = 1 << 40
+
+
+@pytest.mark.parametrize("both,over,code", [
+    (True, {"dtype": 2}, INVALID), (True, {"dtype": -1}, INVALID),
+    (True, {"heads": 0}, INVALID), (True, {"kv_heads": 0}, INVALID), (True, {"kv_heads": 3}, INVALID),
+    (True, {"head_dim": 0}, INVALID), (True, {"head_dim": 129}, UNSUPPORTED),
+    (True, {"causal": 2}, INVALID), (True, {"scale": float("inf")}, INVALID), (True, {"scale": float("nan")}, INVALID),
+    (True, {"tokens": -1}, INVALID), (True, {"tokens": 1 << 31}, UNSUPPORTED), (True, {"tokens": 129}, INVALID),
+    (True, {"num_tiles": 0}, INVALID), (True, {"num_tiles": 101}, INVALID), (True, {"num_tiles": -1}, INVALID),
+    (True, {"plan": None}, INVALID), (True, {"plan": P + 4}, INVALID), (True, {"lse": None}, INVALID),
+    (True, {"lse": P + 2}, INVALID), (True, {"q": H(None, 256, 64)}, INVALID), (True, {"k": H(P + 1, 128, 64)}, INVALID),
+    (True, {"v": H(P, -128, 64)}, INVALID), (True, {"q": H(P, 1 << 41, 64)}, UNSUPPORTED),
+    (True, {"out": H(None, 256, 64)}, INVALID),
+    (False, {"dout": H(None, 256, 64)}, INVALID), (False, {"dq": H(P, 255, 64)}, INVALID),
+    (False, {"dk": H(P, 0, 64)}, INVALID), (False, {"dv": H(P, 128, 63)}, INVALID),
+    (False, {"workspace": None}, INVALID), (False, {"workspace": P + 1}, INVALID),
+    (True, {"tokens": 2 ** 31 - 1, "num_tiles": 2 ** 31 - 1}, UNSUPPORTED),
+])
+def test_attention_refusals(lib, both, over, code):
+    a = _block(**over)
+    calls = [lib.normpre_attention_backward] + ([lib.normpre_attention_forward] if both else [])
+    for call in calls:
+        assert call(ctypes.byref(a), None) == code
+        assert N.normpre_last_error()
+
+
+def test_attention_forward_output_must_not_overlap(lib):
+    for out in (H(P, 0, 64), H(P, 256, 0), H(P, 255, 64), H(P, 64, 64)):
+        assert lib.normpre_attention_forward(ctypes.byref(_block(out=out)), None) == INVALID
+        assert "overlap" in N.normpre_last_error()
+
+
+def test_attention_null_block_and_empty_batch(lib):
+    assert lib.normpre_attention_forward(None, None) == INVALID
+    empty = _block(tokens=0, num_tiles=0, q=H(None, 0, 0), plan=None)
+    assert lib.normpre_attention_forward(ctypes.byref(empty), None) == 0
+    assert lib.normpre_attention_backward(ctypes.byref(empty), None) == 0
+
+
+def test_checkpoint_refusals(lib):
+    pack = lambda act=1, dt=1, rows=4, cols=70, u=P, ldu=70, up=P, ldup=70, h=P, ldh=70, cu=P, eu=P, cup=P, eup=P, \
+        ch=P, eh=P: lib.normpre_checkpoint_pack(act, dt, rows, cols, u, ldu, up, ldup, h, ldh, cu, eu, cup, eup,  # noqa: E731
+                                                ch, eh, None)
+    for bad in ({"act": 3}, {"act": -1}, {"dt": 2}, {"rows": -1}, {"cols": 0}, {"u": None}, {"u": P + 1},
+                {"ldu": 69}, {"cu": None}, {"eu": None}, {"cu": P + 8}, {"h": None}, {"ldh": 69}, {"ch": None},
+                {"act": 2, "up": None}, {"act": 2, "ldup": 3}, {"act": 2, "cup": None}, {"act": 2, "eup": None}):
+        assert pack(**bad) == INVALID, bad
+        assert N.normpre_last_error()
+    assert pack(rows=1 << 40) == UNSUPPORTED
+    assert pack(cols=(1 << 40) + 1, ldu=1 << 62) == UNSUPPORTED
+    assert pack(ldu=1 << 41) == UNSUPPORTED
+    assert pack(rows=0, u=None, cu=None) == 0
+
+    unpack = lambda dt=1, rows=4, cols=70, c=P, e=P, out=P, ld=70: \
+        lib.normpre_checkpoint_unpack(dt, rows, cols, c, e, out, ld, None)  # noqa: E731
+    for bad in ({"dt": 5}, {"rows": -1}, {"cols": -1}, {"c": None}, {"c": P + 1}, {"e": None}, {"out": None},
+                {"ld": 69}):
+        assert unpack(**bad) == INVALID, bad
+    assert unpack(rows=0, out=None) == 0
+
+    grad = lambda act=1, dt=1, rows=4, cols=70, dh=P, ldh=70, cu=P, eu=P, cup=P, eup=P, du=P, ldu=70, dup=P, \
+        ldup=70: lib.normpre_checkpoint_act_grad(act, dt, rows, cols, dh, ldh, cu, eu, cup, eup, du, ldu, dup,  # noqa: E731
+                                                 ldup, None)
+    for bad in ({"act": 0}, {"act": 3}, {"dt": 2}, {"rows": -2}, {"cols": 0}, {"dh": None}, {"cu": P + 4},
+                {"du": None}, {"ldu": 1}, {"act": 2, "cup": None}, {"act": 2, "dup": None}, {"act": 2, "ldup": 0}):
+        assert grad(**bad) == INVALID, bad
+    assert grad(rows=0, du=None) == 0
+
+
+def test_weight_grad_refusals(lib):
+    need = N.normpre_checkpoint_weight_grad_workspace(1, 4096, 128, 128)
+    assert need > 0 and need % (4 * 128 * 128) == 0
+    call = lambda dt=1, layout=0, acc=0, t=4096, i=128, o=128, c=P, e=P, dy=P, ldy=128, dw=P, ldw=128, ws=P, \
+        n=need: lib.normpre_checkpoint_weight_grad(dt, layout, acc, t, i, o, c, e, dy, ldy, dw, ldw, ws, n, None)  # noqa: E731
+    for bad in ({"dt": 2}, {"layout": 2}, {"layout": -1}, {"acc": 2}, {"t": -1}, {"i": 0}, {"o": 0}, {"c": None},
+                {"c": P + 1}, {"e": None}, {"dy": None}, {"dy": P + 1}, {"ldy": 127}, {"dw": None}, {"dw": P + 2},
+                {"ldw": 127}, {"ws": None}, {"ws": P + 8}, {"n": need - 1}):
+        assert call(**bad) == INVALID, bad
+        assert N.normpre_last_error()
+    assert call(t=1 << 31, i=1, o=1) == UNSUPPORTED
+    assert call(i=1 << 31, ldw=1 << 31, o=1, t=1) == UNSUPPORTED
+    size = ctypes.c_int64()
+    assert lib.normpre_checkpoint_weight_grad_workspace(1, 4096, 128, 128, None) == INVALID
+    assert lib.normpre_checkpoint_weight_grad_workspace(7, 4096, 128, 128, ctypes.byref(size)) == INVALID
+    assert lib.normpre_checkpoint_weight_grad_workspace(1, 1, 128, 128, ctypes.byref(size)) == 0 and size.value == 0
+
+
+def test_front_end_needs_a_gpu_tensor():
+    from paper_2609_36692_amd import train_ops as T
+    x = torch.randn(4, 64)
+    for call in (lambda: T.checkpoint_pack(x), lambda: T.checkpoint_act("gelu", x),
+                 lambda: T.attention_forward(x[:, None], x[:, None], x[:, None], T.AttentionPlan([4], device="cpu"))):
+        with pytest.raises(ValueError):
+            call()
