@@ -212,7 +212,7 @@ def _ptr(x) -> int:
 def _stream_handle(stream):
     if stream is None:
         import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
@@ -418,29 +418,38 @@ def normpre_attention_plan(lens, causal: bool) -> np.ndarray:
 
 
 def normpre_attention_forward(args: normpre_attention, stream=None) -> None:
-    _check(load_library().normpre_attention_forward(ctypes.byref(args), _stream_handle(stream)))
+    code = load_library().normpre_attention_forward(args, _stream_handle(stream))
+    if code:
+        _check(code)
 
 
 def normpre_attention_backward(args: normpre_attention, stream=None) -> None:
-    _check(load_library().normpre_attention_backward(ctypes.byref(args), _stream_handle(stream)))
+    code = load_library().normpre_attention_backward(args, _stream_handle(stream))
+    if code:
+        _check(code)
 
 
 def normpre_checkpoint_pack(act: int, dtype: int, rows: int, cols: int, u, ld_u, up, ld_up, h, ld_h, u_codes, u_exps,
                             up_codes, up_exps, h_codes, h_exps, stream=None) -> None:
-    _check(load_library().normpre_checkpoint_pack(act, dtype, rows, cols, u, ld_u, up, ld_up, h, ld_h, u_codes,
-                                                  u_exps, up_codes, up_exps, h_codes, h_exps,
-                                                  _stream_handle(stream)))
+    code = load_library().normpre_checkpoint_pack(act, dtype, rows, cols, u, ld_u, up, ld_up, h, ld_h, u_codes,
+                                                  u_exps, up_codes, up_exps, h_codes, h_exps, _stream_handle(stream))
+    if code:
+        _check(code)
 
 
 def normpre_checkpoint_unpack(dtype: int, rows: int, cols: int, codes, exps, out, ld_out, stream=None) -> None:
-    _check(load_library().normpre_checkpoint_unpack(dtype, rows, cols, codes, exps, out, ld_out,
-                                                    _stream_handle(stream)))
+    code = load_library().normpre_checkpoint_unpack(dtype, rows, cols, codes, exps, out, ld_out,
+                                                    _stream_handle(stream))
+    if code:
+        _check(code)
 
 
 def normpre_checkpoint_act_grad(act: int, dtype: int, rows: int, cols: int, dh, ld_dh, u_codes, u_exps, up_codes,
                                 up_exps, du, ld_du, dup, ld_dup, stream=None) -> None:
-    _check(load_library().normpre_checkpoint_act_grad(act, dtype, rows, cols, dh, ld_dh, u_codes, u_exps, up_codes,
-                                                      up_exps, du, ld_du, dup, ld_dup, _stream_handle(stream)))
+    code = load_library().normpre_checkpoint_act_grad(act, dtype, rows, cols, dh, ld_dh, u_codes, u_exps, up_codes,
+                                                      up_exps, du, ld_du, dup, ld_dup, _stream_handle(stream))
+    if code:
+        _check(code)
 
 
 def normpre_checkpoint_weight_grad_workspace(dtype: int, tokens: int, inner: int, outer: int) -> int:
@@ -452,9 +461,11 @@ def normpre_checkpoint_weight_grad_workspace(dtype: int, tokens: int, inner: int
 def normpre_checkpoint_weight_grad(dtype: int, layout: int, accumulate: bool, tokens: int, inner: int, outer: int,
                                    codes, exps, dy, ld_dy, dw, ld_dw, workspace, workspace_bytes,
                                    stream=None) -> None:
-    _check(load_library().normpre_checkpoint_weight_grad(dtype, layout, int(bool(accumulate)), tokens, inner, outer,
+    code = load_library().normpre_checkpoint_weight_grad(dtype, layout, int(bool(accumulate)), tokens, inner, outer,
                                                          codes, exps, dy, ld_dy, dw, ld_dw, workspace,
-                                                         workspace_bytes, _stream_handle(stream)))
+                                                         workspace_bytes, _stream_handle(stream))
+    if code:
+        _check(code)
 
 
 class NormPre:

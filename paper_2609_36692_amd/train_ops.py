@@ -19,6 +19,7 @@ and ``checkpointed_mlp`` are differentiable.
 from __future__ import annotations
 
 import math
+import struct
 from typing import NamedTuple, Sequence
 
 import torch
@@ -37,13 +38,23 @@ def _dtype(x: torch.Tensor) -> int:
     return _DTYPES[x.dtype]
 
 
-def _same(first: torch.Tensor, **others) -> None:
+def _same(first: torch.Tensor, *others: torch.Tensor) -> None:
     """Operands of one call share device and type."""
-    if first.device.type != "cuda":
+    if not first.is_cuda:
         raise ValueError("expected tensors on a GPU")
-    for name, x in others.items():
+    for x in others:
         if x.device != first.device or x.dtype != first.dtype:
-            raise ValueError(f"{name} is {x.dtype} on {x.device}, expected {first.dtype} on {first.device}")
+            raise ValueError(f"operands differ: {x.dtype} on {x.device}, {first.dtype} on {first.device}")
+
+
+def _elsewhere(x: torch.Tensor) -> bool:
+    """Whether x lies on another device than the current one: the calls below then
+    start over with that device current, so that allocations and launches go there."""
+    return x.get_device() != torch.cuda.current_device()
+
+
+def _stream(x: torch.Tensor) -> int:
+    return torch._C._cuda_getCurrentRawStream(x.get_device())
 
 
 # ------------------------------------------------------------- attention ---
@@ -69,22 +80,29 @@ def _rows(x: torch.Tensor) -> torch.Tensor:
     return x if x.stride(2) == 1 or x.shape[2] == 1 else x.contiguous()
 
 
-def _heads(x: torch.Tensor) -> N.normpre_heads:
-    return N.normpre_heads(x.data_ptr(), x.stride(0), x.stride(1))
+# normpre_attention (include/normpre.h) in one piece: filling a ctypes structure
+# field by field takes as long as the launch itself.
+_ARGS = struct.Struct("=5if3q" + "Q2q" * 4 + "Q" + "Q2q" * 4 + "Q")
+_NONE = (0, 0, 0)
 
 
-def _attention_args(q, k, v, plan: AttentionPlan, scale) -> N.normpre_attention:
-    if q.dim() != 3 or k.dim() != 3 or v.shape != k.shape:
-        raise ValueError("expected q [tokens, heads, dim] and k, v [tokens, kv_heads, dim]")
-    _same(q, k=k, v=v)
-    if q.shape[0] != plan.tokens or k.shape[0] != plan.tokens or k.shape[2] != q.shape[2]:
-        raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} do not fit a plan of {plan.tokens} tokens")
-    if plan.data.device != q.device:
+def _heads(x: torch.Tensor):
+    st = x.stride()
+    return x.data_ptr(), st[0], st[1]
+
+
+def _attention_args(q, k, v, plan: AttentionPlan, scale):
+    """The fields up to v; checks the operands."""
+    tokens, heads, dim = q.shape
+    if k.dim() != 3 or v.shape != k.shape or k.shape[0] != tokens or k.shape[2] != dim or tokens != plan.tokens:
+        raise ValueError(f"expected q [tokens, heads, dim] and k, v [tokens, kv_heads, dim] of {plan.tokens} tokens, "
+                         f"got {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)}")
+    _same(q, k, v)
+    data = plan.data
+    if data.device != q.device:
         raise ValueError("the plan lies on another device")
-    return N.normpre_attention(
-        dtype=_dtype(q), heads=q.shape[1], kv_heads=k.shape[1], head_dim=q.shape[2], causal=int(plan.causal),
-        scale=1.0 / math.sqrt(q.shape[2]) if scale is None else float(scale), tokens=plan.tokens,
-        plan=plan.data.data_ptr(), num_tiles=plan.num_tiles, q=_heads(q), k=_heads(k), v=_heads(v))
+    return (_dtype(q), heads, k.shape[1], dim, int(plan.causal), 1.0 / math.sqrt(dim) if scale is None else scale,
+            tokens, data.data_ptr(), plan.num_tiles, *_heads(q), *_heads(k), *_heads(v))
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: AttentionPlan,
@@ -93,13 +111,18 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: A
     packed batch; q [tokens, heads, dim], k and v [tokens, kv_heads, dim], query
     head h reading key head h * kv_heads // heads; scale 1 / sqrt(dim) if None.
     Any strides; views of one projection's output need no copy."""
+    if q.dim() != 3:
+        raise ValueError(f"expected q [tokens, heads, dim], got {tuple(q.shape)}")
     q, k, v = _rows(q), _rows(k), _rows(v)
-    a = _attention_args(q, k, v, plan, scale)
-    with torch.cuda.device(q.device):
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((q.shape[1], q.shape[0]), dtype=torch.float32, device=q.device)
-        a.out, a.lse = _heads(out), lse.data_ptr()
-        N.normpre_attention_forward(a)
+    args = _attention_args(q, k, v, plan, scale)
+    if _elsewhere(q):
+        with torch.cuda.device(q.device):
+            return attention_forward(q, k, v, plan, scale)
+    tokens, heads, _ = q.shape
+    out = q.new_empty(q.shape)
+    lse = q.new_empty((heads, tokens), dtype=torch.float32)
+    block = _ARGS.pack(*args, *_heads(out), lse.data_ptr(), *_NONE * 4, 0)
+    N.normpre_attention_forward(N.normpre_attention.from_buffer_copy(block), _stream(q))
     return out, lse
 
 
@@ -107,20 +130,22 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
                        lse: torch.Tensor, plan: AttentionPlan, scale: float | None = None):
     """(dq, dk, dv) from the gradient of ``attention_forward``'s output and what
     that call took and returned."""
+    if q.dim() != 3 or out.shape != q.shape or dout.shape != q.shape:
+        raise ValueError("q, out and dout are [tokens, heads, dim]")
     q, k, v, out, dout = _rows(q), _rows(k), _rows(v), _rows(out), _rows(dout)
-    a = _attention_args(q, k, v, plan, scale)
-    _same(q, out=out, dout=dout)
-    if out.shape != q.shape or dout.shape != q.shape:
-        raise ValueError("out and dout have q's shape")
+    args = _attention_args(q, k, v, plan, scale)
+    _same(q, out, dout)
     if lse.shape != (q.shape[1], q.shape[0]) or lse.dtype != torch.float32 or not lse.is_contiguous() \
             or lse.device != q.device:
         raise ValueError("lse is attention_forward's")
-    with torch.cuda.device(q.device):
-        dq, dk, dv = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (q, k, v))
-        delta = torch.empty_like(lse)
-        a.out, a.lse, a.dout, a.workspace = _heads(out), lse.data_ptr(), _heads(dout), delta.data_ptr()
-        a.dq, a.dk, a.dv = _heads(dq), _heads(dk), _heads(dv)
-        N.normpre_attention_backward(a)
+    if _elsewhere(q):
+        with torch.cuda.device(q.device):
+            return attention_backward(dout, q, k, v, out, lse, plan, scale)
+    dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+    delta = lse.new_empty(lse.shape)
+    block = _ARGS.pack(*args, *_heads(out), lse.data_ptr(), *_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv),
+                       delta.data_ptr())
+    N.normpre_attention_backward(N.normpre_attention.from_buffer_copy(block), _stream(q))
     return dq, dk, dv
 
 
@@ -158,48 +183,63 @@ def _matrix(x: torch.Tensor) -> torch.Tensor:
     """2-D, rows of adjacent features."""
     if x.dim() != 2:
         raise ValueError(f"expected a matrix [tokens, features], got {tuple(x.shape)}")
-    return x if (x.stride(1) == 1 or x.shape[1] == 1) and x.stride(0) >= x.shape[1] else x.contiguous()
+    st = x.stride()
+    return x if (st[1] == 1 or x.shape[1] == 1) and st[0] >= x.shape[1] else x.contiguous()
 
 
 def _new_checkpoint(x: torch.Tensor) -> Checkpoint:
     rows, cols = x.shape
-    pitch = -(-cols // GROUP) * GROUP
-    return Checkpoint(torch.empty((rows, pitch), dtype=torch.int8, device=x.device),
-                      torch.empty((rows, pitch // GROUP), dtype=torch.int8, device=x.device), cols)
+    groups = -(-cols // GROUP)
+    return Checkpoint(x.new_empty((rows, groups * GROUP), dtype=torch.int8),
+                      x.new_empty((rows, groups), dtype=torch.int8), cols)
 
 
 def _held(c: Checkpoint, rows: int | None = None):
-    pitch = -(-c.cols // GROUP) * GROUP
-    ok = (c.codes.dtype == torch.int8 and c.exps.dtype == torch.int8 and c.codes.is_contiguous()
-          and c.exps.is_contiguous() and c.codes.device == c.exps.device and c.codes.device.type == "cuda"
-          and c.codes.dim() == 2 and c.codes.shape[1] == pitch
-          and c.exps.shape == (c.codes.shape[0], pitch // GROUP) and rows in (None, c.codes.shape[0]))
-    if not ok:
-        raise ValueError("not a checkpoint of this shape")
-    return c.codes.data_ptr(), c.exps.data_ptr()
+    codes, exps = c.codes, c.exps
+    groups = -(-c.cols // GROUP)
+    if not (codes.dtype == exps.dtype == torch.int8 and codes.dim() == 2 and codes.shape[1] == groups * GROUP
+            and exps.shape == (codes.shape[0], groups) and codes.is_contiguous() and exps.is_contiguous()
+            and codes.is_cuda and codes.device == exps.device and rows in (None, codes.shape[0])):
+        raise ValueError("not a checkpoint of this shape on a GPU")
+    return codes.data_ptr(), exps.data_ptr()
 
 
 def _ld(x: torch.Tensor) -> int:
     return max(x.stride(0), x.shape[1])
 
 
+_NOTHING = (None, 0)
+
+
+def _row_args(x: torch.Tensor | None):
+    return _NOTHING if x is None else (x.data_ptr(), _ld(x))
+
+
+def _held_args(c: Checkpoint | None):
+    return (None, None) if c is None else (c.codes.data_ptr(), c.exps.data_ptr())
+
+
 def checkpoint_pack(x: torch.Tensor) -> Checkpoint:
     """The 8-bit checkpoint of x [tokens, features]."""
     x = _matrix(x)
     _same(x)
-    with torch.cuda.device(x.device):
-        c = _new_checkpoint(x)
-        N.normpre_checkpoint_pack(N.NORMPRE_ACT_NONE, _dtype(x), *x.shape, x.data_ptr(), _ld(x), None, 0, None, 0,
-                                  *_held(c), None, None, None, None)
+    if _elsewhere(x):
+        with torch.cuda.device(x.device):
+            return checkpoint_pack(x)
+    c = _new_checkpoint(x)
+    N.normpre_checkpoint_pack(N.NORMPRE_ACT_NONE, _dtype(x), *x.shape, *_row_args(x), *_NOTHING, *_NOTHING,
+                              *_held_args(c), None, None, None, None, _stream(x))
     return c
 
 
 def checkpoint_unpack(c: Checkpoint, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The values a checkpoint stands for (exact in bf16 and fp32)."""
     held = _held(c)
-    with torch.cuda.device(c.codes.device):
-        out = torch.empty((c.codes.shape[0], c.cols), dtype=dtype, device=c.codes.device)
-        N.normpre_checkpoint_unpack(_dtype(out), *out.shape, *held, out.data_ptr(), _ld(out))
+    if _elsewhere(c.codes):
+        with torch.cuda.device(c.codes.device):
+            return checkpoint_unpack(c, dtype)
+    out = c.codes.new_empty((c.codes.shape[0], c.cols), dtype=dtype)
+    N.normpre_checkpoint_unpack(_dtype(out), *out.shape, *held, *_row_args(out), _stream(out))
     return out
 
 
@@ -212,17 +252,17 @@ def checkpoint_act(act: str, u: torch.Tensor, up: torch.Tensor | None = None):
     _same(u)
     if up is not None:
         up = _matrix(up)
-        _same(u, up=up)
+        _same(u, up)
         if up.shape != u.shape:
             raise ValueError("u and up have one shape")
-    with torch.cuda.device(u.device):
-        h = torch.empty(u.shape, dtype=u.dtype, device=u.device)
-        cu, ch = _new_checkpoint(u), _new_checkpoint(u)
-        cup = None if up is None else _new_checkpoint(u)
-        N.normpre_checkpoint_pack(_ACTS[act], _dtype(u), *u.shape, u.data_ptr(), _ld(u),
-                                  None if up is None else up.data_ptr(), 0 if up is None else _ld(up),
-                                  h.data_ptr(), _ld(h), *_held(cu), *((None, None) if cup is None else _held(cup)),
-                                  *_held(ch))
+    if _elsewhere(u):
+        with torch.cuda.device(u.device):
+            return checkpoint_act(act, u, up)
+    h = u.new_empty(u.shape)
+    cu, ch = _new_checkpoint(u), _new_checkpoint(u)
+    cup = None if up is None else _new_checkpoint(u)
+    N.normpre_checkpoint_pack(_ACTS[act], _dtype(u), *u.shape, *_row_args(u), *_row_args(up), *_row_args(h),
+                              *_held_args(cu), *_held_args(cup), *_held_args(ch), _stream(u))
     return h, cu, cup, ch
 
 
@@ -237,11 +277,13 @@ def checkpoint_act_grad(act: str, dh: torch.Tensor, cu: Checkpoint, cup: Checkpo
             raise ValueError("the checkpoint is of another activation")
     hu = _held(cu, dh.shape[0])
     hup = (None, None) if cup is None else _held(cup, dh.shape[0])
-    with torch.cuda.device(dh.device):
-        du = torch.empty(dh.shape, dtype=dh.dtype, device=dh.device)
-        dup = None if cup is None else torch.empty_like(du)
-        N.normpre_checkpoint_act_grad(_ACTS[act], _dtype(dh), *dh.shape, dh.data_ptr(), _ld(dh), *hu, *hup,
-                                      du.data_ptr(), _ld(du), None if dup is None else dup.data_ptr(), _ld(du))
+    if _elsewhere(dh):
+        with torch.cuda.device(dh.device):
+            return checkpoint_act_grad(act, dh, cu, cup)
+    du = dh.new_empty(dh.shape)
+    dup = None if cup is None else dh.new_empty(dh.shape)
+    N.normpre_checkpoint_act_grad(_ACTS[act], _dtype(dh), *dh.shape, *_row_args(dh), *hu, *hup, *_row_args(du),
+                                  *_row_args(dup), _stream(dh))
     return du, dup
 
 
@@ -262,18 +304,19 @@ def checkpoint_weight_grad(c: Checkpoint, dy: torch.Tensor, layout: str = "oi", 
     if c.codes.device != dy.device:
         raise ValueError("the checkpoint lies on another device")
     shape = (c.cols, outer) if layout == "io" else (outer, c.cols)
-    with torch.cuda.device(dy.device):
-        if out is None:
-            out = torch.empty(shape, dtype=torch.float32, device=dy.device)
-        elif (tuple(out.shape) != shape or out.dtype != torch.float32 or out.device != dy.device
-              or (out.stride(1) != 1 and shape[1] > 1) or (out.stride(0) < shape[1] and shape[0] > 1)):
-            raise ValueError(f"out is a row-major float32 {shape} matrix on {dy.device}")
-        dt = _dtype(dy)
-        need = N.normpre_checkpoint_weight_grad_workspace(dt, tokens, c.cols, outer)
-        ws = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
-        N.normpre_checkpoint_weight_grad(dt, _LAYOUTS[layout], accumulate, tokens, c.cols, outer, *held,
-                                         dy.data_ptr(), _ld(dy), out.data_ptr(), _ld(out),
-                                         None if ws is None else ws.data_ptr(), need)
+    if out is not None and (out.shape != shape or out.dtype != torch.float32 or out.device != dy.device
+                            or (out.stride(1) != 1 and shape[1] > 1) or (out.stride(0) < shape[1] and shape[0] > 1)):
+        raise ValueError(f"out is a row-major float32 {shape} matrix on {dy.device}")
+    if _elsewhere(dy):
+        with torch.cuda.device(dy.device):
+            return checkpoint_weight_grad(c, dy, layout, out, accumulate)
+    if out is None:
+        out = dy.new_empty(shape, dtype=torch.float32)
+    dt = _dtype(dy)
+    need = N.normpre_checkpoint_weight_grad_workspace(dt, tokens, c.cols, outer)
+    ws = dy.new_empty(need, dtype=torch.uint8) if need else None
+    N.normpre_checkpoint_weight_grad(dt, _LAYOUTS[layout], accumulate, tokens, c.cols, outer, *held, *_row_args(dy),
+                                     *_row_args(out), None if ws is None else ws.data_ptr(), need, _stream(dy))
     return out
 
 
