@@ -493,7 +493,7 @@ typedef struct normpre_attention {
     float*  lse;                /* [heads][tokens]: written / read               */
     normpre_heads dout;         /* backward: read                                */
     normpre_heads dq, dk, dv;   /* backward: written                             */
-    float*  workspace;          /* backward: heads * tokens floats               */
+    float*  workspace;          /* backward: 2 * heads * tokens floats           */
 } normpre_attention;
 
 /*

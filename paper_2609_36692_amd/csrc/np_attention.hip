@@ -87,7 +87,7 @@ template <class T, int DP>
 struct Tile {
     static constexpr int E = 16 / sizeof(T);     // elements of a chunk
     static constexpr int CH = DP / E;            // chunks of a row
-    static __device__ __forceinline__ int idx(int r, int c) { return (r * CH + (c ^ swz(r))) * E; }
+    static __device__ __forceinline__ int idx(int r, int c) { return (r * CH + (c & ~7) + ((c & 7) ^ swz(r))) * E; }
 };
 
 // Staging of ROWS x DP from rows [row0, row0 + ROWS) of one operand, rows at
@@ -110,6 +110,76 @@ struct Stage {
         for (int i = 0; i < N; ++i) {
             const int e = tid + i * kThreads;
             *reinterpret_cast<u32x4*>(lds + TL::idx(e / TL::CH, e % TL::CH)) = r[i];
+        }
+    }
+};
+
+// The same tile straight from memory to LDS, without passing through
+// registers.  Rows past the end and chunks past the feature count are copies of
+// the last ones there are: they meet zero weights or zero owned features, and
+// what is not finite among them is caught with the other rows that are not
+// (any_nonfinite).  One instruction fills 1 KB of LDS per wave, so the swizzle
+// is in the order of the chunks that the lanes fetch.
+template <class T, int DP, int ROWS>
+struct Direct {
+    using TL = Tile<T, DP>;
+    static constexpr int N = ROWS * TL::CH / kThreads;
+    static __device__ __forceinline__ void load(T* lds, const T* base, int64_t tok, int row0, int rows, int dim,
+                                                int tid) {
+        const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int e = tid + i * kThreads, r = e / TL::CH;
+            const int c = min((e % TL::CH) ^ swz(r), dim / TL::E - 1);
+            const T* src = base + (int64_t)min(row0 + r, rows - 1) * tok + c * TL::E;
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
+                                             (__attribute__((address_space(3))) void*)(lds + (i * kThreads + wave * 64) * TL::E),
+                                             16, 0, 0);
+        }
+    }
+};
+// Waits for this wave's loads to LDS.
+__device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }   // vmcnt(0)
+
+// Two streamed operands (K and V, or Q and dO) in two LDS buffers.  Tile `it`
+// of a loop is in buffer it % 2.  VEC: each tile is on its way to LDS while the
+// one before it is worked on; a wave waits for its own part of it, the barrier
+// for the other waves', and behind the barrier the other buffer is free, since
+// every wave is done with the tile before.  Otherwise tiles pass through
+// registers with no overlap (rows that do not start on 16 bytes).
+template <class T, int DP, int ROWS, bool VEC>
+struct Pair {
+    const T* p0;
+    int64_t tok0;
+    const T* p1;
+    int64_t tok1;
+    int rows, dim;
+    __device__ __forceinline__ void fill(T (&buf)[2][ROWS * DP], int row0, int tid) const {
+        if constexpr (VEC) {
+            Direct<T, DP, ROWS>::load(buf[0], p0, tok0, row0, rows, dim, tid);
+            Direct<T, DP, ROWS>::load(buf[1], p1, tok1, row0, rows, dim, tid);
+        } else {
+            using ST = Stage<T, DP, ROWS, false>;
+            u32x4 r[ST::N];
+            ST::load(r, p0, tok0, row0, rows, dim, tid);
+            ST::store(r, buf[0], tid);
+            ST::load(r, p1, tok1, row0, rows, dim, tid);
+            ST::store(r, buf[1], tid);
+        }
+    }
+    __device__ __forceinline__ void first(T (&smem)[2][2][ROWS * DP], int row0, int tid) const {
+        if constexpr (VEC) fill(smem[0], row0, tid);
+    }
+    // Tile `it` is ready behind this call; row0: its first row, then: that of
+    // the tile after it, or -1.
+    __device__ __forceinline__ void next(T (&smem)[2][2][ROWS * DP], int it, int row0, int then, int tid) const {
+        if constexpr (VEC) {
+            wait_loads();
+            lds_barrier();
+            if (then >= 0) fill(smem[(it + 1) & 1], then, tid);
+        } else {
+            fill(smem[it & 1], row0, tid);
+            lds_barrier();
         }
     }
 };
@@ -352,6 +422,13 @@ __device__ __forceinline__ uint32_t bad_rows(bool bad) {
 }
 
 // ---------------------------------------------------------------- passes ---
+// Waves per SIMD a kernel is compiled for: two (256 registers), so that one
+// wave's matrix instructions run beside the other's exponentials, unless the
+// owned operands and accumulators (`ops` and `accs` per owned row and feature)
+// leave no room for them.
+template <class T, int DP>
+constexpr int waves(int ops, int accs) { return DP * (ops * (int)sizeof(T) / 4.f + accs) / 2 <= 160 ? 2 : 1; }
+
 // Rows of a streamed tile.
 template <class T> constexpr int kStream = std::is_same_v<T, bf16_t> ? 64 : 32;
 
@@ -365,9 +442,8 @@ __device__ __forceinline__ bool locate(const AttnArgs& a, const AttnTile& t, int
 }
 
 template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(kThreads, 1) attn_fwd_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, (waves<T, DP>(1, 1))) attn_fwd_kernel(AttnArgs a) {
     constexpr int BN = kStream<T>, NB = BN / 32, DT = DP / 32;
-    using ST = Stage<T, DP, BN, VEC>;
     __shared__ __attribute__((aligned(16))) T smem[2][2][BN * DP];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int group = a.heads / a.kv_heads;
@@ -387,19 +463,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_kernel(AttnArgs a) {
 
     f32x16 o[DT] = {};
     float m = -INFINITY, l = 0.f;
-    u32x4 rk[ST::N], rv[ST::N];
-    ST::load(rk, kb, a.k.tok, 0, w.len, a.dim, tid);
-    ST::load(rv, vb, a.v.tok, 0, w.len, a.dim, tid);
-    ST::store(rk, smem[0][0], tid);
-    ST::store(rv, smem[0][1], tid);
+    const Pair<T, DP, BN, VEC> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
+    keys.first(smem, 0, tid);
     for (int it = 0; it < steps; ++it) {
         const int k0 = it * BN;
-        const bool more = it + 1 < steps;
-        if (more) {
-            ST::load(rk, kb, a.k.tok, k0 + BN, w.len, a.dim, tid);
-            ST::load(rv, vb, a.v.tok, k0 + BN, w.len, a.dim, tid);
-        }
-        lds_barrier();
+        keys.next(smem, it, k0, it + 1 < steps ? k0 + BN : -1, tid);
         const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
         if (!a.causal || k0 <= qw + 31) {            // same for the whole wave
             f32x16 s[NB];
@@ -439,10 +507,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_kernel(AttnArgs a) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) accumulate<T, DP>(o, vs, 32 * b, s[b], lane);
         }
-        if (more) {
-            ST::store(rk, smem[(it + 1) & 1][0], tid);
-            ST::store(rv, smem[(it + 1) & 1][1], tid);
-        }
     }
     l += __shfl_xor(l, 32, 64);
     uint32_t bad = bad_rows(live && (any_nonfinite(o) || !(l < INFINITY)));
@@ -454,9 +518,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_fwd_kernel(AttnArgs a) {
 }
 
 template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(kThreads, 1) attn_dq_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 1))) attn_dq_kernel(AttnArgs a) {
     constexpr int BN = kStream<T>, NB = BN / 32, DT = DP / 32;
-    using ST = Stage<T, DP, BN, VEC>;
     __shared__ __attribute__((aligned(16))) T smem[2][2][BN * DP];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int group = a.heads / a.kv_heads;
@@ -492,64 +555,56 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dq_kernel(AttnArgs a) {
     const int end = a.causal ? min(w.len, q0 + kAttnRows) : w.len, steps = (end + BN - 1) / BN;
     const float c2 = a.scale * kLog2e;
 
-    f32x16 g[DT] = {};
-    u32x4 rk[ST::N], rv[ST::N];
+    const Pair<T, DP, BN, VEC> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
+    // p (dp - de) of streamed rows k0 + 32 b .., zero where the row does not see them.
+    auto weights = [&](const T* ks, const T* vs, int k0, int b, float de) {
+        f32x16 s = scores<T, DP>(ks, 32 * b, q, lane);
+        const f32x16 dp = scores<T, DP>(vs, 32 * b, dout, lane);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = exp2_fast(__builtin_fmaf(s[r], c2, -lse2)) * (dp[r] - de);
+        if (k0 + BN > w.len || (a.causal && k0 + BN - 1 > qw)) {
+            const int last = a.causal ? min(qi, w.len - 1) : w.len - 1;
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (k0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4 > last) s[r] = 0.f;
+        }
+        return s;
+    };
     // delta = do . o carries the rounding of o.  Where a row sees few keys, o
     // is as large as a value and that error as large as the other ones, so
     // blocks with up to kAttnRows keys first sum delta = sum_j p dp from the
     // scores; with more keys o averages out (error under a fifth of a
     // rounding of ds) and a second pass over them would cost 2/3 of the first.
-    const bool twice = end <= kAttnRows;
-    float sum = 0.f;
-    for (int it = twice ? -steps : 0; it < steps; ++it) {
-        const int k0 = (it < 0 ? it + steps : it) * BN;
-        const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
-        if (it == 0 || it == -steps) {
-            if (it == 0 && twice) {
-                sum += __shfl_xor(sum, 32, 64);
-                delta = sum;
-                lds_barrier();                       // the first pass has read its tiles
-            }
-            ST::load(rk, kb, a.k.tok, 0, w.len, a.dim, tid);
-            ST::load(rv, vb, a.v.tok, 0, w.len, a.dim, tid);
-            ST::store(rk, smem[it & 1][0], tid);
-            ST::store(rv, smem[it & 1][1], tid);
-        }
-        const bool more = it + 1 < steps && it != -1;
-        if (more) {
-            ST::load(rk, kb, a.k.tok, k0 + BN, w.len, a.dim, tid);
-            ST::load(rv, vb, a.v.tok, k0 + BN, w.len, a.dim, tid);
-        }
-        lds_barrier();
-        if (!a.causal || k0 <= qw + 31) {            // same for the whole wave
-            const bool edge = k0 + BN > w.len || (a.causal && k0 + BN - 1 > qw);
-            const int last = a.causal ? min(qi, w.len - 1) : w.len - 1;
+    if (end <= kAttnRows) {
+        float sum = 0.f;
+        keys.first(smem, 0, tid);
+        for (int it = 0; it < steps; ++it) {
+            const int k0 = it * BN;
+            keys.next(smem, it, k0, it + 1 < steps ? k0 + BN : -1, tid);
+            if (!a.causal || k0 <= qw + 31) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                f32x16 s = scores<T, DP>(ks, 32 * b, q, lane);
-                const f32x16 dp = scores<T, DP>(vs, 32 * b, dout, lane);
-                const float de = it < 0 ? 0.f : delta;
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    s[r] = exp2_fast(__builtin_fmaf(s[r], c2, -lse2)) * (dp[r] - de);
-                if (edge) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        if (k0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4 > last) s[r] = 0.f;
-                }
-                if (it < 0) {
+                for (int b = 0; b < NB; ++b) {
+                    const f32x16 s = weights(smem[it & 1][0], smem[it & 1][1], k0, b, 0.f);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sum += s[r];
-                } else {
-                    accumulate<T, DP>(g, ks, 32 * b, s, lane);
                 }
             }
         }
-        if (more) {
-            ST::store(rk, smem[(it + 1) & 1][0], tid);
-            ST::store(rv, smem[(it + 1) & 1][1], tid);
+        delta = sum + __shfl_xor(sum, 32, 64);
+        lds_barrier();                               // the tiles have been read
+    }
+    f32x16 g[DT] = {};
+    keys.first(smem, 0, tid);
+    for (int it = 0; it < steps; ++it) {
+        const int k0 = it * BN;
+        keys.next(smem, it, k0, it + 1 < steps ? k0 + BN : -1, tid);
+        const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
+        if (!a.causal || k0 <= qw + 31) {            // same for the whole wave
+#pragma unroll
+            for (int b = 0; b < NB; ++b) accumulate<T, DP>(g, ks, 32 * b, weights(ks, vs, k0, b, delta), lane);
         }
     }
+    if (live && half == 0) a.lse2[at] = lse2;
     if (live && half == 0) a.delta[at] = delta;
     uint32_t bad = bad_rows(live && any_nonfinite(g));
     if (live && !(bad >> (lane & 31) & 1))
@@ -561,9 +616,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dq_kernel(AttnArgs a) {
 }
 
 template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(kThreads, 1) attn_dkv_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kernel(AttnArgs a) {
     constexpr int BM = kStream<T>, NB = BM / 32, DT = DP / 32;
-    using ST = Stage<T, DP, BM, VEC>;
     __shared__ __attribute__((aligned(16))) T smem[2][2][BM * DP];
     __shared__ __attribute__((aligned(16))) float stat[2][2][BM];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
@@ -583,33 +637,27 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dkv_kernel(AttnArgs a) {
     const float c2 = a.scale * kLog2e;
 
     f32x16 gk[DT] = {}, gv[DT] = {};
-    u32x4 rq[ST::N], rd[ST::N];
-    float rs = 0.f;
-    // Step i: queries of tile first + i % per, head kv * group + i / per.
-    auto fetch = [&](int i) {
+    // Step i: queries of tile first + i % per, head kv * group + i / per, and
+    // their log-sum-exps and deltas.
+    auto fetch = [&](int i, int buf) {
         const int h = w.head + i / per, row0 = (first + i % per) * BM;
-        ST::load(rq, row_of<T>(a.q, w, 0, h), a.q.tok, row0, w.len, a.dim, tid);
-        ST::load(rd, row_of<T>(a.dout, w, 0, h), a.dout.tok, row0, w.len, a.dim, tid);
-        if (tid < 2 * BM) {
-            const int row = row0 + tid % BM;
-            const float* src = tid < BM ? a.lse : a.delta;
-            // Queries past the end get lse = inf: their weights are zero.
-            rs = row < w.len ? src[h * a.tokens + w.start + row] * (tid < BM ? kLog2e : 1.f)
-                             : (tid < BM ? INFINITY : 0.f);
+        const Pair<T, DP, BM, VEC> rows{row_of<T>(a.q, w, 0, h), a.q.tok, row_of<T>(a.dout, w, 0, h), a.dout.tok,
+                                        w.len, a.dim};
+        rows.fill(smem[buf], row0, tid);
+        if (tid < 2 * BM) {                          // whole waves
+            const float* src = (tid < BM ? a.lse2 : a.delta) + h * a.tokens + w.start + min(row0 + tid % BM, w.len - 1);
+            __builtin_amdgcn_global_load_lds(
+                (const __attribute__((address_space(1))) void*)src,
+                (__attribute__((address_space(3))) void*)(&stat[buf][0][0] + __builtin_amdgcn_readfirstlane(tid >> 6) * 64),
+                4, 0, 0);
         }
     };
-    auto put = [&](int buf) {
-        ST::store(rq, smem[buf][0], tid);
-        ST::store(rd, smem[buf][1], tid);
-        if (tid < 2 * BM) stat[buf][tid / BM][tid % BM] = rs;
-    };
-    fetch(0);
-    put(0);
+    fetch(0, 0);
     for (int it = 0; it < steps; ++it) {
         const int q0 = (first + it % per) * BM;
-        const bool more = it + 1 < steps;
-        if (more) fetch(it + 1);
+        wait_loads();
         lds_barrier();
+        if (it + 1 < steps) fetch(it + 1, (it + 1) & 1);
         const T *qs = smem[it & 1][0], *ds = smem[it & 1][1];
         const float *lse2 = stat[it & 1][0], *delta = stat[it & 1][1];
 #pragma unroll
@@ -623,11 +671,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dkv_kernel(AttnArgs a) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) p[4 * j + i] = exp2_fast(__builtin_fmaf(p[4 * j + i], c2, -ls[i]));
             }
-            const bool edge = a.causal && qb < kw + 31;
+            // Queries of the sequence that see the lane's key.
+            const bool edge = (a.causal && qb < kw + 31) || qb + 32 > w.len;
+            const int from = a.causal ? ki : 0;
             if (edge) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (qb + 8 * (r / 4) + 4 * half + r % 4 < ki) p[r] = 0.f;
+                for (int r = 0; r < 16; ++r) {
+                    const int row = qb + 8 * (r / 4) + 4 * half + r % 4;
+                    if (row < from || row >= w.len) p[r] = 0.f;
+                }
             }
             accumulate<T, DP>(gv, ds, 32 * b, p, lane);
             f32x16 dp = scores<T, DP>(ds, 32 * b, v, lane);
@@ -639,12 +691,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_dkv_kernel(AttnArgs a) {
             }
             if (edge) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (qb + 8 * (r / 4) + 4 * half + r % 4 < ki) dp[r] = 0.f;
+                for (int r = 0; r < 16; ++r) {
+                    const int row = qb + 8 * (r / 4) + 4 * half + r % 4;
+                    if (row < from || row >= w.len) dp[r] = 0.f;
+                }
             }
             accumulate<T, DP>(gk, qs, 32 * b, dp, lane);
         }
-        if (more) put((it + 1) & 1);
     }
     uint32_t bad = bad_rows(live && (any_nonfinite(gk) || any_nonfinite(gv)));
     if (live && !(bad >> (lane & 31) & 1)) {

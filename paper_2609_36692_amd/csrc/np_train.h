@@ -28,7 +28,8 @@ struct AttnOperand {
 struct AttnArgs {
     AttnOperand q, k, v, out, dout, dq, dk, dv;
     float* lse;                 // [heads][tokens], natural logarithms
-    float* delta;               // [heads][tokens], backward workspace
+    float* lse2;                // backward workspace, [heads][tokens] each: lse in
+    float* delta;               // base 2, and delta
     const AttnTile* tiles;      // query tiles, then as many key tiles
     int num_tiles;
     int64_t tokens;

@@ -134,7 +134,8 @@ int attention(const normpre_attention* a, bool backward, void* stream) {
     k.dq = operand(a->dq);
     k.dk = operand(a->dk);
     k.dv = operand(a->dv);
-    k.delta = a->workspace;
+    k.lse2 = a->workspace;
+    k.delta = a->workspace + a->heads * a->tokens;
     return launched(launch_attention_backward(dt, k, (hipStream_t)stream));
 }
 

@@ -142,9 +142,9 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
         with torch.cuda.device(q.device):
             return attention_backward(dout, q, k, v, out, lse, plan, scale)
     dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
-    delta = lse.new_empty(lse.shape)
+    work = lse.new_empty((2, *lse.shape))
     block = _ARGS.pack(*args, *_heads(out), lse.data_ptr(), *_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv),
-                       delta.data_ptr())
+                       work.data_ptr())
     N.normpre_attention_backward(N.normpre_attention.from_buffer_copy(block), _stream(q))
     return dq, dk, dv
 
