@@ -493,8 +493,14 @@ typedef struct normpre_attention {
     float*  lse;                /* [heads][tokens]: written / read               */
     normpre_heads dout;         /* backward: read                                */
     normpre_heads dq, dk, dv;   /* backward: written                             */
-    float*  workspace;          /* backward: 2 * heads * tokens floats           */
+    void*   workspace;          /* backward: 16-byte aligned, of                 */
+    int64_t workspace_bytes;    /* normpre_attention_workspace() bytes or more   */
 } normpre_attention;
+
+/* Workspace bytes of a backward call; reads dtype, heads, kv_heads, head_dim,
+ * tokens and num_tiles of *a.  Host only.  Errors: as the calls below, of those
+ * fields, and INVALID_ARG (null pointers). */
+int normpre_attention_workspace(const normpre_attention* a, int64_t* bytes);
 
 /*
  * out_i = sum_j p_ij v_j, p_ij = exp(c q_i . k_j - lse_i) over the keys j that
@@ -510,7 +516,8 @@ typedef struct normpre_attention {
  * a multiple of kv_heads, head_dim < 1, negative strides, an output whose
  * rows overlap, a non-finite scale, num_tiles < 0, causal not 0 or 1, tokens
  * and num_tiles that contradict each other), UNSUPPORTED (head_dim > 128,
- * 2^31 tokens, strides above 2^40, more than 2^31 - 1 blocks), HIP.
+ * 2^31 tokens, strides above 2^40, more than 2^31 - 1 blocks), HIP.  INVALID_ARG
+ * too for a workspace that is missing, misaligned or too small.
  */
 int normpre_attention_forward(const normpre_attention* a, void* stream);
 int normpre_attention_backward(const normpre_attention* a, void* stream);

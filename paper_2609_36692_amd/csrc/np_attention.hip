@@ -92,23 +92,23 @@ struct Tile {
 
 // Staging of ROWS x DP from rows [row0, row0 + ROWS) of one operand, rows at
 // `rows` and past it zero.
-template <class T, int DP, int ROWS, bool VEC>
+template <class T, int DP, int ROWS, bool VEC, int NT>
 struct Stage {
     using TL = Tile<T, DP>;
-    static constexpr int N = ROWS * TL::CH / kThreads;
-    static_assert(N >= 1 && ROWS * TL::CH % kThreads == 0, "tile does not fill the block");
+    static constexpr int N = ROWS * TL::CH / NT;
+    static_assert(N >= 1 && ROWS * TL::CH % NT == 0, "tile does not fill the block");
     static __device__ __forceinline__ void load(u32x4 (&r)[N], const T* base, int64_t tok, int row0, int rows,
                                                 int dim, int tid) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int e = tid + i * kThreads, row = row0 + e / TL::CH;
+            const int e = tid + i * NT, row = row0 + e / TL::CH;
             r[i] = load_chunk<T, VEC>(base + (int64_t)row * tok, e % TL::CH, dim, row < rows);
         }
     }
     static __device__ __forceinline__ void store(const u32x4 (&r)[N], T* lds, int tid) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int e = tid + i * kThreads;
+            const int e = tid + i * NT;
             *reinterpret_cast<u32x4*>(lds + TL::idx(e / TL::CH, e % TL::CH)) = r[i];
         }
     }
@@ -120,20 +120,20 @@ struct Stage {
 // what is not finite among them is caught with the other rows that are not
 // (any_nonfinite).  One instruction fills 1 KB of LDS per wave, so the swizzle
 // is in the order of the chunks that the lanes fetch.
-template <class T, int DP, int ROWS>
+template <class T, int DP, int ROWS, int NT>
 struct Direct {
     using TL = Tile<T, DP>;
-    static constexpr int N = ROWS * TL::CH / kThreads;
+    static constexpr int N = ROWS * TL::CH / NT;
     static __device__ __forceinline__ void load(T* lds, const T* base, int64_t tok, int row0, int rows, int dim,
                                                 int tid) {
         const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int e = tid + i * kThreads, r = e / TL::CH;
+            const int e = tid + i * NT, r = e / TL::CH;
             const int c = min((e % TL::CH) ^ swz(r), dim / TL::E - 1);
             const T* src = base + (int64_t)min(row0 + r, rows - 1) * tok + c * TL::E;
             __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src,
-                                             (__attribute__((address_space(3))) void*)(lds + (i * kThreads + wave * 64) * TL::E),
+                                             (__attribute__((address_space(3))) void*)(lds + (i * NT + wave * 64) * TL::E),
                                              16, 0, 0);
         }
     }
@@ -147,7 +147,7 @@ __device__ __forceinline__ void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70
 // for the other waves', and behind the barrier the other buffer is free, since
 // every wave is done with the tile before.  Otherwise tiles pass through
 // registers with no overlap (rows that do not start on 16 bytes).
-template <class T, int DP, int ROWS, bool VEC>
+template <class T, int DP, int ROWS, bool VEC, int NT>
 struct Pair {
     const T* p0;
     int64_t tok0;
@@ -156,10 +156,10 @@ struct Pair {
     int rows, dim;
     __device__ __forceinline__ void fill(T (&buf)[2][ROWS * DP], int row0, int tid) const {
         if constexpr (VEC) {
-            Direct<T, DP, ROWS>::load(buf[0], p0, tok0, row0, rows, dim, tid);
-            Direct<T, DP, ROWS>::load(buf[1], p1, tok1, row0, rows, dim, tid);
+            Direct<T, DP, ROWS, NT>::load(buf[0], p0, tok0, row0, rows, dim, tid);
+            Direct<T, DP, ROWS, NT>::load(buf[1], p1, tok1, row0, rows, dim, tid);
         } else {
-            using ST = Stage<T, DP, ROWS, false>;
+            using ST = Stage<T, DP, ROWS, false, NT>;
             u32x4 r[ST::N];
             ST::load(r, p0, tok0, row0, rows, dim, tid);
             ST::store(r, buf[0], tid);
@@ -193,6 +193,10 @@ struct Owned {
     __device__ __forceinline__ void load(const T* row, int dim, bool live, int half) {
 #pragma unroll
         for (int s = 0; s < S; ++s) c[s] = load_chunk<T, VEC>(row, 2 * s + half, dim, live);
+    }
+    __device__ __forceinline__ void negate() {
+#pragma unroll
+        for (int s = 0; s < S; ++s) c[s] ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
     }
 };
 
@@ -264,30 +268,76 @@ __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* lds,
     }
 }
 
-// Writes f * acc of the lane's owned row.
+// Writes f * acc of the wave's owned rows, `keep` (bit r: row r) of them, to
+// rows of `stride` elements from `out`.  The rows pass through the wave's share
+// of the LDS tiles (32 x DP words, which every wave must be done with), so that
+// memory gets whole rows instead of 8 or 16 bytes of 32 rows at a time.
 template <class T, int DP, bool VEC>
-__device__ __forceinline__ void store_row(T* row, const f32x16 (&acc)[DP / 32], float f, int dim, int half) {
+__device__ __forceinline__ void store_rows(void* lds, T* out, int64_t stride, const f32x16 (&acc)[DP / 32], float f,
+                                           int dim, uint32_t keep, int lane) {
+    constexpr int E = 16 / sizeof(T), CH = DP / E, M = (CH < 16 ? CH : 16) - 1;
+    T* mine = static_cast<T*>(lds);
+    const int row = lane & 31, half = lane >> 5;
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int d = 32 * t + 8 * j + 4 * half;
-            if constexpr (VEC) {
-                if (d < dim) {
-                    T e[4];
+            T e[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) e[i] = (T)(f * acc[t][4 * j + i]);
-                    typedef uint32_t V __attribute__((ext_vector_type(sizeof(T))));
-                    V v;
-                    __builtin_memcpy(&v, e, sizeof v);
-                    *reinterpret_cast<V*>(row + d) = v;
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (d + i < dim) row[d + i] = (T)(f * acc[t][4 * j + i]);
-            }
+            for (int i = 0; i < 4; ++i) e[i] = (T)(f * acc[t][4 * j + i]);
+            typedef uint32_t V __attribute__((ext_vector_type(sizeof(T))));
+            V v;
+            __builtin_memcpy(&v, e, sizeof v);
+            *reinterpret_cast<V*>(mine + (row * CH + ((d / E) ^ (row & M))) * E + d % E) = v;
         }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 32 * CH / 64; ++i) {
+        const int r = (i * 64 + lane) / CH, c = lane % CH;
+        if (!(keep >> r & 1)) continue;
+        const u32x4 v = *reinterpret_cast<const u32x4*>(mine + (r * CH + (c ^ (r & M))) * E);
+        T* dst = out + r * stride + c * E;
+        if constexpr (VEC) {
+            if (c * E < dim) *reinterpret_cast<u32x4*>(dst) = v;
+        } else {
+            T e[E];
+            __builtin_memcpy(e, &v, 16);
+#pragma unroll
+            for (int k = 0; k < E; ++k)
+                if (c * E + k < dim) dst[k] = e[k];
+        }
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A wave's accumulators through its share of the LDS tiles to the wave of the
+// other team that owns the same rows, which adds them: acc f0 + other f1.
+template <class T, int DP>
+__device__ __forceinline__ void hand_over(T* lds, const f32x16 (&acc)[DP / 32], int lane) {
+    f32x4* p = reinterpret_cast<f32x4*>(lds) + lane;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            p[(4 * t + j) * 64] = f32x4{acc[t][4 * j], acc[t][4 * j + 1], acc[t][4 * j + 2], acc[t][4 * j + 3]};
+}
+template <class T, int DP>
+__device__ __forceinline__ void take_over(const T* lds, f32x16 (&acc)[DP / 32], float f0, float f1, int lane) {
+    const f32x4* p = reinterpret_cast<const f32x4*>(lds) + lane;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const f32x4 v = p[(4 * t + j) * 64];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[t][4 * j + i] = acc[t][4 * j + i] * f0 + v[i] * f1;
+        }
+}
+
+// Bits of the wave's rows [row0, row0 + 32) that lie before `rows`.
+__device__ __forceinline__ uint32_t live_rows(int row0, int rows) {
+    return row0 >= rows ? 0u : rows - row0 >= 32 ? ~0u : (1u << (rows - row0)) - 1;
 }
 
 template <int NT>
@@ -422,114 +472,165 @@ __device__ __forceinline__ uint32_t bad_rows(bool bad) {
 }
 
 // ---------------------------------------------------------------- passes ---
+// Rows of a streamed tile.
+template <class T> constexpr int kStream = std::is_same_v<T, bf16_t> ? 64 : 32;
+// Rows of each team's tiles in the query passes: half where the tiles of all
+// teams would not fit in LDS.
+template <class T, int DP, int TEAMS>
+constexpr int kStreamed = TEAMS * kStream<T> * DP * 4 * (int)sizeof(T) <= 140 * 1024 ? kStream<T> : kStream<T> / 2;
+
 // Waves per SIMD a kernel is compiled for: two (256 registers), so that one
 // wave's matrix instructions run beside the other's exponentials, unless the
 // owned operands and accumulators (`ops` and `accs` per owned row and feature)
 // leave no room for them.
 template <class T, int DP>
 constexpr int waves(int ops, int accs) { return DP * (ops * (int)sizeof(T) / 4.f + accs) / 2 <= 160 ? 2 : 1; }
-
-// Rows of a streamed tile.
-template <class T> constexpr int kStream = std::is_same_v<T, bf16_t> ? 64 : 32;
+// The same for the query passes, where LDS may hold only one block of four waves.
+template <class T, int DP, int WR, int TEAMS>
+constexpr int query_waves(int ops) {
+    return WR * TEAMS == 4 && TEAMS * kStream<T> * DP * 4 * (int)sizeof(T) > 80 * 1024 ? 1 : waves<T, DP>(ops, 1);
+}
 
 // Block order: key heads fastest, so the blocks of one key head (consecutive
 // workgroups go to the 8 XCDs in turn) stay with one XCD's L2 where the
 // number of key heads is a multiple of 8; the plan's tiles, longest first,
 // slowest.
-__device__ __forceinline__ bool locate(const AttnArgs& a, const AttnTile& t, int rows_per_tile, int& row0) {
-    row0 = t.tile * rows_per_tile;
+__device__ __forceinline__ bool locate(const AttnArgs& a, const AttnTile& t, int within, int& row0) {
+    row0 = t.tile * kAttnRows + within;
     return t.start >= 0 && t.len > 0 && t.tile >= 0 && row0 < t.len && (int64_t)t.start + t.len <= a.tokens;
 }
 
-template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(kThreads, (waves<T, DP>(1, 1))) attn_fwd_kernel(AttnArgs a) {
-    constexpr int BN = kStream<T>, NB = BN / 32, DT = DP / 32;
-    __shared__ __attribute__((aligned(16))) T smem[2][2][BN * DP];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+template <class T, int DP, bool VEC, int WR, int TEAMS>
+__global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS>(1))) attn_fwd_kernel(AttnArgs a) {
+    constexpr int NT = 64 * WR, BN = kStreamed<T, DP, TEAMS>, NB = BN / 32, DT = DP / 32;
+    __shared__ __attribute__((aligned(16))) T tiles[TEAMS][2][2][BN * DP];
+    __shared__ float stat[TEAMS][2][32 * WR];
+    const int tid = threadIdx.x % NT, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int team = TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
     const int group = a.heads / a.kv_heads;
     const AttnTile tile = a.tiles[blockIdx.x / a.heads];
     const int kv = blockIdx.x % a.kv_heads, head = kv * group + (blockIdx.x / a.kv_heads) % group;
     int q0;
-    if (!locate(a, tile, kAttnRows, q0)) return;    // the whole block
+    if (!locate(a, tile, blockIdx.y * 32 * WR, q0)) return;    // the whole block
     const Where w{tile.start, tile.len, head, kv};
     const int qw = q0 + wave * 32, qi = qw + (lane & 31);
     const bool live = qi < w.len;
+    auto& smem = tiles[team];
 
     Owned<T, DP> q;
     q.template load<VEC>(row_of<T>(a.q, w, live ? qi : 0, head), a.dim, live, half);
+    if (a.scale < 0.f) q.negate();                   // so that larger products are larger scores
     const T *kb = row_of<T>(a.k, w, 0, kv), *vb = row_of<T>(a.v, w, 0, kv);
-    const int end = a.causal ? min(w.len, q0 + kAttnRows) : w.len, steps = (end + BN - 1) / BN;
-    const float c2 = a.scale * kLog2e;
+    const int end = a.causal ? min(w.len, q0 + 32 * WR) : w.len, steps = (end + BN - 1) / BN;
+    const float c2 = fabsf(a.scale) * kLog2e;
 
+    // m: the largest product so far, or one that was when it was last raised; o
+    // and l are raised to it only once a score is 2^8 above it, so that most
+    // tiles leave o alone (weights then stay below 2^8, which costs no digit).
     f32x16 o[DT] = {};
     float m = -INFINITY, l = 0.f;
-    const Pair<T, DP, BN, VEC> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
-    keys.first(smem, 0, tid);
-    for (int it = 0; it < steps; ++it) {
-        const int k0 = it * BN;
-        keys.next(smem, it, k0, it + 1 < steps ? k0 + BN : -1, tid);
+    const Pair<T, DP, BN, VEC, NT> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
+    keys.first(smem, team * BN, tid);
+    for (int it = 0; it < (steps + TEAMS - 1) / TEAMS; ++it) {
+        const int k0 = (it * TEAMS + team) * BN;
+        keys.next(smem, it, k0, it * TEAMS + team + TEAMS < steps ? k0 + TEAMS * BN : -1, tid);
         const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
-        if (!a.causal || k0 <= qw + 31) {            // same for the whole wave
+        if (k0 < end && (!a.causal || k0 <= qw + 31)) {    // same for the whole wave
             f32x16 s[NB];
+            float mx = m;
+            const bool edge = k0 + BN > w.len || (a.causal && k0 + BN - 1 > qw);
+            const int last = (a.causal ? min(qi, w.len - 1) : w.len - 1) - k0 - 4 * half;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                s[b] = scores<T, DP>(ks, 32 * b, q, lane);
-                s[b] *= c2;
-            }
-            if (k0 + BN > w.len || (a.causal && k0 + BN - 1 > qw)) {
-                const int last = a.causal ? min(qi, w.len - 1) : w.len - 1;
+            for (int b = 0; b < NB; ++b) s[b] = scores<T, DP>(ks, 32 * b, q, lane);
+            if (edge) {
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
                     for (int r = 0; r < 16; ++r)
-                        if (k0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4 > last) s[b][r] = -INFINITY;
+                        if (32 * b + 8 * (r / 4) + r % 4 > last) s[b][r] = -INFINITY;
             }
-            float mx = m;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[b][r]);
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float mu = mx == -INFINITY ? 0.f : mx, f = exp2_fast(m - mu);
-            m = mx;
-            l *= f;
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[b][r] = exp2_fast(s[b][r] - mu);
-                    l += s[b][r];
-                }
-            if (__any(f != 1.f)) {
+            if (__any((mx - m) * c2 > 8.f || (m == -INFINITY && mx != -INFINITY))) {
+                const float f = m == -INFINITY ? 0.f : exp2_fast((m - mx) * c2);
+                m = mx;
+                l *= f;
 #pragma unroll
                 for (int t = 0; t < DT; ++t) o[t] *= f;
             }
+            const float mu = m == -INFINITY ? 0.f : m * c2;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[b][r] = exp2_fast(__builtin_fmaf(s[b][r], c2, -mu));
+            if (edge) {                              // also where c is 0
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        if (32 * b + 8 * (r / 4) + r % 4 > last) s[b][r] = 0.f;
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) l += s[b][r];
 #pragma unroll
             for (int b = 0; b < NB; ++b) accumulate<T, DP>(o, vs, 32 * b, s[b], lane);
         }
     }
     l += __shfl_xor(l, 32, 64);
-    uint32_t bad = bad_rows(live && (any_nonfinite(o) || !(l < INFINITY)));
-    if (live && !(bad >> (lane & 31) & 1)) {
-        store_row<T, DP, VEC>(row_of<T>(a.out, w, qi, head), o, 1.f / l, a.dim, half);
-        if (half == 0) a.lse[head * a.tokens + w.start + qi] = m * kLn2 + logf(l);
+    lds_barrier();                                   // the tiles are free
+    T* mine = &smem[0][0][0] + wave * (BN * DP * 4 / WR);
+    if constexpr (TEAMS > 1) {
+        if (team > 0) hand_over<T, DP>(mine, o, lane);
+        if (half == 0) {
+            stat[team][0][wave * 32 + lane] = m;
+            stat[team][1][wave * 32 + lane] = l;
+        }
+        lds_barrier();
+        if (team > 0) return;
+        const int row = wave * 32 + (lane & 31);
+        float mx = m;
+#pragma unroll
+        for (int t = 1; t < TEAMS; ++t) mx = fmaxf(mx, stat[t][0][row]);
+        float f = m == -INFINITY ? 0.f : exp2_fast((m - mx) * c2);
+        l *= f;
+#pragma unroll
+        for (int t = 1; t < TEAMS; ++t) {
+            const float mt = stat[t][0][row], ft = mt == -INFINITY ? 0.f : exp2_fast((mt - mx) * c2);
+            take_over<T, DP>(&tiles[t][0][0][0] + wave * (BN * DP * 4 / WR), o, f, ft, lane);
+            l += stat[t][1][row] * ft;
+            f = 1.f;
+        }
+        m = mx;
     }
+    uint32_t bad = bad_rows(live && (any_nonfinite(o) || !(l < INFINITY)));
+    store_rows<T, DP, VEC>(mine, row_of<T>(a.out, w, qw, head), a.out.tok, o, 1.f / l,
+                           a.dim, live_rows(qw, w.len) & ~bad, lane);
+    if (live && half == 0 && !(bad >> lane & 1))
+        a.lse[head * a.tokens + w.start + qi] = m * fabsf(a.scale) + logf(l);
     for (; bad; bad &= bad - 1) forward_row<T>(a, w, qw + __builtin_ctz(bad), lane);
 }
 
-template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 1))) attn_dq_kernel(AttnArgs a) {
-    constexpr int BN = kStream<T>, NB = BN / 32, DT = DP / 32;
-    __shared__ __attribute__((aligned(16))) T smem[2][2][BN * DP];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+template <class T, int DP, bool VEC, int WR, int TEAMS>
+__global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS>(2))) attn_dq_kernel(AttnArgs a) {
+    constexpr int NT = 64 * WR, BN = kStreamed<T, DP, TEAMS>, NB = BN / 32, DT = DP / 32;
+    __shared__ __attribute__((aligned(16))) T tiles[TEAMS][2][2][BN * DP];
+    __shared__ float stat[TEAMS][32 * WR];
+    const int tid = threadIdx.x % NT, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int team = TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
     const int group = a.heads / a.kv_heads;
     const AttnTile tile = a.tiles[blockIdx.x / a.heads];
     const int kv = blockIdx.x % a.kv_heads, head = kv * group + (blockIdx.x / a.kv_heads) % group;
     int q0;
-    if (!locate(a, tile, kAttnRows, q0)) return;    // the whole block
+    if (!locate(a, tile, blockIdx.y * 32 * WR, q0)) return;    // the whole block
     const Where w{tile.start, tile.len, head, kv};
     const int qw = q0 + wave * 32, qi = qw + (lane & 31);
     const bool live = qi < w.len;
+    auto& smem = tiles[team];
 
     Owned<T, DP> q, dout;
     q.template load<VEC>(row_of<T>(a.q, w, live ? qi : 0, head), a.dim, live, half);
@@ -552,10 +653,10 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 1))) attn_dq_kernel
     const int64_t at = head * a.tokens + w.start + (live ? qi : 0);
     const float lse2 = live ? a.lse[at] * kLog2e : INFINITY;
     const T *kb = row_of<T>(a.k, w, 0, kv), *vb = row_of<T>(a.v, w, 0, kv);
-    const int end = a.causal ? min(w.len, q0 + kAttnRows) : w.len, steps = (end + BN - 1) / BN;
+    const int end = a.causal ? min(w.len, q0 + 32 * WR) : w.len, steps = (end + BN - 1) / BN;
     const float c2 = a.scale * kLog2e;
 
-    const Pair<T, DP, BN, VEC> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
+    const Pair<T, DP, BN, VEC, NT> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
     // p (dp - de) of streamed rows k0 + 32 b .., zero where the row does not see them.
     auto weights = [&](const T* ks, const T* vs, int k0, int b, float de) {
         f32x16 s = scores<T, DP>(ks, 32 * b, q, lane);
@@ -575,13 +676,14 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 1))) attn_dq_kernel
     // blocks with up to kAttnRows keys first sum delta = sum_j p dp from the
     // scores; with more keys o averages out (error under a fifth of a
     // rounding of ds) and a second pass over them would cost 2/3 of the first.
+    const int rounds = (steps + TEAMS - 1) / TEAMS;
     if (end <= kAttnRows) {
         float sum = 0.f;
-        keys.first(smem, 0, tid);
-        for (int it = 0; it < steps; ++it) {
-            const int k0 = it * BN;
-            keys.next(smem, it, k0, it + 1 < steps ? k0 + BN : -1, tid);
-            if (!a.causal || k0 <= qw + 31) {
+        keys.first(smem, team * BN, tid);
+        for (int it = 0; it < rounds; ++it) {
+            const int k0 = (it * TEAMS + team) * BN;
+            keys.next(smem, it, k0, it * TEAMS + team + TEAMS < steps ? k0 + TEAMS * BN : -1, tid);
+            if (k0 < end && (!a.causal || k0 <= qw + 31)) {
 #pragma unroll
                 for (int b = 0; b < NB; ++b) {
                     const f32x16 s = weights(smem[it & 1][0], smem[it & 1][1], k0, b, 0.f);
@@ -591,24 +693,40 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 1))) attn_dq_kernel
             }
         }
         delta = sum + __shfl_xor(sum, 32, 64);
+        if (TEAMS > 1 && half == 0) stat[team][wave * 32 + lane] = delta;
         lds_barrier();                               // the tiles have been read
+        if constexpr (TEAMS > 1) {
+            delta = 0.f;
+#pragma unroll
+            for (int t = 0; t < TEAMS; ++t) delta += stat[t][wave * 32 + (lane & 31)];
+        }
     }
     f32x16 g[DT] = {};
-    keys.first(smem, 0, tid);
-    for (int it = 0; it < steps; ++it) {
-        const int k0 = it * BN;
-        keys.next(smem, it, k0, it + 1 < steps ? k0 + BN : -1, tid);
+    keys.first(smem, team * BN, tid);
+    for (int it = 0; it < rounds; ++it) {
+        const int k0 = (it * TEAMS + team) * BN;
+        keys.next(smem, it, k0, it * TEAMS + team + TEAMS < steps ? k0 + TEAMS * BN : -1, tid);
         const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
-        if (!a.causal || k0 <= qw + 31) {            // same for the whole wave
+        if (k0 < end && (!a.causal || k0 <= qw + 31)) {    // same for the whole wave
 #pragma unroll
             for (int b = 0; b < NB; ++b) accumulate<T, DP>(g, ks, 32 * b, weights(ks, vs, k0, b, delta), lane);
         }
     }
+    lds_barrier();                                   // the tiles are free
+    T* mine = &smem[0][0][0] + wave * (BN * DP * 4 / WR);
+    if constexpr (TEAMS > 1) {
+        if (team > 0) hand_over<T, DP>(mine, g, lane);
+        lds_barrier();
+        if (team > 0) return;
+#pragma unroll
+        for (int t = 1; t < TEAMS; ++t)
+            take_over<T, DP>(&tiles[t][0][0][0] + wave * (BN * DP * 4 / WR), g, 1.f, 1.f, lane);
+    }
     if (live && half == 0) a.lse2[at] = lse2;
     if (live && half == 0) a.delta[at] = delta;
     uint32_t bad = bad_rows(live && any_nonfinite(g));
-    if (live && !(bad >> (lane & 31) & 1))
-        store_row<T, DP, VEC>(row_of<T>(a.dq, w, qi, head), g, a.scale, a.dim, half);
+    store_rows<T, DP, VEC>(mine, row_of<T>(a.dq, w, qw, head), a.dq.tok, g,
+                           a.scale, a.dim, live_rows(qw, w.len) & ~bad, lane);
     for (; bad; bad &= bad - 1) {
         const int r = __builtin_ctz(bad);
         dq_row<T>(a, w, qw + r, __shfl(delta, r, 64), lane);
@@ -625,23 +743,27 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
     const AttnTile tile = a.tiles[a.num_tiles + blockIdx.x / a.kv_heads];
     const int kv = blockIdx.x % a.kv_heads;
     int kt;
-    if (!locate(a, tile, kAttnRows, kt)) return;    // the whole block
+    if (!locate(a, tile, 0, kt)) return;    // the whole block
     const Where w{tile.start, tile.len, kv * group, kv};
+    const int share = blockIdx.y;
     const int kw = kt + wave * 32, ki = kw + (lane & 31);
     const bool live = ki < w.len;
 
     Owned<T, DP> k, v;
     k.template load<VEC>(row_of<T>(a.k, w, live ? ki : 0, kv), a.dim, live, half);
     v.template load<VEC>(row_of<T>(a.v, w, live ? ki : 0, kv), a.dim, live, half);
-    const int first = a.causal ? kt / BM : 0, per = (w.len + BM - 1) / BM - first, steps = per * group;
+    const int first = a.causal ? kt / BM : 0, per = (w.len + BM - 1) / BM - first;
+    // Steps of this block's share; step i: queries of tile first + i % per, head
+    // kv * group + i / per.
+    const int all = per * group, beg = (int)((int64_t)all * share / a.splits),
+              steps = (int)((int64_t)all * (share + 1) / a.splits);
     const float c2 = a.scale * kLog2e;
 
     f32x16 gk[DT] = {}, gv[DT] = {};
-    // Step i: queries of tile first + i % per, head kv * group + i / per, and
-    // their log-sum-exps and deltas.
+    // A step's queries, their log-sum-exps and deltas.
     auto fetch = [&](int i, int buf) {
         const int h = w.head + i / per, row0 = (first + i % per) * BM;
-        const Pair<T, DP, BM, VEC> rows{row_of<T>(a.q, w, 0, h), a.q.tok, row_of<T>(a.dout, w, 0, h), a.dout.tok,
+        const Pair<T, DP, BM, VEC, kThreads> rows{row_of<T>(a.q, w, 0, h), a.q.tok, row_of<T>(a.dout, w, 0, h), a.dout.tok,
                                         w.len, a.dim};
         rows.fill(smem[buf], row0, tid);
         if (tid < 2 * BM) {                          // whole waves
@@ -652,8 +774,8 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
                 4, 0, 0);
         }
     };
-    fetch(0, 0);
-    for (int it = 0; it < steps; ++it) {
+    if (beg < steps) fetch(beg, beg & 1);
+    for (int it = beg; it < steps; ++it) {
         const int q0 = (first + it % per) * BM;
         wait_loads();
         lds_barrier();
@@ -699,12 +821,64 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
             accumulate<T, DP>(gk, qs, 32 * b, dp, lane);
         }
     }
-    uint32_t bad = bad_rows(live && (any_nonfinite(gk) || any_nonfinite(gv)));
-    if (live && !(bad >> (lane & 31) & 1)) {
-        store_row<T, DP, VEC>(row_of<T>(a.dk, w, ki, kv), gk, a.scale, a.dim, half);
-        store_row<T, DP, VEC>(row_of<T>(a.dv, w, ki, kv), gv, 1.f, a.dim, half);
+    lds_barrier();                                   // the tiles are free
+    T* mine = &smem[0][0][0] + wave * (BM * DP);
+    const uint32_t keep = live_rows(kw, w.len);
+    if (a.splits > 1) {
+        const int64_t at = (kv * a.tokens + w.start + kw) * DP, one = (int64_t)a.kv_heads * a.tokens * DP;
+        float* part = a.partial + 2 * share * one + at;
+        store_rows<float, DP, true>(mine, part, DP, gk, a.scale, a.dim, keep, lane);
+        store_rows<float, DP, true>(mine, part + one, DP, gv, 1.f, a.dim, keep, lane);
+        return;
     }
+    uint32_t bad = bad_rows(live && (any_nonfinite(gk) || any_nonfinite(gv)));
+    store_rows<T, DP, VEC>(mine, row_of<T>(a.dk, w, kw, kv), a.dk.tok, gk, a.scale, a.dim, keep & ~bad, lane);
+    store_rows<T, DP, VEC>(mine, row_of<T>(a.dv, w, kw, kv), a.dv.tok, gv, 1.f, a.dim, keep & ~bad, lane);
     for (; bad; bad &= bad - 1) dkv_row<T>(a, w, kw + __builtin_ctz(bad), lane);
+}
+
+// Adds the shares of dk and dv, in their order: four features a thread, the rows
+// of a tile over DP / 8 blocks.
+template <class T, int DP>
+__global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a) {
+    constexpr int LR = DP / 4, RB = kThreads / LR;   // threads of a row, rows of a block
+    const int lane = threadIdx.x & 63, r = threadIdx.x / LR, d = threadIdx.x % LR * 4;
+    const AttnTile tile = a.tiles[a.num_tiles + blockIdx.x / a.kv_heads];
+    const int kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads;
+    int kt;
+    if (!locate(a, tile, 0, kt)) return;    // the whole block
+    const Where w{tile.start, tile.len, kv * group, kv};
+    const int64_t one = (int64_t)a.kv_heads * a.tokens * DP;
+    const int ki = kt + blockIdx.y * RB + r;
+    const bool live = ki < w.len;
+    f32x4 gk = {}, gv = {};
+    if (live && d < a.dim) {
+        const float* part = a.partial + (kv * a.tokens + w.start + ki) * DP + d;
+#pragma unroll 4
+        for (int s = 0; s < a.splits; ++s) {
+            gk += *reinterpret_cast<const f32x4*>(part + 2 * s * one);
+            gv += *reinterpret_cast<const f32x4*>(part + (2 * s + 1) * one);
+        }
+    }
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (d + i < a.dim) t += gk[i] * 0.f + gv[i] * 0.f;
+    // Rows that are not finite, of this wave: one by one.
+    const uint64_t bad = __ballot(live && !(t == 0.f));
+    constexpr uint64_t row_lanes = LR == 16 ? 0xffffull : 0xffffffffull;
+    const bool redo = bad >> (lane / LR * LR) & row_lanes;
+    if (live && !redo) {
+        T *dk = row_of<T>(a.dk, w, ki, kv), *dv = row_of<T>(a.dv, w, ki, kv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (d + i < a.dim) {
+                dk[d + i] = (T)gk[i];
+                dv[d + i] = (T)gv[i];
+            }
+    }
+    for (int k = 0; k < 64 / LR; ++k)
+        if (bad >> (k * LR) & row_lanes) dkv_row<T>(a, w, ki - lane / LR + k, lane);
 }
 
 // -------------------------------------------------------------- launches ---
@@ -714,17 +888,38 @@ bool aligned(const AttnOperand& o) {
     return reinterpret_cast<uintptr_t>(o.p) % 16 == 0 && o.tok % E == 0 && o.head % E == 0;
 }
 
+// Forward and dq pass: blocks of WR waves along the rows, TEAMS of them along
+// the keys.
+template <class T, int DP, bool VEC, int WR, int TEAMS>
+void query_pass(const AttnArgs& a, bool backward, hipStream_t s) {
+    const dim3 grid((unsigned)a.num_tiles * a.heads, kAttnRows / (32 * WR));
+    if (backward) attn_dq_kernel<T, DP, VEC, WR, TEAMS><<<grid, 64 * WR * TEAMS, 0, s>>>(a);
+    else attn_fwd_kernel<T, DP, VEC, WR, TEAMS><<<grid, 64 * WR * TEAMS, 0, s>>>(a);
+}
+
 template <class T, int DP, bool VEC>
 hipError_t run(const AttnArgs& a, bool backward, hipStream_t s) {
-    const unsigned n = (unsigned)a.num_tiles;
-    if (!backward) {
-        attn_fwd_kernel<T, DP, VEC><<<n * a.heads, kThreads, 0, s>>>(a);
-    } else {
-        attn_dq_kernel<T, DP, VEC><<<n * a.heads, kThreads, 0, s>>>(a);
-        const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
-        attn_dkv_kernel<T, DP, VEC><<<n * a.kv_heads, kThreads, 0, s>>>(a);
-    }
+    // Few blocks: their waves share the keys, so that a block's chain of tiles is
+    // half as long, and up to 192 (fp32: 448) of 128 rows they are cut in two.
+    // Many blocks: one team, whose blocks run out of step, so that one's softmax
+    // meets the other's products.  Forward us of (4, 1), (4, 2), (2, 2):
+    //   bf16, heads of 64, blocks of 128 rows 96: 19.5 15.6 12.6, 192: 19.9 16.3 15.1,
+    //     288: 20.6 16.5 16.9, 384: 20.9 17.7 18.3, 576: 22.6 26.6 26.2, 960: 31.6 40.5 40.2
+    //   bf16, 128: 256: 47.0 39.0 42.1, 512: 55.4 49.3 84.5, 768: 68.0 78.8 130
+    //   fp32, 64: 384: 103 98 74, 768: 146 137 134, 1536: 240 249 258
+    //   fp32, 128: 256: 143 143 98, 512: 201 169 197, 1024: 317 337 394
+    const int64_t blocks = (int64_t)a.num_tiles * a.heads;
+    constexpr bool small = sizeof(T) == 2;
+    if (!VEC || blocks > (small ? 512 : 448)) query_pass<T, DP, VEC, 4, 1>(a, backward, s);
+    else if (small && blocks > 192) {
+        if constexpr (small) query_pass<T, DP, true, 4, 2>(a, backward, s);
+    } else query_pass<T, DP, true, 2, 2>(a, backward, s);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !backward) return e;
+    attn_dkv_kernel<T, DP, VEC><<<dim3((unsigned)a.num_tiles * a.kv_heads, a.splits), kThreads, 0, s>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    attn_join_kernel<T, DP><<<dim3((unsigned)a.num_tiles * a.kv_heads, DP / 8), kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -738,6 +933,21 @@ hipError_t dispatch(const AttnArgs& a, bool backward, hipStream_t s) {
 }
 
 }  // namespace
+
+// Shares of the queries in the dk/dv pass: enough blocks for two on every CU, at
+// most 4, since the partial sums of a share are written and read once more.
+// Backward us of 1, 2, 4, 8 shares: 64 blocks (heads of 64, 32 over 8) 48.8 35.3
+// 27.4 28.0; 128 (the same) 240 152 124 123; 256 (128, 16 over 8) 445 341 365 429;
+// 1536 (64, 12) 137 223 310 483.
+int attention_splits(int64_t num_tiles, int kv_heads) {
+    const int64_t blocks = num_tiles * kv_heads;
+    return blocks >= 512 ? 1 : blocks >= 256 ? 2 : 4;
+}
+
+int64_t attention_workspace(const AttnArgs& a) {
+    const int64_t rows = 2 * (int64_t)a.heads * a.tokens, pitch = a.dim <= 64 ? 64 : 128;
+    return (rows + 3) / 4 * 4 + (a.splits > 1 ? 2 * a.splits * (int64_t)a.kv_heads * a.tokens * pitch : 0);
+}
 
 hipError_t launch_attention_forward(DType t, const AttnArgs& a, hipStream_t s) {
     return t == DType::BF16 ? dispatch<bf16_t>(a, false, s) : dispatch<float>(a, false, s);

@@ -30,6 +30,8 @@ struct AttnArgs {
     float* lse;                 // [heads][tokens], natural logarithms
     float* lse2;                // backward workspace, [heads][tokens] each: lse in
     float* delta;               // base 2, and delta
+    float* partial;             // [splits][2][kv_heads][tokens][64 or 128], splits > 1
+    int splits;                 // shares of a key's queries (dk/dv pass)
     const AttnTile* tiles;      // query tiles, then as many key tiles
     int num_tiles;
     int64_t tokens;
@@ -37,6 +39,10 @@ struct AttnArgs {
     float scale;
 };
 
+// Shares into which the dk/dv pass cuts the queries of a key, and the floats of
+// workspace that a backward call needs (lse2 and delta, then the partial sums).
+int attention_splits(int64_t num_tiles, int kv_heads);
+int64_t attention_workspace(const AttnArgs& a);
 hipError_t launch_attention_forward(DType t, const AttnArgs& a, hipStream_t s);
 hipError_t launch_attention_backward(DType t, const AttnArgs& a, hipStream_t s);
 

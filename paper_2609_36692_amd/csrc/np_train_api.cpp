@@ -76,7 +76,7 @@ int check_operand(const char* name, const normpre_heads& o, int64_t tokens, int6
 
 AttnOperand operand(const normpre_heads& o) { return {o.data, o.token_stride, o.head_stride}; }
 
-int attention(const normpre_attention* a, bool backward, void* stream) {
+int check_sizes(const normpre_attention* a) {
     if (!a) return bad("the argument block is null");
     if (!known(a->dtype)) return fail(NORMPRE_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
     if (a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads)
@@ -92,8 +92,26 @@ int attention(const normpre_attention* a, bool backward, void* stream) {
     if (a->num_tiles > a->tokens || a->num_tiles * kAttnRows < a->tokens)
         return fail(NORMPRE_ERR_INVALID_ARG, "%lld tiles cannot hold %lld tokens", (long long)a->num_tiles,
                     (long long)a->tokens);
-    if (a->tokens == 0) return NORMPRE_OK;
     if (a->num_tiles * a->heads > kMaxBlocks) return fail(NORMPRE_ERR_UNSUPPORTED, "more than 2^31 - 1 blocks");
+    return NORMPRE_OK;
+}
+
+// The sizes alone, with what the backward pass makes of them.
+AttnArgs sizes(const normpre_attention* a) {
+    AttnArgs k{};
+    k.num_tiles = (int)a->num_tiles;
+    k.tokens = a->tokens;
+    k.heads = a->heads;
+    k.kv_heads = a->kv_heads;
+    k.dim = a->head_dim;
+    k.splits = attention_splits(a->num_tiles, a->kv_heads);
+    return k;
+}
+
+int attention(const normpre_attention* a, bool backward, void* stream) {
+    const int sized = check_sizes(a);
+    if (sized != NORMPRE_OK) return sized;
+    if (a->tokens == 0) return NORMPRE_OK;
     if (!a->plan || !on(a->plan, 16)) return bad("plan is null or not 16-byte aligned");
     if (!a->lse || !on(a->lse, 4)) return bad("lse is null or misaligned");
     const int64_t t = a->tokens, hq = a->heads, hk = a->kv_heads, d = a->head_dim, e = size_of(a->dtype);
@@ -110,22 +128,16 @@ int attention(const normpre_attention* a, bool backward, void* stream) {
         operand_ok("dq", a->dq, hq, true);
         operand_ok("dk", a->dk, hk, true);
         operand_ok("dv", a->dv, hk, true);
-        if (rc == NORMPRE_OK && (!a->workspace || !on(a->workspace, 4))) return bad("workspace is null or misaligned");
     }
     if (rc != NORMPRE_OK) return rc;
 
-    AttnArgs k{};
+    AttnArgs k = sizes(a);
     k.q = operand(a->q);
     k.k = operand(a->k);
     k.v = operand(a->v);
     k.out = operand(a->out);
     k.lse = a->lse;
     k.tiles = reinterpret_cast<const AttnTile*>(a->plan);
-    k.num_tiles = (int)a->num_tiles;
-    k.tokens = a->tokens;
-    k.heads = a->heads;
-    k.kv_heads = a->kv_heads;
-    k.dim = a->head_dim;
     k.causal = a->causal;
     k.scale = a->scale;
     const DType dt = (DType)a->dtype;
@@ -134,8 +146,13 @@ int attention(const normpre_attention* a, bool backward, void* stream) {
     k.dq = operand(a->dq);
     k.dk = operand(a->dk);
     k.dv = operand(a->dv);
-    k.lse2 = a->workspace;
-    k.delta = a->workspace + a->heads * a->tokens;
+    float* ws = static_cast<float*>(a->workspace);
+    if (!ws || !on(ws, 16) || a->workspace_bytes < 4 * attention_workspace(k))
+        return bad("workspace is null, misaligned or too small");
+    const int64_t rows = (int64_t)a->heads * a->tokens;
+    k.lse2 = ws;
+    k.delta = ws + rows;
+    k.partial = ws + (2 * rows + 3) / 4 * 4;
     return launched(launch_attention_backward(dt, k, (hipStream_t)stream));
 }
 
@@ -214,6 +231,13 @@ int normpre_attention_plan(int64_t num_seqs, const int64_t* lens, int causal, in
     } catch (const std::bad_alloc&) {
         return fail(NORMPRE_ERR_OOM, "no memory for the plan");
     }
+    return NORMPRE_OK;
+}
+
+int normpre_attention_workspace(const normpre_attention* a, int64_t* bytes) {
+    if (!bytes) return bad("bytes is null");
+    NP_CHECK(check_sizes(a));
+    *bytes = 4 * attention_workspace(sizes(a));
     return NORMPRE_OK;
 }
 

@@ -125,6 +125,7 @@ class normpre_attention(ctypes.Structure):
         ("dout", normpre_heads),
         ("dq", normpre_heads), ("dk", normpre_heads), ("dv", normpre_heads),
         ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_int64),
     ]
 
 
@@ -174,6 +175,7 @@ def load_library(path: str = LIB_PATH):
                                                 ctypes.POINTER(P), i64p, hpp, P]),
         "normpre_attention_plan_tiles": (ctypes.c_int, [ctypes.c_int64, i64p, i64p]),
         "normpre_attention_plan": (ctypes.c_int, [ctypes.c_int64, i64p, ctypes.c_int, P, ctypes.c_int64]),
+        "normpre_attention_workspace": (ctypes.c_int, [ctypes.POINTER(normpre_attention), i64p]),
         "normpre_attention_forward": (ctypes.c_int, [ctypes.POINTER(normpre_attention), P]),
         "normpre_attention_backward": (ctypes.c_int, [ctypes.POINTER(normpre_attention), P]),
         "normpre_checkpoint_pack": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int64, ctypes.c_int64,
@@ -415,6 +417,14 @@ def normpre_attention_plan(lens, causal: bool) -> np.ndarray:
     plan = np.zeros((2, tiles.value, 4), dtype=np.int32)
     _check(lib.normpre_attention_plan(n, arr, int(bool(causal)), plan.ctypes.data_as(ctypes.c_void_p), plan.size))
     return plan
+
+
+def normpre_attention_workspace(args: normpre_attention) -> int:
+    out = ctypes.c_int64()
+    code = load_library().normpre_attention_workspace(args, out)
+    if code:
+        _check(code)
+    return out.value
 
 
 def normpre_attention_forward(args: normpre_attention, stream=None) -> None:

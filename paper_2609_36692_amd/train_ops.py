@@ -82,7 +82,7 @@ def _rows(x: torch.Tensor) -> torch.Tensor:
 
 # normpre_attention (include/normpre.h) in one piece: filling a ctypes structure
 # field by field takes as long as the launch itself.
-_ARGS = struct.Struct("=5if3q" + "Q2q" * 4 + "Q" + "Q2q" * 4 + "Q")
+_ARGS = struct.Struct("=5if3q" + "Q2q" * 4 + "Q" + "Q2q" * 4 + "Qq")
 _NONE = (0, 0, 0)
 
 
@@ -121,7 +121,7 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: A
     tokens, heads, _ = q.shape
     out = q.new_empty(q.shape)
     lse = q.new_empty((heads, tokens), dtype=torch.float32)
-    block = _ARGS.pack(*args, *_heads(out), lse.data_ptr(), *_NONE * 4, 0)
+    block = _ARGS.pack(*args, *_heads(out), lse.data_ptr(), *_NONE * 4, 0, 0)
     N.normpre_attention_forward(N.normpre_attention.from_buffer_copy(block), _stream(q))
     return out, lse
 
@@ -142,10 +142,12 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
         with torch.cuda.device(q.device):
             return attention_backward(dout, q, k, v, out, lse, plan, scale)
     dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
-    work = lse.new_empty((2, *lse.shape))
-    block = _ARGS.pack(*args, *_heads(out), lse.data_ptr(), *_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv),
-                       work.data_ptr())
-    N.normpre_attention_backward(N.normpre_attention.from_buffer_copy(block), _stream(q))
+    block = N.normpre_attention.from_buffer_copy(_ARGS.pack(
+        *args, *_heads(out), lse.data_ptr(), *_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv), 0, 0))
+    block.workspace_bytes = N.normpre_attention_workspace(block)
+    work = lse.new_empty(block.workspace_bytes, dtype=torch.uint8)
+    block.workspace = work.data_ptr()
+    N.normpre_attention_backward(block, _stream(q))
     return dq, dk, dv
 
 

@@ -72,6 +72,23 @@ def test_attention_matches_reference(dev, dtype, lens, hq, hk, d, causal):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("crowd", [0, 250, 400, 600])
+@pytest.mark.parametrize("nonfinite", [False, True])
+def test_attention_in_a_crowd(dev, dtype, d, crowd, nonfinite):
+    # How blocks share their work goes by the size of the batch: the same long
+    # sequences alone and among ever more one-token ones.
+    lens = [1] * (crowd // 2) + [300, 129] + [1] * (crowd - crowd // 2)
+    q, k, v, dout = _qkv(dev, 25, sum(lens), 1, 1, d, dtype)
+    if nonfinite:
+        at = crowd // 2 + 200
+        v[at, 0, 5] = float("inf")
+        k[at + 20, 0, 2] = float("nan")
+        dout[at + 40, 0, 1] = float("-inf")
+    _check(q, k, v, dout, lens, True)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
 def test_attention_scales(dev, dtype, scale):
     q, k, v, dout = _qkv(dev, 5, 97, 2, 1, 64, dtype)

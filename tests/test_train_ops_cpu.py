@@ -64,7 +64,7 @@ def _block(**over):
     rows = lambda i, h: N.normpre_heads(at + (i << 30), h * 64, 64)  # noqa: E731
     a = N.normpre_attention(dtype=1, heads=4, kv_heads=2, head_dim=64, causal=1, scale=0.125, tokens=100, plan=at,
                             num_tiles=1, q=rows(1, 4), k=rows(2, 2), v=rows(3, 2), out=rows(4, 4), lse=at + (5 << 30),
-                            dout=rows(6, 4), dq=rows(7, 4), dk=rows(8, 2), dv=rows(9, 2), workspace=at + (10 << 30))
+                            dout=rows(6, 4), dq=rows(7, 4), dk=rows(8, 2), dv=rows(9, 2), workspace=at + (10 << 30), workspace_bytes=1 << 30)
     for k, v in over.items():
         setattr(a, k, v)
     return a
@@ -87,7 +87,8 @@ P = 1 << 40
     (True, {"out": H(None, 256, 64)}, INVALID),
     (False, {"dout": H(None, 256, 64)}, INVALID), (False, {"dq": H(P, 255, 64)}, INVALID),
     (False, {"dk": H(P, 0, 64)}, INVALID), (False, {"dv": H(P, 128, 63)}, INVALID),
-    (False, {"workspace": None}, INVALID), (False, {"workspace": P + 1}, INVALID),
+    (False, {"workspace": None}, INVALID), (False, {"workspace": P + 4}, INVALID),
+    (False, {"workspace_bytes": 4 * 2 * 4 * 100 - 1}, INVALID),
     (True, {"tokens": 2 ** 31 - 1, "num_tiles": 2 ** 31 - 1}, UNSUPPORTED),
 ])
 def test_attention_refusals(lib, both, over, code):
@@ -109,6 +110,19 @@ def test_attention_null_block_and_empty_batch(lib):
     empty = _block(tokens=0, num_tiles=0, q=H(None, 0, 0), plan=None)
     assert lib.normpre_attention_forward(ctypes.byref(empty), None) == 0
     assert lib.normpre_attention_backward(ctypes.byref(empty), None) == 0
+
+
+def test_attention_workspace(lib):
+    a = _block()
+    size = ctypes.c_int64()
+    assert lib.normpre_attention_workspace(ctypes.byref(a), ctypes.byref(size)) == 0
+    assert size.value >= 4 * 2 * 4 * 100
+    a.workspace_bytes = size.value - 1
+    assert lib.normpre_attention_backward(ctypes.byref(a), None) == INVALID
+    assert lib.normpre_attention_workspace(ctypes.byref(a), None) == INVALID
+    assert lib.normpre_attention_workspace(None, ctypes.byref(size)) == INVALID
+    a.head_dim = 0
+    assert lib.normpre_attention_workspace(ctypes.byref(a), ctypes.byref(size)) == INVALID
 
 
 def test_checkpoint_refusals(lib):

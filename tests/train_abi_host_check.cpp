@@ -16,6 +16,8 @@ namespace np {
 int set_thread_error(int code, const char* msg) { g_error = msg; return code; }
 hipError_t launch_attention_forward(DType, const AttnArgs&, hipStream_t) { ++g_launches; return hipSuccess; }
 hipError_t launch_attention_backward(DType, const AttnArgs&, hipStream_t) { ++g_launches; return hipSuccess; }
+int attention_splits(int64_t, int) { return 2; }
+int64_t attention_workspace(const AttnArgs& a) { return 2 * (int64_t)a.heads * a.tokens; }
 hipError_t launch_ckpt_pack(DType, Act, const CkptPackArgs&, hipStream_t) { ++g_launches; return hipSuccess; }
 hipError_t launch_ckpt_unpack(DType, const CkptUnpackArgs&, hipStream_t) { ++g_launches; return hipSuccess; }
 hipError_t launch_ckpt_act_grad(DType, Act, const CkptGradArgs&, hipStream_t) { ++g_launches; return hipSuccess; }
@@ -60,7 +62,10 @@ int main() {
     a.num_tiles = 1;
     a.q = a.out = a.dout = a.dq = {mem, 256, 64};
     a.k = a.v = a.dk = a.dv = {mem, 128, 64};
-    a.lse = a.workspace = reinterpret_cast<float*>(mem);
+    a.lse = reinterpret_cast<float*>(mem);
+    a.workspace = mem;
+    EXPECT(normpre_attention_workspace(&a, &a.workspace_bytes), NORMPRE_OK);
+    EXPECT(a.workspace_bytes, 4 * 2 * 4 * 100);
     EXPECT(normpre_attention_forward(&a, nullptr), NORMPRE_OK);
     EXPECT(normpre_attention_backward(&a, nullptr), NORMPRE_OK);
     EXPECT(g_launches, 2);
