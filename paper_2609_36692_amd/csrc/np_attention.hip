@@ -66,6 +66,9 @@ __device__ __forceinline__ u32x4 load_chunk(const T* row, int chunk, int dim, bo
     const int d = chunk * E;
     if constexpr (VEC) {
         if (live && d < dim) r = *reinterpret_cast<const u32x4*>(row + d);
+    } else if (live && d + E <= dim) {               // at any element
+        typedef u32x4 u32x4_any __attribute__((aligned(2)));
+        r = *reinterpret_cast<const u32x4_any*>(row + d);
     } else {
         T e[E];
 #pragma unroll
