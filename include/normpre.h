@@ -516,7 +516,7 @@ int normpre_attention_workspace(const normpre_attention* a, int64_t* bytes);
  * a multiple of kv_heads, head_dim < 1, negative strides, an output whose
  * rows overlap, a non-finite scale, num_tiles < 0, causal not 0 or 1, tokens
  * and num_tiles that contradict each other), UNSUPPORTED (head_dim > 128,
- * 2^31 tokens, strides above 2^40, more than 2^31 - 1 blocks), HIP.  INVALID_ARG
+ * 2^31 tokens, strides above 2^40, num_tiles * heads above 2^23 - 1), HIP.  INVALID_ARG
  * too for a workspace that is missing, misaligned or too small.
  */
 int normpre_attention_forward(const normpre_attention* a, void* stream);
@@ -533,8 +533,8 @@ int normpre_attention_backward(const normpre_attention* a, void* stream);
  *   codes: int8 [rows][pitch], pitch = cols rounded up to 64; 16-byte aligned
  *   exps : int8 [rows][pitch / 64]
  * The padding of a row is written as codes 0.
- * ld_*: row strides in elements, >= cols; rows on 16 bytes are accessed in
- * 16-byte pieces.  rows = 0 is a successful no-op.
+ * ld_*: row strides in elements, >= cols; any alignment of an element.  rows = 0
+ * is a successful no-op.
  */
 #define NORMPRE_CHECKPOINT_GROUP 64
 #define NORMPRE_ACT_NONE   0    /* checkpoint of u alone                        */
@@ -549,7 +549,8 @@ int normpre_attention_backward(const normpre_attention* a, void* stream);
  * NORMPRE_ACT_NONE only packs u; up, h and their checkpoints are ignored, as
  * is up with NORMPRE_ACT_GELU.
  * Errors: INVALID_ARG (unknown act or dtype, null or misaligned pointers,
- * rows < 0, cols < 1, ld < cols), UNSUPPORTED (more than 2^40 elements), HIP.
+ * rows < 0, cols < 1, ld < cols), UNSUPPORTED (more than 2^34 elements, a row
+ * stride above 2^40), HIP.
  */
 int normpre_checkpoint_pack(int act, int dtype, int64_t rows, int64_t cols,
                             const void* u, int64_t ld_u, const void* up, int64_t ld_up,
@@ -585,8 +586,8 @@ int normpre_checkpoint_act_grad(int act, int dtype, int64_t rows, int64_t cols, 
  * workspace: normpre_checkpoint_weight_grad_workspace() bytes, 16-byte aligned
  * (null where that is 0).
  * Errors: INVALID_ARG (as above, unknown layout, accumulate not 0 or 1, too
- * small a workspace), UNSUPPORTED (a dimension above 2^31 - 1, more than 2^40
- * elements), HIP.
+ * small a workspace), UNSUPPORTED (2^31 tokens or more, more than 2^29 features,
+ * more than 2^34 elements), HIP.
  */
 int normpre_checkpoint_weight_grad_workspace(int dtype, int64_t tokens, int64_t inner, int64_t outer,
                                              int64_t* bytes);

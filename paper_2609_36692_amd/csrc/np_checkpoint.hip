@@ -164,7 +164,8 @@ __global__ void __launch_bounds__(kThreads) act_grad_kernel(CkptGradArgs a, int6
 #pragma unroll
         for (int j = 0; j < kV; ++j) {
             const float x = u[j], s = logistic(kGeluA * (x + kGeluB * x * x * x));
-            u[j] = dh[j] * (s + x * s * (1.f - s) * kGeluA * (1.f + 3.f * kGeluB * x * x));
+            // Far out s (1 - s) is 0: x^2 must not overflow beside it.
+            u[j] = dh[j] * (s + x * s * (1.f - s) * kGeluA * (1.f + 3.f * kGeluB * fminf(x * x, 1e30f)));
         }
     } else {
         float g[kV];

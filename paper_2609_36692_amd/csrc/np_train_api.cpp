@@ -19,8 +19,11 @@ namespace {
 
 constexpr int64_t kMaxTokens = INT32_MAX;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
-constexpr int64_t kMaxElements = int64_t(1) << 40;
-constexpr int64_t kMaxBlocks = INT32_MAX;
+// A launch holds fewer than 2^32 threads a dimension: blocks of up to 512, and
+// eight elements a thread.
+constexpr int64_t kMaxElements = int64_t(1) << 34;
+constexpr int64_t kMaxBlocks = (int64_t(1) << 23) - 1;
+constexpr int64_t kMaxFeatures = int64_t(1) << 29;
 
 int fail(int code, const char* f, ...) {
     char buf[256];
@@ -92,7 +95,7 @@ int check_sizes(const normpre_attention* a) {
     if (a->num_tiles > a->tokens || a->num_tiles * kAttnRows < a->tokens)
         return fail(NORMPRE_ERR_INVALID_ARG, "%lld tiles cannot hold %lld tokens", (long long)a->num_tiles,
                     (long long)a->tokens);
-    if (a->num_tiles * a->heads > kMaxBlocks) return fail(NORMPRE_ERR_UNSUPPORTED, "more than 2^31 - 1 blocks");
+    if (a->num_tiles * a->heads > kMaxBlocks) return fail(NORMPRE_ERR_UNSUPPORTED, "more than 2^23 - 1 blocks of 128 rows");
     return NORMPRE_OK;
 }
 
@@ -162,7 +165,7 @@ int check_matrix(int dtype, int64_t rows, int64_t cols) {
     if (rows < 0 || cols < 1)
         return fail(NORMPRE_ERR_INVALID_ARG, "bad shape %lld x %lld", (long long)rows, (long long)cols);
     if (cols > kMaxElements || rows > kMaxElements / ckpt_pitch(cols))
-        return fail(NORMPRE_ERR_UNSUPPORTED, "more than 2^40 elements");
+        return fail(NORMPRE_ERR_UNSUPPORTED, "more than 2^34 elements");
     return NORMPRE_OK;
 }
 
@@ -322,8 +325,8 @@ static int check_weight(int dtype, int64_t tokens, int64_t inner, int64_t outer)
     NP_CHECK(check_matrix(dtype, tokens, inner));
     NP_CHECK(check_matrix(dtype, tokens, outer));
     NP_CHECK(check_matrix(dtype, inner, outer));
-    if (tokens > INT32_MAX || inner > INT32_MAX || outer > INT32_MAX)
-        return fail(NORMPRE_ERR_UNSUPPORTED, "a dimension above 2^31 - 1");
+    if (tokens > kMaxTokens || inner > kMaxFeatures || outer > kMaxFeatures)
+        return fail(NORMPRE_ERR_UNSUPPORTED, "2^31 tokens or more, or more than 2^29 features");
     return NORMPRE_OK;
 }
 

@@ -337,7 +337,7 @@ class _Linear(torch.autograd.Function):
         y = _times(x, w, layout)
         if bias is not None:
             y += bias.to(y.dtype)
-        ctx.layout, ctx.bias, ctx.cols = layout, bias is not None, x.shape[1]
+        ctx.layout, ctx.bias, ctx.cols = layout, None if bias is None else bias.dtype, x.shape[1]
         c = checkpoint_pack(x) if ctx.needs_input_grad[1] else None
         ctx.save_for_backward(weight, *(() if c is None else (c.codes, c.exps)))
         return y
@@ -350,18 +350,19 @@ class _Linear(torch.autograd.Function):
         dw = None
         if held:
             dw = checkpoint_weight_grad(Checkpoint(*held, ctx.cols), dy, ctx.layout).to(weight.dtype)
-        db = dy.sum(0, dtype=torch.float32).to(weight.dtype) if ctx.bias and ctx.needs_input_grad[2] else None
+        db = dy.sum(0, dtype=torch.float32).to(ctx.bias) if ctx.needs_input_grad[2] else None
         return dx, dw, db, None
 
 
 def checkpointed_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None,
                         layout: str = "oi") -> torch.Tensor:
     """A linear layer on x [tokens, inner] that keeps x in 8 bits for its weight
-    gradient.  The product runs in x's type; weights and their gradients may be
-    fp32.  layout: "oi" for y = x W^T, "io" for y = x W."""
+    gradient.  The product runs in x's type, also under autocast; weights and
+    their gradients may be fp32.  layout: "oi" for y = x W^T, "io" for y = x W."""
     if layout not in _LAYOUTS:
         raise ValueError("layout is 'io' or 'oi'")
-    return _Linear.apply(x, weight, bias, layout)
+    with torch.autocast("cuda", enabled=False):
+        return _Linear.apply(x, weight, bias, layout)
 
 
 class _Mlp(torch.autograd.Function):
@@ -377,7 +378,7 @@ class _Mlp(torch.autograd.Function):
             y += b_out.to(y.dtype)
         cx = checkpoint_pack(x)
         ctx.act, ctx.layout, ctx.cols = act, layout, (x.shape[1], u.shape[1])
-        ctx.bias = b_in is not None, b_out is not None
+        ctx.bias = tuple(None if b is None else b.dtype for b in (b_in, b_out))
         held = [cx, cu, ch] + ([] if cup is None else [cup])
         ctx.save_for_backward(w_in, w_up, w_out, *(t for c in held for t in (c.codes, c.exps)))
         return y
@@ -389,16 +390,19 @@ class _Mlp(torch.autograd.Function):
         inner, mid = ctx.cols
         cx, cu, ch = (Checkpoint(*held[2 * i:2 * i + 2], c) for i, c in enumerate((inner, mid, mid)))
         cup = Checkpoint(*held[6:8], mid) if w_up is not None else None
+        need = ctx.needs_input_grad
         dh = _back(dy, w_out.to(dy.dtype), ctx.layout)
-        d_out = checkpoint_weight_grad(ch, dy, ctx.layout).to(w_out.dtype)
         du, dup = checkpoint_act_grad(ctx.act, dh, cu, cup)
-        d_in = checkpoint_weight_grad(cx, du, ctx.layout).to(w_in.dtype)
-        dx, d_up = _back(du, w_in.to(du.dtype), ctx.layout), None
-        if dup is not None:
-            d_up = checkpoint_weight_grad(cx, dup, ctx.layout).to(w_up.dtype)
-            dx += _back(dup, w_up.to(dup.dtype), ctx.layout)
-        b_in = du.sum(0, dtype=torch.float32).to(w_in.dtype) if ctx.bias[0] else None
-        b_out = dy.sum(0, dtype=torch.float32).to(w_out.dtype) if ctx.bias[1] else None
+        d_out = checkpoint_weight_grad(ch, dy, ctx.layout).to(w_out.dtype) if need[6] else None
+        d_in = checkpoint_weight_grad(cx, du, ctx.layout).to(w_in.dtype) if need[3] else None
+        d_up = checkpoint_weight_grad(cx, dup, ctx.layout).to(w_up.dtype) if need[5] else None
+        dx = None
+        if need[0]:
+            dx = _back(du, w_in.to(du.dtype), ctx.layout)
+            if dup is not None:
+                dx += _back(dup, w_up.to(dup.dtype), ctx.layout)
+        b_in = du.sum(0, dtype=torch.float32).to(ctx.bias[0]) if need[4] else None
+        b_out = dy.sum(0, dtype=torch.float32).to(ctx.bias[1]) if need[7] else None
         return dx, None, None, d_in, b_in, d_up, d_out, b_out
 
 
@@ -413,4 +417,5 @@ def checkpointed_mlp(x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *
         raise ValueError("act is 'gelu', or 'swiglu' with w_up")
     if layout not in _LAYOUTS:
         raise ValueError("layout is 'io' or 'oi'")
-    return _Mlp.apply(x, act, layout, w_in, b_in, w_up, w_out, b_out)
+    with torch.autocast("cuda", enabled=False):
+        return _Mlp.apply(x, act, layout, w_in, b_in, w_up, w_out, b_out)

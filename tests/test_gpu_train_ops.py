@@ -370,6 +370,20 @@ def test_act_grad(dev, dtype, act, rows, cols):
 
 
 @pytest.mark.parametrize("act", ["gelu", "swiglu"])
+def test_act_far_out(dev, act):
+    # Far from zero the derivative is 0 or 1 (times up), whatever the formula's
+    # terms do on the way.
+    big = torch.tensor([1e3, 1e8, 1e20, 1e37], device=dev)
+    u = torch.stack([big, -big])[:, :, None].expand(2, 4, 64).reshape(2, 256)
+    cu = T.checkpoint_pack(u)
+    cup = T.checkpoint_pack(torch.ones(2, 256, device=dev)) if act == "swiglu" else None
+    du, _ = T.checkpoint_act_grad(act, torch.ones(2, 256, device=dev), cu, cup)
+    assert torch.equal(du, torch.tensor([[1.0], [0.0]], device=dev).expand(2, 256))
+    h = T.checkpoint_act(act, u, None if cup is None else torch.ones(2, 256, device=dev))[0]
+    assert torch.equal(h, u.clamp(min=0))
+
+
+@pytest.mark.parametrize("act", ["gelu", "swiglu"])
 def test_act_grad_against_differences(dev, act):
     # Central differences of the activation at the held values, in 64 bits: step
     # 2^-12, third derivatives below 4 here, so the error is below 4 2^-24 / 6,
@@ -531,6 +545,19 @@ def test_checkpointed_mlp_against_formula(dev, act, layout):
         # amax / 63 at a few places; fp32 elsewhere.
         err = np.linalg.norm(got[name] - want[name]) / np.linalg.norm(want[name])
         assert err <= 1e-3, (name, err)
+
+
+def test_checkpointed_layers_with_frozen_parts(dev):
+    x = torch.randn(40, 64, device=dev)
+    w1, w2 = torch.randn(128, 64, device=dev), torch.randn(64, 128, device=dev).requires_grad_()
+    b = torch.randn(128, device=dev, dtype=torch.float64).requires_grad_()
+    with torch.autocast("cuda", torch.bfloat16):
+        y = T.checkpointed_mlp(T.checkpointed_linear(x, w1, b) @ w1, w1, w2)
+    assert y.dtype == BF16
+    y.float().sum().backward()
+    assert w1.grad is None and w2.grad.shape == w2.shape and b.grad.dtype == torch.float64
+    with torch.no_grad():
+        assert torch.equal(T.checkpointed_linear(x, w1, layout="oi"), x @ w1.t())
 
 
 def test_checkpointed_layers_keep_8_bits(dev):
