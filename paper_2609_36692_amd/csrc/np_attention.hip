@@ -203,27 +203,41 @@ struct Owned {
     }
 };
 
-// 32 x 32 scores: streamed rows [base, base + 32) of the tile against the
-// wave's owned rows.  Lane l gets owned row l % 32, register r streamed row
-// base + 8 (r / 4) + 4 (l / 32) + r % 4.
-template <class T, int DP>
-__device__ __forceinline__ f32x16 scores(const T* lds, int base, const Owned<T, DP>& b, int lane) {
+// N blocks of 32 x 32 scores: streamed rows [base[n], base[n] + 32) of a tile
+// against the wave's owned rows.  Lane l gets owned row l % 32, register r
+// streamed row base + 8 (r / 4) + 4 (l / 32) + r % 4.  The blocks take turns, so
+// that no product waits for the one before it.
+template <class T, int DP, int N>
+__device__ __forceinline__ void scores(f32x16 (&acc)[N], const T* const (&lds)[N], const int (&base)[N],
+                                       const Owned<T, DP>* const (&own)[N], int lane) {
     using TL = Tile<T, DP>;
-    f32x16 acc = {};
-    const int row = base + (lane & 31), half = lane >> 5;
+    const int half = lane >> 5;
 #pragma unroll
-    for (int s = 0; s < Owned<T, DP>::S; ++s) {
-        const u32x4 a = *reinterpret_cast<const u32x4*>(lds + TL::idx(row, 2 * s + half));
-        if constexpr (std::is_same_v<T, bf16_t>) {
-            acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                          __builtin_bit_cast(bf16x8, b.c[s]), acc, 0, 0, 0);
-        } else {
-            const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b.c[s]);
+    for (int n = 0; n < N; ++n) acc[n] = f32x16{};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], acc, 0, 0, 0);
+    for (int s = 0; s < Owned<T, DP>::S; ++s)
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const u32x4 a = *reinterpret_cast<const u32x4*>(lds[n] + TL::idx(base[n] + (lane & 31), 2 * s + half));
+            if constexpr (std::is_same_v<T, bf16_t>) {
+                acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                                 __builtin_bit_cast(bf16x8, own[n]->c[s]), acc[n], 0, 0, 0);
+            } else {
+                const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, own[n]->c[s]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], acc[n], 0, 0, 0);
+            }
         }
-    }
-    return acc;
+}
+
+template <class T, int DP>
+__device__ __forceinline__ f32x16 scores(const T* lds, int base, const Owned<T, DP>& own, int lane) {
+    f32x16 acc[1];
+    const T* const l[1] = {lds};
+    const int b[1] = {base};
+    const Owned<T, DP>* const o[1] = {&own};
+    scores<T, DP, 1>(acc, l, b, o, lane);
+    return acc[0];
 }
 
 // acc[t] (features 32 t .. of the result, by owned row) += tile^T weights,
@@ -662,18 +676,22 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
     const Pair<T, DP, BN, VEC, NT> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
     // p (dp - de) of streamed rows k0 + 32 b .., zero where the row does not see them.
     auto weights = [&](const T* ks, const T* vs, int k0, int b, float de) {
-        f32x16 s = scores<T, DP>(ks, 32 * b, q, lane);
-        const f32x16 dp = scores<T, DP>(vs, 32 * b, dout, lane);
+        f32x16 s[2];
+        const T* const lds[2] = {ks, vs};
+        const int base[2] = {32 * b, 32 * b};
+        const Owned<T, DP>* const own[2] = {&q, &dout};
+        scores<T, DP, 2>(s, lds, base, own, lane);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = exp2_fast(__builtin_fmaf(s[r], c2, -lse2)) * (dp[r] - de);
-        if (k0 + BN > w.len || (a.causal && k0 + BN - 1 > qw)) {
-            const int last = a.causal ? min(qi, w.len - 1) : w.len - 1;
+        for (int r = 0; r < 16; ++r) s[0][r] = exp2_fast(__builtin_fmaf(s[0][r], c2, -lse2)) * (s[1][r] - de);
+        if (k0 + 32 * b + 32 > w.len || (a.causal && k0 + 32 * b + 31 > qw)) {
+            const int last = (a.causal ? min(qi, w.len - 1) : w.len - 1) - k0 - 32 * b - 4 * half;
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (k0 + 32 * b + 8 * (r / 4) + 4 * half + r % 4 > last) s[r] = 0.f;
+            for (int r = 0; r < 16; ++r) s[0][r] = 8 * (r / 4) + r % 4 > last ? 0.f : s[0][r];
         }
-        return s;
+        return s[0];
     };
+    // Whether some row of the wave sees block b of the tile from k0 on.
+    auto seen = [&](int k0, int b) { return k0 + 32 * b < end && (!a.causal || k0 + 32 * b <= qw + 31); };
     // delta = do . o carries the rounding of o.  Where a row sees few keys, o
     // is as large as a value and that error as large as the other ones, so
     // blocks with up to kAttnRows keys first sum delta = sum_j p dp from the
@@ -686,14 +704,13 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
         for (int it = 0; it < rounds; ++it) {
             const int k0 = (it * TEAMS + team) * BN;
             keys.next(smem, it, k0, it * TEAMS + team + TEAMS < steps ? k0 + TEAMS * BN : -1, tid);
-            if (k0 < end && (!a.causal || k0 <= qw + 31)) {
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
+            for (int b = 0; b < NB; ++b)
+                if (seen(k0, b)) {
                     const f32x16 s = weights(smem[it & 1][0], smem[it & 1][1], k0, b, 0.f);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sum += s[r];
                 }
-            }
         }
         delta = sum + __shfl_xor(sum, 32, 64);
         if (TEAMS > 1 && half == 0) stat[team][wave * 32 + lane] = delta;
@@ -710,10 +727,9 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
         const int k0 = (it * TEAMS + team) * BN;
         keys.next(smem, it, k0, it * TEAMS + team + TEAMS < steps ? k0 + TEAMS * BN : -1, tid);
         const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
-        if (k0 < end && (!a.causal || k0 <= qw + 31)) {    // same for the whole wave
 #pragma unroll
-            for (int b = 0; b < NB; ++b) accumulate<T, DP>(g, ks, 32 * b, weights(ks, vs, k0, b, delta), lane);
-        }
+        for (int b = 0; b < NB; ++b)
+            if (seen(k0, b)) accumulate<T, DP>(g, ks, 32 * b, weights(ks, vs, k0, b, delta), lane);
     }
     lds_barrier();                                   // the tiles are free
     T* mine = &smem[0][0][0] + wave * (BN * DP * 4 / WR);
@@ -789,7 +805,12 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
         for (int b = 0; b < NB; ++b) {
             const int qb = q0 + 32 * b;
             if (qb >= w.len || (a.causal && qb + 31 < kw)) continue;   // same for the whole wave
-            f32x16 p = scores<T, DP>(qs, 32 * b, k, lane);
+            f32x16 pd[2];
+            const T* const lds[2] = {qs, ds};
+            const int base[2] = {32 * b, 32 * b};
+            const Owned<T, DP>* const own[2] = {&k, &v};
+            scores<T, DP, 2>(pd, lds, base, own, lane);
+            f32x16 &p = pd[0], &dp = pd[1];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const f32x4 ls = *reinterpret_cast<const f32x4*>(lse2 + 32 * b + 8 * j + 4 * half);
@@ -807,7 +828,6 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
                 }
             }
             accumulate<T, DP>(gv, ds, 32 * b, p, lane);
-            f32x16 dp = scores<T, DP>(ds, 32 * b, v, lane);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const f32x4 de = *reinterpret_cast<const f32x4*>(delta + 32 * b + 8 * j + 4 * half);
