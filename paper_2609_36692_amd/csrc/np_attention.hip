@@ -197,6 +197,13 @@ struct Owned {
 #pragma unroll
         for (int s = 0; s < S; ++s) c[s] = load_chunk<T, VEC>(row, 2 * s + half, dim, live);
     }
+    // From a tile in LDS, rows [base, base + 32).
+    __device__ __forceinline__ void load(const T* lds, int base, int lane) {
+        using TL = Tile<T, DP>;
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+            c[s] = *reinterpret_cast<const u32x4*>(lds + TL::idx(base + (lane & 31), 2 * s + (lane >> 5)));
+    }
     __device__ __forceinline__ void negate() {
 #pragma unroll
         for (int s = 0; s < S; ++s) c[s] ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
@@ -752,10 +759,13 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
     }
 }
 
-template <class T, int DP, bool VEC>
-__global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kernel(AttnArgs a) {
-    constexpr int BM = kStream<T>, NB = BM / 32, DT = DP / 32;
-    __shared__ __attribute__((aligned(16))) T smem[2][2][BM * DP];
+// HELD: v's rows wait in LDS instead of registers.
+template <class T, int DP, bool VEC, bool HELD>
+__global__ void __launch_bounds__(kThreads, (HELD ? 2 : waves<T, DP>(2, 2))) attn_dkv_kernel(AttnArgs a) {
+    constexpr int BM = HELD ? 32 : kStream<T>, NB = BM / 32, DT = DP / 32;
+    __shared__ __attribute__((aligned(16))) char shared[4 * BM * DP * sizeof(T) + (HELD ? kAttnRows * DP * sizeof(T) : 0)];
+    auto& smem = *reinterpret_cast<T (*)[2][2][BM * DP]>(shared);
+    T* vrows = reinterpret_cast<T*>(shared) + 4 * BM * DP;   // of the block, if held
     __shared__ __attribute__((aligned(16))) float stat[2][2][BM];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int group = a.heads / a.kv_heads;
@@ -768,9 +778,15 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
     const int kw = kt + wave * 32, ki = kw + (lane & 31);
     const bool live = ki < w.len;
 
-    Owned<T, DP> k, v;
+    Owned<T, DP> k;
+    Owned<T, HELD ? 32 : DP> v;                      // not used if held in LDS
     k.template load<VEC>(row_of<T>(a.k, w, live ? ki : 0, kv), a.dim, live, half);
-    v.template load<VEC>(row_of<T>(a.v, w, live ? ki : 0, kv), a.dim, live, half);
+    if constexpr (HELD) {                            // with zeros for what is not there, as in registers
+        using ST = Stage<T, DP, kAttnRows, true, kThreads>;
+        u32x4 r[ST::N];
+        ST::load(r, row_of<T>(a.v, w, 0, kv), a.v.tok, kt, w.len, a.dim, tid);
+        ST::store(r, vrows, tid);
+    } else v.template load<VEC>(row_of<T>(a.v, w, live ? ki : 0, kv), a.dim, live, half);
     const int first = a.causal ? kt / BM : 0, per = (w.len + BM - 1) / BM - first;
     // Steps of this block's share; step i: queries of tile first + i % per, head
     // kv * group + i / per.
@@ -784,7 +800,9 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
         const int h = w.head + i / per, row0 = (first + i % per) * BM;
         const Pair<T, DP, BM, VEC, kThreads> rows{row_of<T>(a.q, w, 0, h), a.q.tok, row_of<T>(a.dout, w, 0, h), a.dout.tok,
                                         w.len, a.dim};
-        rows.fill(smem[buf], row0, tid);
+        int td = tid;
+        if constexpr (HELD) asm volatile("" : "+v"(td));     // as below
+        rows.fill(smem[buf], row0, td);
         if (tid < 2 * BM) {                          // whole waves
             const float* src = (tid < BM ? a.lse2 : a.delta) + h * a.tokens + w.start + min(row0 + tid % BM, w.len - 1);
             __builtin_amdgcn_global_load_lds(
@@ -800,17 +818,25 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
         lds_barrier();
         if (it + 1 < steps) fetch(it + 1, (it + 1) & 1);
         const T *qs = smem[it & 1][0], *ds = smem[it & 1][1];
+        // The lane as of this step: addresses in LDS are then made anew in each, and
+        // take no registers from one to the next.
+        int ln = lane;
+        if constexpr (HELD) asm volatile("" : "+v"(ln));
         const float *lse2 = stat[it & 1][0], *delta = stat[it & 1][1];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             const int qb = q0 + 32 * b;
             if (qb >= w.len || (a.causal && qb + 31 < kw)) continue;   // same for the whole wave
             f32x16 pd[2];
-            const T* const lds[2] = {qs, ds};
-            const int base[2] = {32 * b, 32 * b};
-            const Owned<T, DP>* const own[2] = {&k, &v};
-            scores<T, DP, 2>(pd, lds, base, own, lane);
             f32x16 &p = pd[0], &dp = pd[1];
+            if constexpr (HELD) {
+                p = scores<T, DP>(qs, 32 * b, k, ln);
+            } else {
+                const T* const lds[2] = {qs, ds};
+                const int base[2] = {32 * b, 32 * b};
+                const Owned<T, DP>* const own[2] = {&k, &v};
+                scores<T, DP, 2>(pd, lds, base, own, ln);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const f32x4 ls = *reinterpret_cast<const f32x4*>(lse2 + 32 * b + 8 * j + 4 * half);
@@ -827,7 +853,12 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
                     if (row < from || row >= w.len) p[r] = 0.f;
                 }
             }
-            accumulate<T, DP>(gv, ds, 32 * b, p, lane);
+            accumulate<T, DP>(gv, ds, 32 * b, p, ln);
+            if constexpr (HELD) {
+                Owned<T, DP> held;
+                held.load(vrows, wave * 32, ln);
+                dp = scores<T, DP>(ds, 32 * b, held, ln);
+            }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const f32x4 de = *reinterpret_cast<const f32x4*>(delta + 32 * b + 8 * j + 4 * half);
@@ -841,11 +872,11 @@ __global__ void __launch_bounds__(kThreads, (waves<T, DP>(2, 2))) attn_dkv_kerne
                     if (row < from || row >= w.len) dp[r] = 0.f;
                 }
             }
-            accumulate<T, DP>(gk, qs, 32 * b, dp, lane);
+            accumulate<T, DP>(gk, qs, 32 * b, dp, ln);
         }
     }
     lds_barrier();                                   // the tiles are free
-    T* mine = &smem[0][0][0] + wave * (BM * DP);
+    T* mine = reinterpret_cast<T*>(shared + wave * (sizeof shared / 4));
     const uint32_t keep = live_rows(kw, w.len);
     if (a.splits > 1) {
         const int64_t at = (kv * a.tokens + w.start + kw) * DP, one = (int64_t)a.kv_heads * a.tokens * DP;
@@ -939,7 +970,15 @@ hipError_t run(const AttnArgs& a, bool backward, hipStream_t s) {
     } else query_pass<T, DP, true, 2, 2>(a, backward, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !backward) return e;
-    attn_dkv_kernel<T, DP, VEC><<<dim3((unsigned)a.num_tiles * a.kv_heads, a.splits), kThreads, 0, s>>>(a);
+    // bf16 heads of 128: with v's rows in LDS two blocks fit a CU instead of one,
+    // for more LDS reads and half tiles.  us with them there / in registers: packed
+    // 16418 tokens (1032 blocks) 827 / 873, 16 x 2048 (2048) 1146 / 1254, 4 x 8192
+    // (2048) 3890 / 4195; 4 x 2048 (512) 338 / 295, 2 x 2048 (256) 222 / 183.
+    const dim3 keys((unsigned)a.num_tiles * a.kv_heads, a.splits);
+    constexpr bool can_hold = VEC && sizeof(T) == 2 && DP == 128;
+    if (can_hold && (int64_t)a.num_tiles * a.kv_heads >= 1024)
+        attn_dkv_kernel<T, DP, VEC, can_hold><<<keys, kThreads, 0, s>>>(a);
+    else attn_dkv_kernel<T, DP, VEC, false><<<keys, kThreads, 0, s>>>(a);
     e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     attn_join_kernel<T, DP><<<dim3((unsigned)a.num_tiles * a.kv_heads, DP / 8), kThreads, 0, s>>>(a);

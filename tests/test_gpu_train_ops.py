@@ -73,7 +73,7 @@ def test_attention_matches_reference(dev, dtype, lens, hq, hk, d, causal):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("crowd", [0, 250, 400, 600])
+@pytest.mark.parametrize("crowd", [0, 250, 400, 600, 1100])
 @pytest.mark.parametrize("nonfinite", [False, True])
 def test_attention_in_a_crowd(dev, dtype, d, crowd, nonfinite):
     # How blocks share their work goes by the size of the batch: the same long
