@@ -6,9 +6,9 @@
 // rint(amax 2^-e) <= 127, and a code is rint(x 2^-e) within +-127.  The step
 // is a power of two so that code 2^e is exact in bf16 (7 bits and a sign):
 // matrix products of checkpoints on the bf16 matrix instructions then add no
-// rounding to that of the codes.  It costs up to one bit against a free
-// step; an 8-bit floating type (3 bits of mantissa) keeps 4% of a value
-// near the top where these codes keep 0.8% of it at worst.
+// rounding to that of the codes.  It costs up to one bit against a free step.
+// An 8-bit floating type with 3 bits of mantissa is off by up to 6% of every
+// value, these codes by up to 0.8% of the group's largest.
 // A group with a NaN or an infinity has codes 0, e = -128, and stands for NaN.
 #include "np_train.h"
 

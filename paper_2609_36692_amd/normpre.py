@@ -215,6 +215,8 @@ def _stream_handle(stream):
     if stream is None:
         import torch
         return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    if isinstance(stream, ctypes.c_void_p):
+        return stream
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)

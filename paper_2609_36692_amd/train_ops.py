@@ -18,6 +18,7 @@ and ``checkpointed_mlp`` are differentiable.
 """
 from __future__ import annotations
 
+import ctypes
 import math
 import struct
 from typing import NamedTuple, Sequence
@@ -38,23 +39,25 @@ def _dtype(x: torch.Tensor) -> int:
     return _DTYPES[x.dtype]
 
 
-def _same(first: torch.Tensor, *others: torch.Tensor) -> None:
-    """Operands of one call share device and type."""
+def _same(first: torch.Tensor, *others: torch.Tensor) -> int:
+    """Operands of one call share device and type; the device's index."""
     if not first.is_cuda:
         raise ValueError("expected tensors on a GPU")
+    at, dtype = first.get_device(), first.dtype
     for x in others:
-        if x.device != first.device or x.dtype != first.dtype:
-            raise ValueError(f"operands differ: {x.dtype} on {x.device}, {first.dtype} on {first.device}")
+        if x.get_device() != at or x.dtype != dtype:
+            raise ValueError(f"operands differ: {x.dtype} on {x.device}, {dtype} on {first.device}")
+    return at
 
 
-def _elsewhere(x: torch.Tensor) -> bool:
-    """Whether x lies on another device than the current one: the calls below then
-    start over with that device current, so that allocations and launches go there."""
-    return x.get_device() != torch.cuda.current_device()
+def _elsewhere(at: int) -> bool:
+    """Whether `at` is not the current device: the calls below then start over with
+    it current, so that allocations and launches go there."""
+    return at != torch.cuda.current_device()
 
 
-def _stream(x: torch.Tensor) -> int:
-    return torch._C._cuda_getCurrentRawStream(x.get_device())
+def _stream(at: int) -> ctypes.c_void_p:
+    return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(at))
 
 
 # ------------------------------------------------------------- attention ---
@@ -92,17 +95,17 @@ def _heads(x: torch.Tensor):
 
 
 def _attention_args(q, k, v, plan: AttentionPlan, scale):
-    """The fields up to v; checks the operands."""
+    """(device index, the fields up to v); checks the operands."""
     tokens, heads, dim = q.shape
-    if k.dim() != 3 or v.shape != k.shape or k.shape[0] != tokens or k.shape[2] != dim or tokens != plan.tokens:
+    ks = k.shape
+    if len(ks) != 3 or v.shape != ks or ks[0] != tokens or ks[2] != dim or tokens != plan.tokens:
         raise ValueError(f"expected q [tokens, heads, dim] and k, v [tokens, kv_heads, dim] of {plan.tokens} tokens, "
                          f"got {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)}")
-    _same(q, k, v)
-    data = plan.data
-    if data.device != q.device:
+    at, data = _same(q, k, v), plan.data
+    if data.get_device() != at:
         raise ValueError("the plan lies on another device")
-    return (_dtype(q), heads, k.shape[1], dim, int(plan.causal), 1.0 / math.sqrt(dim) if scale is None else scale,
-            tokens, data.data_ptr(), plan.num_tiles, *_heads(q), *_heads(k), *_heads(v))
+    return at, (_dtype(q), heads, ks[1], dim, int(plan.causal), 1.0 / math.sqrt(dim) if scale is None else scale,
+                tokens, data.data_ptr(), plan.num_tiles, *_heads(q), *_heads(k), *_heads(v))
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: AttentionPlan,
@@ -114,15 +117,15 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: A
     if q.dim() != 3:
         raise ValueError(f"expected q [tokens, heads, dim], got {tuple(q.shape)}")
     q, k, v = _rows(q), _rows(k), _rows(v)
-    args = _attention_args(q, k, v, plan, scale)
-    if _elsewhere(q):
-        with torch.cuda.device(q.device):
+    at, args = _attention_args(q, k, v, plan, scale)
+    if _elsewhere(at):
+        with torch.cuda.device(at):
             return attention_forward(q, k, v, plan, scale)
-    tokens, heads, _ = q.shape
-    out = q.new_empty(q.shape)
+    tokens, heads, dim = q.shape
+    out = q.new_empty((tokens, heads, dim))
     lse = q.new_empty((heads, tokens), dtype=torch.float32)
-    block = _ARGS.pack(*args, *_heads(out), lse.data_ptr(), *_NONE * 4, 0, 0)
-    N.normpre_attention_forward(N.normpre_attention.from_buffer_copy(block), _stream(q))
+    block = _ARGS.pack(*args, out.data_ptr(), heads * dim, dim, lse.data_ptr(), *_NONE * 4, 0, 0)
+    N.normpre_attention_forward(N.normpre_attention.from_buffer_copy(block), _stream(at))
     return out, lse
 
 
@@ -133,13 +136,13 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     if q.dim() != 3 or out.shape != q.shape or dout.shape != q.shape:
         raise ValueError("q, out and dout are [tokens, heads, dim]")
     q, k, v, out, dout = _rows(q), _rows(k), _rows(v), _rows(out), _rows(dout)
-    args = _attention_args(q, k, v, plan, scale)
+    at, args = _attention_args(q, k, v, plan, scale)
     _same(q, out, dout)
     if lse.shape != (q.shape[1], q.shape[0]) or lse.dtype != torch.float32 or not lse.is_contiguous() \
-            or lse.device != q.device:
+            or lse.get_device() != at:
         raise ValueError("lse is attention_forward's")
-    if _elsewhere(q):
-        with torch.cuda.device(q.device):
+    if _elsewhere(at):
+        with torch.cuda.device(at):
             return attention_backward(dout, q, k, v, out, lse, plan, scale)
     dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
     block = N.normpre_attention.from_buffer_copy(_ARGS.pack(
@@ -147,7 +150,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     block.workspace_bytes = N.normpre_attention_workspace(block)
     work = lse.new_empty(block.workspace_bytes, dtype=torch.uint8)
     block.workspace = work.data_ptr()
-    N.normpre_attention_backward(block, _stream(q))
+    N.normpre_attention_backward(block, _stream(at))
     return dq, dk, dv
 
 
@@ -201,7 +204,7 @@ def _held(c: Checkpoint, rows: int | None = None):
     groups = -(-c.cols // GROUP)
     if not (codes.dtype == exps.dtype == torch.int8 and codes.dim() == 2 and codes.shape[1] == groups * GROUP
             and exps.shape == (codes.shape[0], groups) and codes.is_contiguous() and exps.is_contiguous()
-            and codes.is_cuda and codes.device == exps.device and rows in (None, codes.shape[0])):
+            and codes.is_cuda and codes.get_device() == exps.get_device() and rows in (None, codes.shape[0])):
         raise ValueError("not a checkpoint of this shape on a GPU")
     return codes.data_ptr(), exps.data_ptr()
 
@@ -224,24 +227,25 @@ def _held_args(c: Checkpoint | None):
 def checkpoint_pack(x: torch.Tensor) -> Checkpoint:
     """The 8-bit checkpoint of x [tokens, features]."""
     x = _matrix(x)
-    _same(x)
-    if _elsewhere(x):
-        with torch.cuda.device(x.device):
+    at = _same(x)
+    if _elsewhere(at):
+        with torch.cuda.device(at):
             return checkpoint_pack(x)
     c = _new_checkpoint(x)
     N.normpre_checkpoint_pack(N.NORMPRE_ACT_NONE, _dtype(x), *x.shape, *_row_args(x), *_NOTHING, *_NOTHING,
-                              *_held_args(c), None, None, None, None, _stream(x))
+                              *_held_args(c), None, None, None, None, _stream(at))
     return c
 
 
 def checkpoint_unpack(c: Checkpoint, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The values a checkpoint stands for (exact in bf16 and fp32)."""
-    held = _held(c)
-    if _elsewhere(c.codes):
-        with torch.cuda.device(c.codes.device):
+    held, at = _held(c), c.codes.get_device()
+    if _elsewhere(at):
+        with torch.cuda.device(at):
             return checkpoint_unpack(c, dtype)
-    out = c.codes.new_empty((c.codes.shape[0], c.cols), dtype=dtype)
-    N.normpre_checkpoint_unpack(_dtype(out), *out.shape, *held, *_row_args(out), _stream(out))
+    rows, cols = c.codes.shape[0], c.cols
+    out = c.codes.new_empty((rows, cols), dtype=dtype)
+    N.normpre_checkpoint_unpack(_dtype(out), rows, cols, *held, out.data_ptr(), cols, _stream(at))
     return out
 
 
@@ -251,20 +255,21 @@ def checkpoint_act(act: str, u: torch.Tensor, up: torch.Tensor | None = None):
     if act not in ("gelu", "swiglu") or (act == "swiglu") != (up is not None):
         raise ValueError("act is 'gelu' with u, or 'swiglu' with u and up")
     u = _matrix(u)
-    _same(u)
+    at = _same(u)
     if up is not None:
         up = _matrix(up)
         _same(u, up)
         if up.shape != u.shape:
             raise ValueError("u and up have one shape")
-    if _elsewhere(u):
-        with torch.cuda.device(u.device):
+    if _elsewhere(at):
+        with torch.cuda.device(at):
             return checkpoint_act(act, u, up)
-    h = u.new_empty(u.shape)
+    rows, cols = u.shape
+    h = u.new_empty((rows, cols))
     cu, ch = _new_checkpoint(u), _new_checkpoint(u)
     cup = None if up is None else _new_checkpoint(u)
-    N.normpre_checkpoint_pack(_ACTS[act], _dtype(u), *u.shape, *_row_args(u), *_row_args(up), *_row_args(h),
-                              *_held_args(cu), *_held_args(cup), *_held_args(ch), _stream(u))
+    N.normpre_checkpoint_pack(_ACTS[act], _dtype(u), rows, cols, *_row_args(u), *_row_args(up), h.data_ptr(), cols,
+                              *_held_args(cu), *_held_args(cup), *_held_args(ch), _stream(at))
     return h, cu, cup, ch
 
 
@@ -273,19 +278,20 @@ def checkpoint_act_grad(act: str, dh: torch.Tensor, cu: Checkpoint, cup: Checkpo
     if act not in ("gelu", "swiglu") or (act == "swiglu") != (cup is not None):
         raise ValueError("act is 'gelu' with u's checkpoint, or 'swiglu' with those of u and up")
     dh = _matrix(dh)
-    _same(dh)
+    at = _same(dh)
+    rows, cols = dh.shape
     for c in (cu, cup):
-        if c is not None and (c.cols != dh.shape[1] or c.codes.device != dh.device):
+        if c is not None and (c.cols != cols or c.codes.get_device() != at):
             raise ValueError("the checkpoint is of another activation")
-    hu = _held(cu, dh.shape[0])
-    hup = (None, None) if cup is None else _held(cup, dh.shape[0])
-    if _elsewhere(dh):
-        with torch.cuda.device(dh.device):
+    hu = _held(cu, rows)
+    hup = (None, None) if cup is None else _held(cup, rows)
+    if _elsewhere(at):
+        with torch.cuda.device(at):
             return checkpoint_act_grad(act, dh, cu, cup)
-    du = dh.new_empty(dh.shape)
-    dup = None if cup is None else dh.new_empty(dh.shape)
-    N.normpre_checkpoint_act_grad(_ACTS[act], _dtype(dh), *dh.shape, *_row_args(dh), *hu, *hup, *_row_args(du),
-                                  *_row_args(dup), _stream(dh))
+    du = dh.new_empty((rows, cols))
+    dup = None if cup is None else dh.new_empty((rows, cols))
+    N.normpre_checkpoint_act_grad(_ACTS[act], _dtype(dh), rows, cols, *_row_args(dh), *hu, *hup, du.data_ptr(), cols,
+                                  None if dup is None else dup.data_ptr(), cols, _stream(at))
     return du, dup
 
 
@@ -300,17 +306,17 @@ def checkpoint_weight_grad(c: Checkpoint, dy: torch.Tensor, layout: str = "oi", 
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
     dy = _matrix(dy)
-    _same(dy)
+    at = _same(dy)
     tokens, outer = dy.shape
     held = _held(c, tokens)
-    if c.codes.device != dy.device:
+    if c.codes.get_device() != at:
         raise ValueError("the checkpoint lies on another device")
     shape = (c.cols, outer) if layout == "io" else (outer, c.cols)
     if out is not None and (out.shape != shape or out.dtype != torch.float32 or out.device != dy.device
                             or (out.stride(1) != 1 and shape[1] > 1) or (out.stride(0) < shape[1] and shape[0] > 1)):
         raise ValueError(f"out is a row-major float32 {shape} matrix on {dy.device}")
-    if _elsewhere(dy):
-        with torch.cuda.device(dy.device):
+    if _elsewhere(at):
+        with torch.cuda.device(at):
             return checkpoint_weight_grad(c, dy, layout, out, accumulate)
     if out is None:
         out = dy.new_empty(shape, dtype=torch.float32)
@@ -318,7 +324,7 @@ def checkpoint_weight_grad(c: Checkpoint, dy: torch.Tensor, layout: str = "oi", 
     need = N.normpre_checkpoint_weight_grad_workspace(dt, tokens, c.cols, outer)
     ws = dy.new_empty(need, dtype=torch.uint8) if need else None
     N.normpre_checkpoint_weight_grad(dt, _LAYOUTS[layout], accumulate, tokens, c.cols, outer, *held, *_row_args(dy),
-                                     *_row_args(out), None if ws is None else ws.data_ptr(), need, _stream(dy))
+                                     *_row_args(out), None if ws is None else ws.data_ptr(), need, _stream(at))
     return out
 
 
