@@ -269,7 +269,11 @@ __device__ __forceinline__ f32x16 scores(const T* lds, int base, const Owned<T, 
 // acc[t] (features 32 t .. of the result, by owned row) += tile^T weights,
 // over streamed rows [base, base + 32); w in the layout of scores().  The
 // weights of bf16 operands are rounded to bf16, as matrix instructions take
-// them: relative error 2^-9 each, below the rounding of the bf16 result.
+// them: relative error 2^-9 each, below the rounding of the bf16 result.  fp32
+// tiles are summed apart and then added, so that a sum over n rows rounds n / 32
+// times at its full size and not n / 2 times: error of dk and dv of seven sequences
+// of 195 .. 1571 (heads of 64, 32 over 8) 1.04e-6 -> 0.49e-6 of their norm, of out
+// 0.35e-6 -> 0.26e-6, for 2% of the forward's time and 1% of the backward's.
 template <class T, int DP>
 __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* lds, int base, const f32x16& w,
                                            int lane) {
@@ -300,13 +304,15 @@ __device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* lds,
     } else {
         const int half = lane >> 5, n = lane & 31;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = base + 8 * (r / 4) + 4 * half + r % 4;
+        for (int t = 0; t < DP / 32; ++t) {
+            f32x16 sum = {};
 #pragma unroll
-            for (int t = 0; t < DP / 32; ++t) {
+            for (int r = 0; r < 16; ++r) {
+                const int row = base + 8 * (r / 4) + 4 * half + r % 4;
                 const float a = lds[TL::idx(row, 8 * t + n / 4) + n % 4];
-                acc[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], acc[t], 0, 0, 0);
+                sum = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], sum, 0, 0, 0);
             }
+            acc[t] += sum;
         }
     }
 }
