@@ -447,7 +447,8 @@ int normpre_stream_ceiling(int mix, int64_t n, const float* a, const float* b, c
  *     arguments give the same bits.
  *   - Outputs must not overlap inputs or each other.
  * Element types: NORMPRE_DTYPE_F32, NORMPRE_DTYPE_BF16.  Products of fp32
- * operands keep fp32 accuracy, sums and softmax statistics are fp32 for both.
+ * operands keep fp32 accuracy (for operands from 2^-100 up: they are summed as
+ * products of three bf16 terms), sums and softmax statistics are fp32 for both.
  */
 #define NORMPRE_DTYPE_F32  0
 #define NORMPRE_DTYPE_BF16 1

@@ -1,5 +1,6 @@
 // Attention over packed sequences with grouped heads, forward and backward,
-// on the matrix instructions of gfx950 (32x32x16 bf16, 32x32x2 fp32).
+// on the bf16 matrix instructions of gfx950 (32x32x16); fp32 operands are split
+// into three bf16 terms.
 //
 // For query i and the keys j of its sequence that it sees (j <= i if causal),
 //   s_ij = c q_i . k_j,  p_ij = exp(s_ij - lse_i),  o_i = sum_j p_ij v_j,
@@ -31,12 +32,16 @@
 //   packed 16418 tokens (lengths 3 to 4096), same heads: forward 245 us (860),
 //     dq 343 us, dk/dv 480-500 us
 //   16 x 1024 tokens, 12 heads of 64, bf16: forward 45 us (570), dq 58, dk/dv 77
-//   4 x 1024 tokens, 12 heads of 64, fp32: forward 74 us (87), backward 250
+//   4 x 1024 tokens, 12 heads of 64, fp32: forward 52-54 us (122), backward 194
 // Of the forward pass's cycles at heads of 128 the matrix instructions take 48%,
 // the vector instructions 57%, LDS reads 49%: two waves per SIMD overlap them in
 // part.  At heads of 64 the vector instructions (an exponential for every pair)
-// bound it: 65%, the matrix instructions 26%.  fp32 is bound by its matrix
-// instructions, which run at a sixteenth of the bf16 rate.
+// bound it: 65%, the matrix instructions 26%.  fp32 takes six
+// products for one, which is still 1.3 to 1.9 times as fast as the fp32 instructions
+// (a sixteenth of the bf16 rate), us with those / with bf16 terms: 4 x 1024 tokens, 12
+// heads of 64, forward 76 / 53, backward 255 / 194; 2948 tokens, 16/8 heads of 128,
+// forward 258 / 216, backward 937 / 728; of 126, forward 526 / 299.  Error of dk and dv
+// over 6000 rows 1.04e-6 / 0.43e-6 of their norm, of out 0.35e-6 / 0.23e-6.
 #include "np_train.h"
 
 #include <type_traits>
@@ -136,6 +141,67 @@ struct Stage {
     }
 };
 
+// fp32 operands as three bf16 terms of eight digits each: the digits are cut off,
+// so the terms add up to the operand exactly (from 2^-100 up: matrix instructions
+// take smaller terms for zero).  A product of two takes the six products of terms
+// that are not below 2^-24 of it; the three left out add less than a rounding does.
+// What is not finite comes out as NaN, and its rows are made again one by one.
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t& t0, uint32_t& t1, uint32_t& t2) {
+    auto upper = [](float a, float b) {              // of both, a's below
+        return __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+    };
+    auto rest = [](float a) { return a - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a) & 0xffff0000u); };
+    t0 = upper(x, y);
+    x = rest(x);
+    y = rest(y);
+    t1 = upper(x, y);
+    t2 = upper(rest(x), rest(y));
+}
+__device__ __forceinline__ void split(const f32x4& a, const f32x4& b, u32x4 (&t)[3]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x4& v = i < 2 ? a : b;
+        uint32_t t0, t1, t2;
+        split_pair(v[2 * (i & 1)], v[2 * (i & 1) + 1], t0, t1, t2);
+        t[0][i] = t0;
+        t[1][i] = t1;
+        t[2][i] = t2;
+    }
+}
+
+// bf16 numbers that stand for an operand, and the elements of a tile's part of
+// one of them.
+template <class T> constexpr int kTerms = std::is_same_v<T, bf16_t> ? 1 : 3;
+template <int DP> constexpr int kPlane = 32 * DP;    // fp32: tiles of 32 rows
+
+// Staging of 32 x DP fp32 numbers, rows at `rows` and past it zero, to three tiles
+// of bf16 terms: loaded while the tile before is worked on.
+template <int DP, bool VEC, int NT>
+struct Split {
+    using TL = Tile<bf16_t, DP>;
+    static constexpr int N = 32 * TL::CH / NT;
+    static_assert(N >= 1 && 32 * TL::CH % NT == 0, "tile does not fill the block");
+    u32x4 r[2 * N];
+    __device__ __forceinline__ void load(const float* base, int64_t tok, int row0, int rows, int dim, int tid) {
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i) {
+            const int e = tid + i / 2 * NT, row = row0 + e / TL::CH;
+            r[i] = load_chunk<float, VEC>(base + (int64_t)row * tok, 2 * (e % TL::CH) + i % 2, dim, row < rows);
+        }
+    }
+    __device__ __forceinline__ void store(bf16_t* lds, int tid) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int e = tid + i * NT;
+            u32x4 t[3];
+            split(__builtin_bit_cast(f32x4, r[2 * i]), __builtin_bit_cast(f32x4, r[2 * i + 1]), t);
+#pragma unroll
+            for (int n = 0; n < 3; ++n)
+                *reinterpret_cast<u32x4*>(lds + n * kPlane<DP> + TL::idx(e / TL::CH, e % TL::CH)) = t[n];
+        }
+    }
+};
+
 // The same tile straight from memory to LDS, without passing through
 // registers.  Rows past the end and chunks past the feature count are copies of
 // the last ones there are: they meet zero weights or zero owned features, and
@@ -206,26 +272,58 @@ struct Pair {
     }
 };
 
+// fp32: through registers, in which a tile waits while the one before it is worked
+// on; one buffer or two.
+template <int DP, bool VEC, int NT, int BUFS>
+struct SplitPair {
+    const float* p0;
+    int64_t tok0;
+    const float* p1;
+    int64_t tok1;
+    int rows, dim;
+    Split<DP, VEC, NT> r0, r1;
+    __device__ __forceinline__ void fetch(int row0, int tid) {
+        r0.load(p0, tok0, row0, rows, dim, tid);
+        r1.load(p1, tok1, row0, rows, dim, tid);
+    }
+    template <class S> __device__ __forceinline__ void first(S&, int row0, int tid) { fetch(row0, tid); }
+    template <class S> __device__ __forceinline__ void next(S& smem, int it, int, int then, int tid) {
+        if constexpr (BUFS == 1) lds_barrier();
+        r0.store(smem[it % BUFS][0], tid);
+        r1.store(smem[it % BUFS][1], tid);
+        lds_barrier();
+        if (then >= 0) fetch(then, tid);
+    }
+};
+template <class T, int DP, int ROWS, bool VEC, int NT, int BUFS>
+using Streamed = std::conditional_t<std::is_same_v<T, bf16_t>, Pair<bf16_t, DP, ROWS, VEC, NT>, SplitPair<DP, VEC, NT, BUFS>>;
+
 // Owned operand of one wave: chunk 2 s + half of row lane % 32, for every s.
 template <class T, int DP>
 struct Owned {
-    static constexpr int S = Tile<T, DP>::CH / 2;
-    u32x4 c[S];
+    static constexpr int S = Tile<bf16_t, DP>::CH / 2;
+    u32x4 c[S][kTerms<T>];
     template <bool VEC>
     __device__ __forceinline__ void load(const T* row, int dim, bool live, int half) {
 #pragma unroll
-        for (int s = 0; s < S; ++s) c[s] = load_chunk<T, VEC>(row, 2 * s + half, dim, live);
+        for (int s = 0; s < S; ++s) {
+            if constexpr (kTerms<T> == 1) c[s][0] = load_chunk<T, VEC>(row, 2 * s + half, dim, live);
+            else split(__builtin_bit_cast(f32x4, load_chunk<T, VEC>(row, 4 * s + 2 * half, dim, live)),
+                       __builtin_bit_cast(f32x4, load_chunk<T, VEC>(row, 4 * s + 2 * half + 1, dim, live)), c[s]);
+        }
     }
     // From a tile in LDS, rows [base, base + 32).
     __device__ __forceinline__ void load(const T* lds, int base, int lane) {
         using TL = Tile<T, DP>;
 #pragma unroll
         for (int s = 0; s < S; ++s)
-            c[s] = *reinterpret_cast<const u32x4*>(lds + TL::idx(base + (lane & 31), 2 * s + (lane >> 5)));
+            c[s][0] = *reinterpret_cast<const u32x4*>(lds + TL::idx(base + (lane & 31), 2 * s + (lane >> 5)));
     }
     __device__ __forceinline__ void negate() {
 #pragma unroll
-        for (int s = 0; s < S; ++s) c[s] ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+            for (int t = 0; t < kTerms<T>; ++t) c[s][t] ^= 0x80008000u;
     }
 };
 
@@ -234,83 +332,108 @@ struct Owned {
 // streamed row base + 8 (r / 4) + 4 (l / 32) + r % 4.  The blocks take turns, so
 // that no product waits for the one before it.
 template <class T, int DP, int N>
-__device__ __forceinline__ void scores(f32x16 (&acc)[N], const T* const (&lds)[N], const int (&base)[N],
+__device__ __forceinline__ void scores(f32x16 (&acc)[N], const bf16_t* const (&lds)[N], const int (&base)[N],
                                        const Owned<T, DP>* const (&own)[N], int lane) {
-    using TL = Tile<T, DP>;
+    using TL = Tile<bf16_t, DP>;
     const int half = lane >> 5;
 #pragma unroll
     for (int n = 0; n < N; ++n) acc[n] = f32x16{};
 #pragma unroll
-    for (int s = 0; s < Owned<T, DP>::S; ++s)
+    for (int s = 0; s < Owned<T, DP>::S; ++s) {
+        auto read = [&](int n, int t) {
+            return *reinterpret_cast<const bf16x8*>(lds[n] + t * kPlane<DP> + TL::idx(base[n] + (lane & 31), 2 * s + half));
+        };
+        auto owned = [&](int n, int t) { return __builtin_bit_cast(bf16x8, own[n]->c[s][t]); };
+        if constexpr (kTerms<T> == 1) {
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const u32x4 a = *reinterpret_cast<const u32x4*>(lds[n] + TL::idx(base[n] + (lane & 31), 2 * s + half));
-            if constexpr (std::is_same_v<T, bf16_t>) {
-                acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
-                                                                 __builtin_bit_cast(bf16x8, own[n]->c[s]), acc[n], 0, 0, 0);
-            } else {
-                const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, own[n]->c[s]);
+            for (int n = 0; n < N; ++n)
+                acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(read(n, 0), owned(n, 0), acc[n], 0, 0, 0);
+        } else {
+            bf16x8 x[N][3];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[n] = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], acc[n], 0, 0, 0);
-            }
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int t = 0; t < 3; ++t) x[n][t] = read(n, t);
+            // The smallest products first.
+#pragma unroll
+            for (int t = 2; t >= 0; --t)
+#pragma unroll
+                for (int i = 0; i <= t; ++i)
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        acc[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[n][i], owned(n, t - i), acc[n], 0, 0, 0);
         }
+    }
 }
 
 template <class T, int DP>
-__device__ __forceinline__ f32x16 scores(const T* lds, int base, const Owned<T, DP>& own, int lane) {
+__device__ __forceinline__ f32x16 scores(const bf16_t* lds, int base, const Owned<T, DP>& own, int lane) {
     f32x16 acc[1];
-    const T* const l[1] = {lds};
+    const bf16_t* const l[1] = {lds};
     const int b[1] = {base};
     const Owned<T, DP>* const o[1] = {&own};
     scores<T, DP, 1>(acc, l, b, o, lane);
     return acc[0];
 }
 
+// Streamed rows r0 .. r0 + 3 and r0 + 8 .. r0 + 11 of the group's lanes (r0 is
+// that of lane p / 4) at the lane's column of features 32 t ..: within each 16-lane
+// group the transposing read returns to lane j the j-th column of the 4 x 16
+// block the group addresses (lane p supplies row p / 4, elements 4 (p % 4) ..).
+template <int DP>
+__device__ __forceinline__ bf16x8 columns(const bf16_t* lds, int r0, int t, int g, int p) {
+    using TL = Tile<bf16_t, DP>;
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+    const int r1 = r0 + 8, c = 4 * t + 2 * (g & 1) + ((p & 3) >> 1), in = 4 * (p & 1);
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + TL::idx(r0, c) + in));
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + TL::idx(r1, c) + in));
+    const s16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, a);
+}
+
 // acc[t] (features 32 t .. of the result, by owned row) += tile^T weights,
 // over streamed rows [base, base + 32); w in the layout of scores().  The
 // weights of bf16 operands are rounded to bf16, as matrix instructions take
 // them: relative error 2^-9 each, below the rounding of the bf16 result.  fp32
-// tiles are summed apart and then added, so that a sum over n rows rounds n / 32
-// times at its full size and not n / 2 times: error of dk and dv of seven sequences
-// of 195 .. 1571 (heads of 64, 32 over 8) 1.04e-6 -> 0.49e-6 of their norm, of out
-// 0.35e-6 -> 0.26e-6, for 2% of the forward's time and 1% of the backward's.
+// tiles are summed apart and then added, so that a long sum rounds once a tile at
+// its full size: half the error of dk and dv over 6000 rows for 1% of the time.
 template <class T, int DP>
-__device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const T* lds, int base, const f32x16& w,
+__device__ __forceinline__ void accumulate(f32x16 (&acc)[DP / 32], const bf16_t* lds, int base, const f32x16& w,
                                            int lane) {
-    using TL = Tile<T, DP>;
+    const int g = lane >> 4, p = lane & 15;          // group of 16 lanes, lane of it
     if constexpr (std::is_same_v<T, bf16_t>) {
-        typedef short s16x4 __attribute__((ext_vector_type(4)));
-        typedef short s16x8 __attribute__((ext_vector_type(8)));
-        typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        // Within each 16-lane group the transposing read returns to lane j
-        // the j-th column of the 4 x 16 block the group addresses (lane p
-        // supplies row p / 4, elements 4 (p % 4) ..).
-        const int g = lane >> 4, p = lane & 15;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             bf16x8 b;
 #pragma unroll
             for (int i = 0; i < 8; ++i) b[i] = (bf16_t)w[8 * s + i];
-            const int r0 = base + 16 * s + 4 * (g >> 1) + (p >> 2), r1 = r0 + 8;
+            const int r0 = base + 16 * s + 4 * (g >> 1) + (p >> 2);
 #pragma unroll
-            for (int t = 0; t < DP / 32; ++t) {
-                const int c = 4 * t + 2 * (g & 1) + ((p & 3) >> 1), in = 4 * (p & 1);
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + TL::idx(r0, c) + in));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(lds + TL::idx(r1, c) + in));
-                const s16x8 a = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), b, acc[t], 0, 0, 0);
-            }
+            for (int t = 0; t < DP / 32; ++t)
+                acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(columns<DP>(lds, r0, t, g, p), b, acc[t], 0, 0, 0);
         }
     } else {
-        const int half = lane >> 5, n = lane & 31;
+        u32x4 b[2][3];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            split(f32x4{w[8 * s], w[8 * s + 1], w[8 * s + 2], w[8 * s + 3]},
+                  f32x4{w[8 * s + 4], w[8 * s + 5], w[8 * s + 6], w[8 * s + 7]}, b[s]);
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t) {
             f32x16 sum = {};
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = base + 8 * (r / 4) + 4 * half + r % 4;
-                const float a = lds[TL::idx(row, 8 * t + n / 4) + n % 4];
-                sum = __builtin_amdgcn_mfma_f32_32x32x2f32(a, w[r], sum, 0, 0, 0);
+            for (int s = 0; s < 2; ++s) {
+                const int r0 = base + 16 * s + 4 * (g >> 1) + (p >> 2);
+                bf16x8 x[3];
+#pragma unroll
+                for (int i = 0; i < 3; ++i) x[i] = columns<DP>(lds + i * kPlane<DP>, r0, t, g, p);
+#pragma unroll
+                for (int n = 2; n >= 0; --n)
+#pragma unroll
+                    for (int i = 0; i <= n; ++i)
+                        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], __builtin_bit_cast(bf16x8, b[s][n - i]), sum, 0, 0, 0);
             }
             acc[t] += sum;
         }
@@ -362,8 +485,8 @@ __device__ __forceinline__ void store_rows(void* lds, T* out, int64_t stride, co
 
 // A wave's accumulators through its share of the LDS tiles to the wave of the
 // other team that owns the same rows, which adds them: acc f0 + other f1.
-template <class T, int DP>
-__device__ __forceinline__ void hand_over(T* lds, const f32x16 (&acc)[DP / 32], int lane) {
+template <int DP>
+__device__ __forceinline__ void hand_over(bf16_t* lds, const f32x16 (&acc)[DP / 32], int lane) {
     f32x4* p = reinterpret_cast<f32x4*>(lds) + lane;
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
@@ -371,8 +494,8 @@ __device__ __forceinline__ void hand_over(T* lds, const f32x16 (&acc)[DP / 32], 
         for (int j = 0; j < 4; ++j)
             p[(4 * t + j) * 64] = f32x4{acc[t][4 * j], acc[t][4 * j + 1], acc[t][4 * j + 2], acc[t][4 * j + 3]};
 }
-template <class T, int DP>
-__device__ __forceinline__ void take_over(const T* lds, f32x16 (&acc)[DP / 32], float f0, float f1, int lane) {
+template <int DP>
+__device__ __forceinline__ void take_over(const bf16_t* lds, f32x16 (&acc)[DP / 32], float f0, float f1, int lane) {
     const f32x4* p = reinterpret_cast<const f32x4*>(lds) + lane;
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
@@ -452,6 +575,18 @@ __device__ void forward_row(const AttnArgs& a, const Where& w, int qi, int lane)
     if (lane == 0) a.lse[w.head * a.tokens + w.start + qi] = m * kLn2 + logf(l);
 }
 
+// sum_j p dp of one row.
+template <class T>
+__device__ float delta_row(const AttnArgs& a, const Where& w, int qi, int lane) {
+    const T *q = row_of<T>(a.q, w, qi, w.head), *dout = row_of<T>(a.dout, w, qi, w.head);
+    const int end = a.causal ? qi + 1 : w.len;
+    const float c2 = a.scale * kLog2e, lse2 = a.lse[w.head * a.tokens + w.start + qi] * kLog2e;
+    float sum = 0.f;
+    for (int j = lane; j < end; j += 64)
+        sum += exp2_fast(dot(q, row_of<T>(a.k, w, j, w.kv), a.dim) * c2 - lse2) * dot(dout, row_of<T>(a.v, w, j, w.kv), a.dim);
+    return wave_sum(sum);
+}
+
 template <class T>
 __device__ void dq_row(const AttnArgs& a, const Where& w, int qi, float delta, int lane) {
     const T *q = row_of<T>(a.q, w, qi, w.head), *dout = row_of<T>(a.dout, w, qi, w.head);
@@ -521,23 +656,32 @@ __device__ __forceinline__ uint32_t bad_rows(bool bad) {
 }
 
 // ---------------------------------------------------------------- passes ---
-// Rows of a streamed tile.
+// Rows of a streamed tile (fp32: three terms of it).
 template <class T> constexpr int kStream = std::is_same_v<T, bf16_t> ? 64 : 32;
 // Rows of each team's tiles in the query passes: half where the tiles of all
 // teams would not fit in LDS.
 template <class T, int DP, int TEAMS>
-constexpr int kStreamed = TEAMS * kStream<T> * DP * 4 * (int)sizeof(T) <= 140 * 1024 ? kStream<T> : kStream<T> / 2;
+constexpr int kStreamed = TEAMS * kStream<T> * DP * 4 * 2 <= 140 * 1024 || kTerms<T> == 3 ? kStream<T> : kStream<T> / 2;
+// Buffers for tiles (one where two would leave a CU one block), and the bf16 numbers
+// of one tile in the query passes' LDS; the rows of the result pass through the same
+// LDS in the end.
+template <class T, int DP, int TEAMS> constexpr int kBufs = kTerms<T> == 1 || (TEAMS == 1 && DP == 64) ? 2 : 1;
+template <class T, int DP, int WR, int TEAMS>
+constexpr int tile_elements() {
+    const int tile = kStreamed<T, DP, TEAMS> * DP * kTerms<T>, rows = 32 * DP * WR / kBufs<T, DP, TEAMS>;
+    return kTerms<T> == 1 || tile > rows ? tile : rows;
+}
 
 // Waves per SIMD a kernel is compiled for: two (256 registers), so that one
 // wave's matrix instructions run beside the other's exponentials, unless the
 // owned operands and accumulators (`ops` and `accs` per owned row and feature)
 // leave no room for them.
 template <class T, int DP>
-constexpr int waves(int ops, int accs) { return DP * (ops * (int)sizeof(T) / 4.f + accs) / 2 <= 160 ? 2 : 1; }
+constexpr int waves(int ops, int accs) { return DP * (ops * kTerms<T> / 2.f + accs) / 2 <= 160 ? 2 : 1; }
 // The same for the query passes, where LDS may hold only one block of four waves.
 template <class T, int DP, int WR, int TEAMS>
 constexpr int query_waves(int ops) {
-    return WR * TEAMS == 4 && TEAMS * kStream<T> * DP * 4 * (int)sizeof(T) > 80 * 1024 ? 1 : waves<T, DP>(ops, 1);
+    return WR * TEAMS == 4 && TEAMS * kBufs<T, DP, TEAMS> * 4 * tile_elements<T, DP, WR, TEAMS>() > 80 * 1024 ? 1 : waves<T, DP>(ops, 1);
 }
 
 // Block order: key heads fastest, so the blocks of one key head (consecutive
@@ -555,7 +699,8 @@ __device__ __forceinline__ bool locate(const AttnArgs& a, const AttnTile& t, int
 template <class T, int DP, bool VEC, int WR, int TEAMS>
 __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS>(1))) attn_fwd_kernel(AttnArgs a) {
     constexpr int NT = 64 * WR, BN = kStreamed<T, DP, TEAMS>, NB = BN / 32, DT = DP / 32;
-    __shared__ __attribute__((aligned(16))) T tiles[TEAMS][2][2][BN * DP];
+    constexpr int BUFS = kBufs<T, DP, TEAMS>, TE = tile_elements<T, DP, WR, TEAMS>(), SHARE = BUFS * 2 * TE / WR;
+    __shared__ __attribute__((aligned(16))) bf16_t tiles[TEAMS][BUFS][2][TE];
     __shared__ float stat[TEAMS][2][32 * WR];
     const int tid = threadIdx.x % NT, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int team = TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
@@ -581,12 +726,12 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
     // tiles leave o alone (weights then stay below 2^8, which costs no digit).
     f32x16 o[DT] = {};
     float m = -INFINITY, l = 0.f;
-    const Pair<T, DP, BN, VEC, NT> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
+    Streamed<T, DP, BN, VEC, NT, BUFS> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
     keys.first(smem, team * BN, tid);
     for (int it = 0; it < (steps + TEAMS - 1) / TEAMS; ++it) {
         const int k0 = (it * TEAMS + team) * BN;
         keys.next(smem, it, k0, it * TEAMS + team + TEAMS < steps ? k0 + TEAMS * BN : -1, tid);
-        const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
+        const bf16_t *ks = smem[it % BUFS][0], *vs = smem[it % BUFS][1];
         if (k0 < end && (!a.causal || k0 <= qw + 31)) {    // same for the whole wave
             f32x16 s[NB];
             float mx = m;
@@ -635,9 +780,9 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
     }
     l += __shfl_xor(l, 32, 64);
     lds_barrier();                                   // the tiles are free
-    T* mine = &smem[0][0][0] + wave * (BN * DP * 4 / WR);
+    bf16_t* mine = &smem[0][0][0] + wave * SHARE;
     if constexpr (TEAMS > 1) {
-        if (team > 0) hand_over<T, DP>(mine, o, lane);
+        if (team > 0) hand_over<DP>(mine, o, lane);
         if (half == 0) {
             stat[team][0][wave * 32 + lane] = m;
             stat[team][1][wave * 32 + lane] = l;
@@ -653,7 +798,7 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
 #pragma unroll
         for (int t = 1; t < TEAMS; ++t) {
             const float mt = stat[t][0][row], ft = mt == -INFINITY ? 0.f : exp2_fast((mt - mx) * c2);
-            take_over<T, DP>(&tiles[t][0][0][0] + wave * (BN * DP * 4 / WR), o, f, ft, lane);
+            take_over<DP>(&tiles[t][0][0][0] + wave * SHARE, o, f, ft, lane);
             l += stat[t][1][row] * ft;
             f = 1.f;
         }
@@ -672,7 +817,8 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
 template <class T, int DP, bool VEC, int WR, int TEAMS>
 __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS>(2))) attn_dq_kernel(AttnArgs a) {
     constexpr int NT = 64 * WR, BN = kStreamed<T, DP, TEAMS>, NB = BN / 32, DT = DP / 32;
-    __shared__ __attribute__((aligned(16))) T tiles[TEAMS][2][2][BN * DP];
+    constexpr int BUFS = kBufs<T, DP, TEAMS>, TE = tile_elements<T, DP, WR, TEAMS>(), SHARE = BUFS * 2 * TE / WR;
+    __shared__ __attribute__((aligned(16))) bf16_t tiles[TEAMS][BUFS][2][TE];
     __shared__ float stat[TEAMS][32 * WR];
     const int tid = threadIdx.x % NT, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int team = TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / NT) : 0;
@@ -692,13 +838,16 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
     // delta of the lane's row: its half of the chunks, then the other half's.
     float delta = 0.f;
     {
-        const T* orow = row_of<T>(a.out, w, live ? qi : 0, head);
+        const T *orow = row_of<T>(a.out, w, live ? qi : 0, head), *drow = row_of<T>(a.dout, w, live ? qi : 0, head);
 #pragma unroll
-        for (int s = 0; s < Owned<T, DP>::S; ++s) {
+        for (int s = 0; s < Tile<T, DP>::CH / 2; ++s) {
             const u32x4 oc = load_chunk<T, VEC>(orow, 2 * s + half, a.dim, live);
+            u32x4 dc;
+            if constexpr (kTerms<T> == 1) dc = dout.c[s][0];
+            else dc = load_chunk<T, VEC>(drow, 2 * s + half, a.dim, live);
             T x[16 / sizeof(T)], y[16 / sizeof(T)];
             __builtin_memcpy(x, &oc, 16);
-            __builtin_memcpy(y, &dout.c[s], 16);
+            __builtin_memcpy(y, &dc, 16);
 #pragma unroll
             for (int i = 0; i < (int)(16 / sizeof(T)); ++i) delta = __builtin_fmaf((float)x[i], (float)y[i], delta);
         }
@@ -710,11 +859,11 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
     const int end = a.causal ? min(w.len, q0 + 32 * WR) : w.len, steps = (end + BN - 1) / BN;
     const float c2 = a.scale * kLog2e;
 
-    const Pair<T, DP, BN, VEC, NT> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
+    Streamed<T, DP, BN, VEC, NT, BUFS> keys{kb, a.k.tok, vb, a.v.tok, w.len, a.dim};
     // p (dp - de) of streamed rows k0 + 32 b .., zero where the row does not see them.
-    auto weights = [&](const T* ks, const T* vs, int k0, int b, float de) {
+    auto weights = [&](const bf16_t* ks, const bf16_t* vs, int k0, int b, float de) {
         f32x16 s[2];
-        const T* const lds[2] = {ks, vs};
+        const bf16_t* const lds[2] = {ks, vs};
         const int base[2] = {32 * b, 32 * b};
         const Owned<T, DP>* const own[2] = {&q, &dout};
         scores<T, DP, 2>(s, lds, base, own, lane);
@@ -744,7 +893,7 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
 #pragma unroll
             for (int b = 0; b < NB; ++b)
                 if (seen(k0, b)) {
-                    const f32x16 s = weights(smem[it & 1][0], smem[it & 1][1], k0, b, 0.f);
+                    const f32x16 s = weights(smem[it % BUFS][0], smem[it % BUFS][1], k0, b, 0.f);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) sum += s[r];
                 }
@@ -763,24 +912,31 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
     for (int it = 0; it < rounds; ++it) {
         const int k0 = (it * TEAMS + team) * BN;
         keys.next(smem, it, k0, it * TEAMS + team + TEAMS < steps ? k0 + TEAMS * BN : -1, tid);
-        const T *ks = smem[it & 1][0], *vs = smem[it & 1][1];
+        const bf16_t *ks = smem[it % BUFS][0], *vs = smem[it % BUFS][1];
 #pragma unroll
         for (int b = 0; b < NB; ++b)
             if (seen(k0, b)) accumulate<T, DP>(g, ks, 32 * b, weights(ks, vs, k0, b, delta), lane);
     }
     lds_barrier();                                   // the tiles are free
-    T* mine = &smem[0][0][0] + wave * (BN * DP * 4 / WR);
+    bf16_t* mine = &smem[0][0][0] + wave * SHARE;
     if constexpr (TEAMS > 1) {
-        if (team > 0) hand_over<T, DP>(mine, g, lane);
+        if (team > 0) hand_over<DP>(mine, g, lane);
         lds_barrier();
         if (team > 0) return;
 #pragma unroll
         for (int t = 1; t < TEAMS; ++t)
-            take_over<T, DP>(&tiles[t][0][0][0] + wave * (BN * DP * 4 / WR), g, 1.f, 1.f, lane);
+            take_over<DP>(&tiles[t][0][0][0] + wave * SHARE, g, 1.f, 1.f, lane);
     }
+    uint32_t bad = bad_rows(live && any_nonfinite(g));
+    // fp32: the scores of a key that is not finite are NaN, where p may well be 0.
+    if (kTerms<T> == 3 && end <= kAttnRows)
+        for (uint32_t left = bad; left; left &= left - 1) {
+            const int r = __builtin_ctz(left);
+            const float d = delta_row<T>(a, w, qw + r, lane);
+            if ((lane & 31) == r) delta = d;
+        }
     if (live && half == 0) a.lse2[at] = lse2;
     if (live && half == 0) a.delta[at] = delta;
-    uint32_t bad = bad_rows(live && any_nonfinite(g));
     store_rows<T, DP, VEC>(mine, row_of<T>(a.dq, w, qw, head), a.dq.tok, g,
                            a.scale, a.dim, live_rows(qw, w.len) & ~bad, lane);
     for (; bad; bad &= bad - 1) {
@@ -793,13 +949,15 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
 // that shares it, so the sum over heads stays in registers; four products a tile,
 // Q and dO read both ways.  blockIdx.y: share of the queries.  Owned k and v and
 // two sets of accumulators take 192 registers at heads of 128 in bf16: one wave
-// per SIMD, or, HELD, two with v's rows in LDS instead.
+// per SIMD, or, HELD, two with v's rows in LDS instead.  fp32 takes 160 at heads of
+// 64, and two waves per SIMD would spill 60 more: backward of 4 x 1024 tokens, 12
+// heads, 205 us with two, 193 with one.
 template <class T, int DP, bool VEC, bool HELD>
-__global__ void __launch_bounds__(kThreads, (HELD ? 2 : waves<T, DP>(2, 2))) attn_dkv_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, (HELD ? 2 : kTerms<T> == 3 ? 1 : waves<T, DP>(2, 2))) attn_dkv_kernel(AttnArgs a) {
     constexpr int BM = HELD ? 32 : kStream<T>, NB = BM / 32, DT = DP / 32;
-    __shared__ __attribute__((aligned(16))) char shared[4 * BM * DP * sizeof(T) + (HELD ? kAttnRows * DP * sizeof(T) : 0)];
-    auto& smem = *reinterpret_cast<T (*)[2][2][BM * DP]>(shared);
-    T* vrows = reinterpret_cast<T*>(shared) + 4 * BM * DP;   // of the block, if held
+    __shared__ __attribute__((aligned(16))) char shared[8 * kTerms<T> * BM * DP + (HELD ? 2 * kAttnRows * DP : 0)];
+    auto& smem = *reinterpret_cast<bf16_t (*)[2][2][kTerms<T> * BM * DP]>(shared);
+    bf16_t* vrows = reinterpret_cast<bf16_t*>(shared) + 4 * BM * DP;   // of the block, if held
     __shared__ __attribute__((aligned(16))) float stat[2][2][BM];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
     const int group = a.heads / a.kv_heads;
@@ -816,9 +974,9 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : waves<T, DP>(2, 2))) att
     Owned<T, HELD ? 32 : DP> v;                      // not used if held in LDS
     k.template load<VEC>(row_of<T>(a.k, w, live ? ki : 0, kv), a.dim, live, half);
     if constexpr (HELD) {                            // with zeros for what is not there, as in registers
-        using ST = Stage<T, DP, kAttnRows, true, kThreads>;
+        using ST = Stage<bf16_t, DP, kAttnRows, true, kThreads>;
         u32x4 r[ST::N];
-        ST::load(r, row_of<T>(a.v, w, 0, kv), a.v.tok, kt, w.len, a.dim, tid);
+        ST::load(r, row_of<bf16_t>(a.v, w, 0, kv), a.v.tok, kt, w.len, a.dim, tid);
         ST::store(r, vrows, tid);
     } else v.template load<VEC>(row_of<T>(a.v, w, live ? ki : 0, kv), a.dim, live, half);
     const int first = a.causal ? kt / BM : 0, per = (w.len + BM - 1) / BM - first;
@@ -829,14 +987,20 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : waves<T, DP>(2, 2))) att
     const float c2 = a.scale * kLog2e;
 
     f32x16 gk[DT] = {}, gv[DT] = {};
-    // A step's queries, their log-sum-exps and deltas.
+    // A step's queries, their log-sum-exps and deltas; fp32: the tile on its way.
+    std::conditional_t<kTerms<T> == 1, int, Split<DP, VEC, kThreads>> rq, rd;
     auto fetch = [&](int i, int buf) {
         const int h = w.head + i / per, row0 = (first + i % per) * BM;
-        const Pair<T, DP, BM, VEC, kThreads> rows{row_of<T>(a.q, w, 0, h), a.q.tok, row_of<T>(a.dout, w, 0, h), a.dout.tok,
-                                        w.len, a.dim};
         int td = tid;
         if constexpr (HELD) asm volatile("" : "+v"(td));     // as below
-        rows.fill(smem[buf], row0, td);
+        if constexpr (kTerms<T> == 1) {
+            const Pair<T, DP, BM, VEC, kThreads> rows{row_of<T>(a.q, w, 0, h), a.q.tok, row_of<T>(a.dout, w, 0, h),
+                                                      a.dout.tok, w.len, a.dim};
+            rows.fill(smem[buf], row0, td);
+        } else {
+            rq.load(row_of<T>(a.q, w, 0, h), a.q.tok, row0, w.len, a.dim, td);
+            rd.load(row_of<T>(a.dout, w, 0, h), a.dout.tok, row0, w.len, a.dim, td);
+        }
         if (tid < 2 * BM) {                          // whole waves
             const float* src = (tid < BM ? a.lse2 : a.delta) + h * a.tokens + w.start + min(row0 + tid % BM, w.len - 1);
             __builtin_amdgcn_global_load_lds(
@@ -849,9 +1013,13 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : waves<T, DP>(2, 2))) att
     for (int it = beg; it < steps; ++it) {
         const int q0 = (first + it % per) * BM;
         wait_loads();
+        if constexpr (kTerms<T> == 3) {
+            rq.store(smem[it & 1][0], tid);
+            rd.store(smem[it & 1][1], tid);
+        }
         lds_barrier();
         if (it + 1 < steps) fetch(it + 1, (it + 1) & 1);
-        const T *qs = smem[it & 1][0], *ds = smem[it & 1][1];
+        const bf16_t *qs = smem[it & 1][0], *ds = smem[it & 1][1];
         // The lane as of this step: addresses in LDS are then made anew in each, and
         // take no registers from one to the next.
         int ln = lane;
@@ -866,7 +1034,7 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : waves<T, DP>(2, 2))) att
             if constexpr (HELD) {
                 p = scores<T, DP>(qs, 32 * b, k, ln);
             } else {
-                const T* const lds[2] = {qs, ds};
+                const bf16_t* const lds[2] = {qs, ds};
                 const int base[2] = {32 * b, 32 * b};
                 const Owned<T, DP>* const own[2] = {&k, &v};
                 scores<T, DP, 2>(pd, lds, base, own, ln);
@@ -994,8 +1162,8 @@ hipError_t run(const AttnArgs& a, bool backward, hipStream_t s) {
     //   bf16, heads of 64, blocks of 128 rows 96: 19.5 15.6 12.6, 192: 19.9 16.3 15.1,
     //     288: 20.6 16.5 16.9, 384: 20.9 17.7 18.3, 576: 22.6 26.6 26.2, 960: 31.6 40.5 40.2
     //   bf16, 128: 256: 47.0 39.0 42.1, 512: 55.4 49.3 84.5, 768: 68.0 78.8 130
-    //   fp32, 64: 384: 103 98 74, 768: 146 137 134, 1536: 240 249 258
-    //   fp32, 128: 256: 143 143 98, 512: 201 169 197, 1024: 317 337 394
+    //   fp32, 64, (4, 1) and (2, 2): 96: 62 44, 384: 66 54, 768: 86 99, 1536: 159 187
+    //   fp32, 128: 128: 127 73, 256: 263 158, 512: 275 297, 1024: 402 593
     const int64_t blocks = (int64_t)a.num_tiles * a.heads;
     constexpr bool small = sizeof(T) == 2;
     if (!VEC || blocks > (small ? 512 : 448)) query_pass<T, DP, VEC, 4, 1>(a, backward, s);
