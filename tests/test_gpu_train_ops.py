@@ -123,6 +123,15 @@ def test_attention_extreme_scores(dev):
     _check(8 * q, 8 * k, v, dout, [140], True)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("fq,fk,fv,fdout", [(2.0 ** 50, 2.0 ** -50, 2.0 ** -60, 2.0 ** 30),
+                                            (2.0 ** -45, 2.0 ** 45, 2.0 ** 60, 2.0 ** -70)])
+def test_attention_fp32_magnitudes(dev, d, fq, fk, fv, fdout):
+    # All 24 digits of an operand count, whatever its size.
+    q, k, v, dout = _qkv(dev, 23, 190, 2, 1, d, F32)
+    _check(fq * q, fk * k, fv * v, fdout * dout, [150, 40], True)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_long_rows(dev, dtype):
     # A sequence of many tiles.
