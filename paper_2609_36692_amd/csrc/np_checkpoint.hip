@@ -291,17 +291,16 @@ __global__ void __launch_bounds__(64 * WI * WO, 2) wgrad_kernel(WgradArgs a, int
         }
         py[n] += BK * a.ld_dy;
     };
-    // Codes as bytes of code + 128: value = byte * step - 128 step, exactly.
+    // value = code * step, exactly for every step from 2^-126 to 2^121; the builtin
+    // makes the byte's sign a part of its conversion (one instruction).
     auto store_x = [&](int n, int buf, int64_t t, auto last) {
         const int e = tid + n * NTH, c = e % (BI / 16), k = e / (BI / 16);
         float step = step_of(re[n]);
-        u32x4 u = rx[n] ^ 0x80808080u;
         if (decltype(last)::value && t + k >= t1) step = 0.f;
-        const float off = -128.f * step;
         bf16x8 v[2];
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-            v[i / 8][i % 8] = (bf16_t)__builtin_fmaf((float)(u[i / 4] >> (8 * (i % 4)) & 0xffu), step, off);
+            v[i / 8][i % 8] = (bf16_t)((float)(int)__builtin_amdgcn_sbfe(rx[n][i / 4], 8 * (i % 4), 8) * step);
         *reinterpret_cast<bf16x8*>(xs[buf] + widx<BI>(k, 2 * c)) = v[0];
         *reinterpret_cast<bf16x8*>(xs[buf] + widx<BI>(k, 2 * c + 1)) = v[1];
     };

@@ -498,6 +498,25 @@ def test_weight_grad_fp32_terms(dev):
         assert ((got[i] - want).abs() <= 3 * U * want.abs()).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["io", "oi"])
+def test_weight_grad_of_the_largest_values(dev, dtype, layout):
+    # Magnitudes past 2^127 give a group the largest exponent, 121; dy makes the
+    # products ordinary numbers.
+    g = _gen(dev, 68)
+    x = _activations(dev, 69, 40, 200, dtype)
+    x[3:20, 64:128] = (3.3e38 * (2 * torch.rand(17, 64, generator=g, device=dev) - 1)).to(dtype)
+    x[3:20, 70] = 3.3e38
+    c = T.checkpoint_pack(x)
+    assert (c.exps[3:20, 1] == 121).all()
+    dy = (1e-25 * torch.randn(40, 90, generator=g, device=dev)).to(dtype)
+    held, d = decode_reference(c.codes, c.exps, 200), dy.double().cpu().numpy()
+    want, tol = held.T @ d, _weight_bound(held, d, 40)
+    if layout == "oi":
+        want, tol = want.T, tol.T
+    assert_within("dw", T.checkpoint_weight_grad(c, dy, layout), want, tol)
+
+
 # ------------------------------------------------------------------ layers ---
 @pytest.mark.parametrize("layout", ["io", "oi"])
 @pytest.mark.parametrize("dtype", [BF16, F32])
