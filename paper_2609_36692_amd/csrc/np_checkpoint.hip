@@ -10,6 +10,7 @@
 // An 8-bit floating type with 3 bits of mantissa is off by up to 6% of every
 // value, these codes by up to 0.8% of the group's largest.
 // A group with a NaN or an infinity has codes 0, e = -128, and stands for NaN.
+#include "np_dy_rows.h"
 #include "np_train.h"
 
 #include <cmath>
@@ -227,9 +228,9 @@ __device__ __forceinline__ bf16x8 wfrag(const bf16_t* lds, int mb, int s, int la
 
 // Tile of BI inner by BO outer features, WI x WO waves, each with the accumulators
 // of BI / WI by BO / WO of them.
-template <class T, bool OI, bool EVEN, int BI, int BO, int WI, int WO>
+template <class T, bool OI, DyRows ROWS, int BI, int BO, int WI, int WO>
 __global__ void __launch_bounds__(64 * WI * WO, 2) wgrad_kernel(WgradArgs a, int64_t pitch, int64_t chunk) {
-    constexpr int NTH = 64 * WI * WO, NT = std::is_same_v<T, bf16_t> ? 1 : 3, BK = 32;
+    constexpr int NTH = 64 * WI * WO, NT = std::is_same_v<T, bf16_t> ? 1 : 3, BK = (int)kDyTile;
     constexpr int NX = BK * BI / 16 / NTH;               // 16 codes each
     constexpr int E = 16 / sizeof(T), NY = BK * BO / E / NTH;
     constexpr int FI = BI / WI / 32, FO = BO / WO / 32;
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(64 * WI * WO, 2) wgrad_kernel(WgradArgs a, int
 #pragma unroll
     for (int n = 0; n < NY; ++n) {
         const int64_t c = o0 + E * ((tid + n * NTH) % (BO / E)), row = t0 + (tid + n * NTH) / (BO / E);
-        py[n] = dy + row * a.ld_dy + min(c, EVEN ? a.outer - E : a.outer - 1);
+        py[n] = dy + row * a.ld_dy + min(c, ROWS == DyRows::Whole ? a.outer - E : a.outer - 1);
     }
     // Item n of the tile of tokens t .., `last` if that is the last one; moves on.
     auto load_x = [&](int n, int64_t t, auto last) {
@@ -278,9 +279,7 @@ __global__ void __launch_bounds__(64 * WI * WO, 2) wgrad_kernel(WgradArgs a, int
     auto load_y = [&](int n, int64_t t, auto last) {
         const int64_t over = decltype(last)::value ? max(t + (tid + n * NTH) / (BO / E) - (t1 - 1), (int64_t)0) : 0;
         const T* p = py[n] - over * a.ld_dy;
-        // EVEN: rows are a whole number of 16-byte pieces.  Otherwise a row's last
-        // piece runs into the row after it, which exists in all but the last tile.
-        if constexpr (EVEN || !decltype(last)::value) {
+        if constexpr (ROWS == DyRows::Whole || (ROWS == DyRows::Ragged && !decltype(last)::value)) {
             ry[n] = *reinterpret_cast<const typename Sixteen<T>::type*>(p);
         } else {
             const int64_t left = a.outer - (o0 + E * ((tid + n * NTH) % (BO / E)));
@@ -486,25 +485,30 @@ hipError_t act_grad(Act act, const CkptGradArgs& a, hipStream_t s) {
 }
 
 template <class T, bool OI, int BI, int BO, int WI, int WO>
-void wgrad_pass(const WgradArgs& a, hipStream_t s) {
+void wgrad_pass(const WgradArgs& a, DyRows rows, hipStream_t s) {
     const int64_t tiles = ((a.inner + BI - 1) / BI) * ((a.outer + BO - 1) / BO);
     const int64_t chunk = ((a.tokens + a.splits - 1) / a.splits + 31) / 32 * 32;
     const dim3 grid((unsigned)tiles, (unsigned)a.splits);
     const int64_t pitch = ckpt_pitch(a.inner);
-    if (a.outer % (16 / (int)sizeof(T)) == 0)
-        wgrad_kernel<T, OI, true, BI, BO, WI, WO><<<grid, 64 * WI * WO, 0, s>>>(a, pitch, chunk);
-    else wgrad_kernel<T, OI, false, BI, BO, WI, WO><<<grid, 64 * WI * WO, 0, s>>>(a, pitch, chunk);
+    if (rows == DyRows::Whole)
+        wgrad_kernel<T, OI, DyRows::Whole, BI, BO, WI, WO><<<grid, 64 * WI * WO, 0, s>>>(a, pitch, chunk);
+    else if (rows == DyRows::Ragged)
+        wgrad_kernel<T, OI, DyRows::Ragged, BI, BO, WI, WO><<<grid, 64 * WI * WO, 0, s>>>(a, pitch, chunk);
+    else if constexpr (BI * BO < 256 * 256)
+        wgrad_kernel<T, OI, DyRows::Narrow, BI, BO, WI, WO><<<grid, 64 * WI * WO, 0, s>>>(a, pitch, chunk);
 }
 
 // bf16: 256 x 256 tiles (64 KB of LDS, 128 accumulators a lane) where there are
-// 128 of them or more, else 128 x 128; fp32, three products a tile: 256 x 128.
+// 128 of them or more, else 128 x 128, as for a few narrow columns of dy; fp32,
+// three products a tile: 256 x 128.
 bool wgrad_large(int64_t inner, int64_t outer) { return ((inner + 255) / 256) * ((outer + 255) / 256) >= 128; }
 
 template <bool OI>
 void wgrad(DType t, const WgradArgs& a, hipStream_t s) {
-    if (t == DType::F32) wgrad_pass<float, OI, 256, 128, 4, 2>(a, s);
-    else if (wgrad_large(a.inner, a.outer)) wgrad_pass<bf16_t, OI, 256, 256, 2, 4>(a, s);
-    else wgrad_pass<bf16_t, OI, 128, 128, 2, 2>(a, s);
+    const DyRows rows = dy_rows(a.outer, a.ld_dy, t == DType::F32 ? 4 : 8);
+    if (t == DType::F32) wgrad_pass<float, OI, 256, 128, 4, 2>(a, rows, s);
+    else if (wgrad_large(a.inner, a.outer) && rows != DyRows::Narrow) wgrad_pass<bf16_t, OI, 256, 256, 2, 4>(a, rows, s);
+    else wgrad_pass<bf16_t, OI, 128, 128, 2, 2>(a, rows, s);
 }
 
 }  // namespace

@@ -517,6 +517,24 @@ def test_weight_grad_of_the_largest_values(dev, dtype, layout):
     assert_within("dw", T.checkpoint_weight_grad(c, dy, layout), want, tol)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("layout", ["io", "oi"])
+@pytest.mark.parametrize("tokens", [33, 97, 129, 1025])
+@pytest.mark.parametrize("outer,ld", [(1, 1), (2, 2), (3, 3), (6, 6), (3, 7), (9, 9)])
+def test_weight_grad_of_narrow_rows(dev, dtype, layout, tokens, outer, ld):
+    # Rows of dy shorter than the pieces that wider ones are read in, up to the very
+    # end of their buffer.
+    c = T.checkpoint_pack(_activations(dev, 70, tokens, 70, dtype))
+    buf = torch.full(((tokens - 1) * ld + outer,), float("nan"), dtype=dtype, device=dev)
+    dy = buf.as_strided((tokens, outer), (ld, 1))
+    dy.copy_(_activations(dev, 71, tokens, outer, dtype))
+    x, d = decode_reference(c.codes, c.exps, 70), dy.double().cpu().numpy()
+    want, tol = x.T @ d, _weight_bound(x, d, tokens)
+    if layout == "oi":
+        want, tol = want.T, tol.T
+    assert_within("dw", T.checkpoint_weight_grad(c, dy, layout), want, tol)
+
+
 # ------------------------------------------------------------------ layers ---
 @pytest.mark.parametrize("layout", ["io", "oi"])
 @pytest.mark.parametrize("dtype", [BF16, F32])
