@@ -207,7 +207,8 @@ struct Split {
 // registers.  Rows past the end and chunks past the feature count are copies of
 // the last ones there are: they meet zero weights or zero owned features, and
 // what is not finite among them is caught with the other rows that are not
-// (any_nonfinite).  One instruction fills 1 KB of LDS per wave, so the swizzle
+// (any_nonfinite): an infinity in a row's last chunk makes NaN of the row's score.
+// Zeros in place of the copied chunks cost 1.3% at full heads.  One instruction fills 1 KB of LDS per wave, so the swizzle
 // is in the order of the chunks that the lanes fetch.
 template <class T, int DP, int ROWS, int NT>
 struct Direct {
@@ -929,8 +930,9 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
             take_over<DP>(&tiles[t][0][0][0] + wave * SHARE, g, 1.f, 1.f, lane);
     }
     uint32_t bad = bad_rows(live && any_nonfinite(g));
-    // fp32: the scores of a key that is not finite are NaN, where p may well be 0.
-    if (kTerms<T> == 3 && end <= kAttnRows)
+    // Where p may well be 0 the score of a key that is not finite came out as NaN:
+    // fp32, and heads that leave a part of the tile to copies (Direct).
+    if ((kTerms<T> == 3 || a.dim < DP) && end <= kAttnRows)
         for (uint32_t left = bad; left; left &= left - 1) {
             const int r = __builtin_ctz(left);
             const float d = delta_row<T>(a, w, qw + r, lane);

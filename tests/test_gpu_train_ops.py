@@ -160,6 +160,22 @@ def test_attention_nonfinite_stays_with_rows_that_see_it(dev, dtype, d, value, w
         assert torch.isfinite(y[others]).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [40, 72, 96])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("where", ["q", "k", "v", "dout"])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_attention_nonfinite_in_the_last_features(dev, dtype, d, value, where, sign):
+    # Heads that fill their tiles in part.  An infinite key makes the scores of all
+    # queries, of one sign there, +inf or -inf: a weight of zero in the second case.
+    lens, hq, hk = [50, 150, 40], 2, 1
+    x = dict(zip(("q", "k", "v", "dout"), _qkv(dev, 43, sum(lens), hq, hk, d, dtype)))
+    x[where][50 + 77, 0, d - 1] = value
+    if where == "k":
+        x["q"][:, :, d - 1] = sign * x["q"][:, :, d - 1].abs().clamp(min=0.01)
+    _check(**x, lens=lens, causal=True)
+
+
 def test_attention_all_scores_minus_infinity(dev):
     # Formula of a row whose scores are all -inf: 0 / 0.
     q = torch.ones(4, 1, 64, device=dev)
