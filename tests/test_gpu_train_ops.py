@@ -458,6 +458,38 @@ def test_weight_grad(dev, dtype, layout, tokens, inner, outer):
     assert (big == 3.0).all()
 
 
+@pytest.mark.parametrize("layout", ["io", "oi"])
+@pytest.mark.parametrize("tokens,inner,outer", [
+    (1, 2049, 3843), (33, 2048, 4096), (100, 4096, 2056), (161, 2049, 3843), (70, 33000, 3), (70, 33000, 250),
+])
+def test_weight_grad_of_large_matrices(dev, layout, tokens, inner, outer):
+    # 128 tiles of 256 x 256 or more, the widths a multiple of the tile, of 8, or
+    # odd.  fp64 on the GPU: the same numbers as the other tests' reference.
+    print(f"weight_grad large {layout} {tokens} {inner} {outer}", flush=True)
+    x = _activations(dev, 39, tokens, inner, BF16)
+    if tokens == 100:
+        x[7, 1030] = float("nan")
+    c = T.checkpoint_pack(x)
+    dy = _activations(dev, 40, tokens, outer, BF16)
+    held, d = torch.from_numpy(decode_reference(c.codes, c.exps, inner)).to(dev), dy.double()
+    want = held.T @ d if layout == "io" else d.T @ held
+    tol = (tokens + 8) * U * (held.abs().T @ d.abs() if layout == "io" else d.abs().T @ held.abs()) + 1e-38
+    got = T.checkpoint_weight_grad(c, dy, layout)
+    assert torch.equal(torch.isfinite(got), torch.isfinite(want))
+    fine = torch.isfinite(want)
+    assert fine.all() or (~fine).sum() == 64 * outer
+    assert ((got.double() - want).abs() <= tol)[fine].all()
+    assert torch.equal(got.nan_to_num(7.0), T.checkpoint_weight_grad(c, dy, layout).nan_to_num(7.0))
+    # Into a part of a larger matrix, added to what is there.
+    big = torch.full((got.shape[0] + 2, got.shape[1] + 5), 3.0, device=dev)
+    part = big[1:-1, 2:-3]
+    T.checkpoint_weight_grad(c, dy, layout, out=part, accumulate=True)
+    assert ((part.double() - want - 3.0).abs() <= tol + 2 * U * (want.abs() + 3.0))[fine].all()
+    assert torch.equal(torch.isfinite(part), fine)
+    big[1:-1, 2:-3] = 3.0
+    assert (big == 3.0).all()
+
+
 @pytest.mark.parametrize("how", ["strided", "odd_stride", "misaligned", "transposed"])
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_weight_grad_strides(dev, dtype, how):
