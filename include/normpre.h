@@ -446,9 +446,11 @@ int normpre_stream_ceiling(int mix, int64_t n, const float* a, const float* b, c
  *   - Results do not depend on the order in which blocks run: the same
  *     arguments give the same bits.
  *   - Outputs must not overlap inputs or each other.
- * Element types: NORMPRE_DTYPE_F32, NORMPRE_DTYPE_BF16.  Products of fp32
- * operands keep fp32 accuracy (for operands from 2^-100 up: they are summed as
- * products of three bf16 terms), sums and softmax statistics are fp32 for both.
+ * Element types: NORMPRE_DTYPE_F32, NORMPRE_DTYPE_BF16.  fp32 operands (and in
+ * attention the softmax weights and score gradients) are multiplied as three bf16
+ * terms each: exactly in the weight gradient, to 8 2^-24 of a product in attention,
+ * for magnitudes from 2^-100 up.  Sums and softmax statistics are fp32 for both
+ * types.
  */
 #define NORMPRE_DTYPE_F32  0
 #define NORMPRE_DTYPE_BF16 1

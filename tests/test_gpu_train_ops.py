@@ -132,6 +132,21 @@ def test_attention_fp32_magnitudes(dev, d, fq, fk, fv, fdout):
     _check(fq * q, fk * k, fv * v, fdout * dout, [150, 40], True)
 
 
+def test_attention_fp32_products(dev):
+    # One token a sequence, one feature: the log-sum-exp is the product q k.  The
+    # split may leave out 8 u of it, the sum of the terms' products may cut off 2 u,
+    # the exponent's rounding is taken back by the logarithm to 1 u, and their sum
+    # rounds.  Among the operands some whose upper 16 bits fall short of them by
+    # the most.
+    n = 4096
+    g = _gen(dev, 24)
+    q, k = (torch.randn(n, 1, 1, generator=g, device=dev) for _ in range(2))
+    q[:8] = k[:8] = torch.tensor(0x3f80ffff, dtype=torch.int32).view(F32).item()
+    _, lse = T.attention_forward(q, k, k, T.AttentionPlan([1] * n, True, dev), 1.0)
+    want = (q.double() * k.double()).flatten()
+    assert ((lse[0].double() - want).abs() <= 12 * U * want.abs()).all()
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_attention_long_rows(dev, dtype):
     # A sequence of many tiles.
