@@ -25,6 +25,7 @@ no dropout there.
 from __future__ import annotations
 
 import argparse
+import inspect
 import json
 import time
 import types
@@ -32,6 +33,8 @@ import types
 import torch
 
 HIDDEN_SUFFIXES = ("attn.c_attn.weight", "attn.c_proj.weight", "mlp.c_fc.weight", "mlp.c_proj.weight")
+# Arguments of a GPT2Model that its blocks need not know of.
+HONOURED = ("input_ids", "inputs_embeds", "position_ids", "token_type_ids", "output_hidden_states", "return_dict")
 
 
 def build(seq):
@@ -60,10 +63,28 @@ class Packing:
 
 def use_train_ops(model, packing: Packing, dtype=torch.float32):
     """Runs the attention and the MLP of every block of a GPT2LMHeadModel on the
-    operators of ``train_ops`` (parameters stay where they are)."""
+    operators of ``train_ops`` (parameters stay where they are).  Which token sees
+    which is the packing's plan alone, nothing is cached between calls, and attention
+    weights have no dropout: a call with an argument that would change any of it
+    (a mask, a cache, attention weights asked for) raises ValueError."""
     from . import train_ops as T
+    cfg = model.config
+    if cfg.activation_function not in ("gelu_new", "gelu_pytorch_tanh") or cfg.add_cross_attention:
+        raise ValueError("expected blocks with the tanh form of GELU and without cross-attention")
 
-    def attention(self, hidden_states, *args, **kwargs):
+    def check(module, args, kwargs):
+        bound = inspect.signature(module.forward).bind(*args, **kwargs)
+        given = dict(bound.arguments)
+        given |= given.pop("kwargs", {})
+        for name, value in given.items():
+            if name not in HONOURED and value is not None and value is not False:
+                raise ValueError(f"blocks on the training-step operators take no {name}")
+        if packing.plan is None:
+            raise ValueError("set the packing's lengths before a forward pass")
+        bound.arguments["use_cache"] = False
+        return bound.args, bound.kwargs
+
+    def attention(self, hidden_states, *args, **kwargs):     # the rest: checked above, or the model's own
         x = hidden_states.flatten(0, 1).to(dtype)
         qkv = T.checkpointed_linear(x, self.c_attn.weight, self.c_attn.bias, layout="io")
         q, k, v = (t.unflatten(1, (-1, self.head_dim)) for t in qkv.split(self.split_size, dim=1))
@@ -80,6 +101,7 @@ def use_train_ops(model, packing: Packing, dtype=torch.float32):
     for block in model.transformer.h:
         block.attn.forward = types.MethodType(attention, block.attn)
         block.mlp.forward = types.MethodType(mlp, block.mlp)
+    model.transformer.register_forward_pre_hook(check, with_kwargs=True)
 
 
 def document_lengths(total, count, longest, gen):

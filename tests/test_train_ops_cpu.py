@@ -180,3 +180,36 @@ def test_front_end_needs_a_gpu_tensor():
                  lambda: T.attention_forward(x[:, None], x[:, None], x[:, None], T.AttentionPlan([4], device="cpu"))):
         with pytest.raises(ValueError):
             call()
+
+
+def _small_gpt2(**over):
+    transformers = pytest.importorskip("transformers")
+    cfg = dict(n_layer=1, n_embd=64, n_head=1, n_positions=32, vocab_size=50, bos_token_id=0, eos_token_id=0)
+    return transformers.GPT2LMHeadModel(transformers.GPT2Config(**cfg | over))
+
+
+def test_patched_model_refuses_what_its_blocks_would_ignore():
+    from paper_2609_36692_amd import e2e_gpt2 as E
+    model, packing = _small_gpt2(), E.Packing("cpu")
+    E.use_train_ops(model, packing)
+    tokens = torch.zeros(1, 4, dtype=torch.long)
+    with pytest.raises(ValueError, match="lengths"):
+        model(tokens)
+    packing.set([3, 1])
+    mask = torch.tensor([[1, 1, 0, 0]])
+    for name, value in {"attention_mask": mask, "past_key_values": object(), "use_cache": True, "output_attentions": True,
+                        "encoder_hidden_states": torch.zeros(1, 4, 64), "head_mask": torch.ones(1)}.items():
+        with pytest.raises(ValueError, match=name):
+            model(tokens, **{name: value})
+    with pytest.raises(ValueError, match="past_key_values|attention_mask|use_cache"):
+        model.generate(tokens, max_new_tokens=1)
+    # What it honours comes as far as the first kernel's check of its device.
+    with pytest.raises(ValueError, match="GPU"):
+        model(tokens, position_ids=torch.tensor([[0, 1, 2, 0]]), labels=tokens, attention_mask=None, use_cache=False)
+
+
+def test_models_that_the_operators_do_not_compute_are_refused():
+    from paper_2609_36692_amd import e2e_gpt2 as E
+    for over in ({"activation_function": "relu"}, {"activation_function": "gelu"}, {"add_cross_attention": True}):
+        with pytest.raises(ValueError):
+            E.use_train_ops(_small_gpt2(**over), E.Packing("cpu"))
