@@ -73,16 +73,16 @@ def use_train_ops(model, packing: Packing, dtype=torch.float32):
         raise ValueError("expected blocks with the tanh form of GELU and without cross-attention")
 
     def check(module, args, kwargs):
-        bound = inspect.signature(module.forward).bind(*args, **kwargs)
-        given = dict(bound.arguments)
+        given = inspect.signature(module.forward).bind(*args, **kwargs).arguments
         given |= given.pop("kwargs", {})
         for name, value in given.items():
             if name not in HONOURED and value is not None and value is not False:
                 raise ValueError(f"blocks on the training-step operators take no {name}")
         if packing.plan is None:
             raise ValueError("set the packing's lengths before a forward pass")
-        bound.arguments["use_cache"] = False
-        return bound.args, bound.kwargs
+        if "use_cache" in given and "use_cache" not in kwargs:       # as a positional argument
+            return None
+        return args, kwargs | {"use_cache": False}
 
     def attention(self, hidden_states, *args, **kwargs):     # the rest: checked above, or the model's own
         x = hidden_states.flatten(0, 1).to(dtype)
