@@ -328,6 +328,15 @@ def checkpoint_weight_grad(c: Checkpoint, dy: torch.Tensor, layout: str = "oi", 
     return out
 
 
+def _plain_types(backward):
+    """A backward pass whose products run in their operands' types, also where it is
+    called under autocast."""
+    def call(*args):
+        with torch.autocast("cuda", enabled=False):
+            return backward(*args)
+    return staticmethod(torch.autograd.function.once_differentiable(call))
+
+
 def _times(x: torch.Tensor, w: torch.Tensor, layout: str) -> torch.Tensor:
     return x @ (w if layout == "io" else w.t())
 
@@ -348,8 +357,7 @@ class _Linear(torch.autograd.Function):
         ctx.save_for_backward(weight, *(() if c is None else (c.codes, c.exps)))
         return y
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_plain_types
     def backward(ctx, dy):
         weight, *held = ctx.saved_tensors
         dx = _back(dy, weight.to(dy.dtype), ctx.layout) if ctx.needs_input_grad[0] else None
@@ -363,8 +371,8 @@ class _Linear(torch.autograd.Function):
 def checkpointed_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None,
                         layout: str = "oi") -> torch.Tensor:
     """A linear layer on x [tokens, inner] that keeps x in 8 bits for its weight
-    gradient.  The product runs in x's type, also under autocast; weights and
-    their gradients may be fp32.  layout: "oi" for y = x W^T, "io" for y = x W."""
+    gradient.  The products run in x's type, also under autocast (forward and
+    backward); weights and their gradients may be fp32.  layout: "oi" for y = x W^T, "io" for y = x W."""
     if layout not in _LAYOUTS:
         raise ValueError("layout is 'io' or 'oi'")
     with torch.autocast("cuda", enabled=False):
@@ -389,8 +397,7 @@ class _Mlp(torch.autograd.Function):
         ctx.save_for_backward(w_in, w_up, w_out, *(t for c in held for t in (c.codes, c.exps)))
         return y
 
-    @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_plain_types
     def backward(ctx, dy):
         w_in, w_up, w_out, *held = ctx.saved_tensors
         inner, mid = ctx.cols

@@ -669,6 +669,32 @@ def test_checkpointed_layers_with_frozen_parts(dev):
         assert torch.equal(T.checkpointed_linear(x, w1, layout="oi"), x @ w1.t())
 
 
+@pytest.mark.parametrize("act", ["linear", "gelu", "swiglu"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_checkpointed_layers_backward_under_autocast(dev, act, dtype):
+    # The same gradients whether the backward pass is called under autocast or not.
+    grads = []
+    for inside in (False, True):
+        g = _gen(dev, 79)
+        x = torch.randn(70, 64, generator=g, device=dev).to(dtype).requires_grad_()
+        w1, w3 = ((torch.randn(160, 64, generator=g, device=dev) * 0.1).requires_grad_() for _ in range(2))
+        w2 = (torch.randn(64, 160, generator=g, device=dev) * 0.1).requires_grad_()
+        with torch.autocast("cuda", BF16):
+            if act == "linear":
+                y = T.checkpointed_linear(x, w1)
+            else:
+                y = T.checkpointed_mlp(x, w1, w2, act=act, w_up=w3 if act == "swiglu" else None)
+            dy = torch.randn(y.shape, generator=g, device=dev).to(dtype)
+            if inside:
+                y.backward(dy)
+        if not inside:
+            y.backward(dy)
+        grads.append([t.grad for t in (x, w1, w2, w3) if t.grad is not None])
+    assert len(grads[0]) == len(grads[1]) == {"linear": 2, "gelu": 3, "swiglu": 4}[act]
+    for a, b in zip(*grads):
+        assert torch.equal(a, b)
+
+
 def test_checkpointed_layers_keep_8_bits(dev):
     x = torch.randn(256, 128, device=dev).requires_grad_()
     w = torch.randn(512, 128, device=dev).requires_grad_()
