@@ -80,6 +80,8 @@ class AttentionPlan:
 
 def _rows(x: torch.Tensor) -> torch.Tensor:
     """[tokens, heads, dim] with the feature stride the kernels take."""
+    if x.dim() != 3:
+        raise ValueError(f"expected a tensor [tokens, heads, dim], got {tuple(x.shape)}")
     return x if x.stride(2) == 1 or x.shape[2] == 1 else x.contiguous()
 
 
@@ -98,13 +100,13 @@ def _attention_args(q, k, v, plan: AttentionPlan, scale):
     """(device index, the fields up to v); checks the operands."""
     tokens, heads, dim = q.shape
     ks = k.shape
-    if len(ks) != 3 or v.shape != ks or ks[0] != tokens or ks[2] != dim or tokens != plan.tokens:
+    if v.shape != ks or ks[0] != tokens or ks[2] != dim or tokens != plan.tokens:
         raise ValueError(f"expected q [tokens, heads, dim] and k, v [tokens, kv_heads, dim] of {plan.tokens} tokens, "
                          f"got {tuple(q.shape)}, {tuple(k.shape)}, {tuple(v.shape)}")
     at, data = _same(q, k, v), plan.data
     if data.get_device() != at:
         raise ValueError("the plan lies on another device")
-    return at, (_dtype(q), heads, ks[1], dim, int(plan.causal), 1.0 / math.sqrt(dim) if scale is None else scale,
+    return at, (_dtype(q), heads, ks[1], dim, int(plan.causal), scale if scale is not None else 1.0 / math.sqrt(dim) if dim else 0.0,
                 tokens, data.data_ptr(), plan.num_tiles, *_heads(q), *_heads(k), *_heads(v))
 
 
@@ -114,8 +116,6 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: A
     packed batch; q [tokens, heads, dim], k and v [tokens, kv_heads, dim], query
     head h reading key head h * kv_heads // heads; scale 1 / sqrt(dim) if None.
     Any strides; views of one projection's output need no copy."""
-    if q.dim() != 3:
-        raise ValueError(f"expected q [tokens, heads, dim], got {tuple(q.shape)}")
     q, k, v = _rows(q), _rows(k), _rows(v)
     at, args = _attention_args(q, k, v, plan, scale)
     if _elsewhere(at):
@@ -133,8 +133,8 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
                        lse: torch.Tensor, plan: AttentionPlan, scale: float | None = None):
     """(dq, dk, dv) from the gradient of ``attention_forward``'s output and what
     that call took and returned."""
-    if q.dim() != 3 or out.shape != q.shape or dout.shape != q.shape:
-        raise ValueError("q, out and dout are [tokens, heads, dim]")
+    if out.shape != q.shape or dout.shape != q.shape:
+        raise ValueError("q, out and dout have one shape")
     q, k, v, out, dout = _rows(q), _rows(k), _rows(v), _rows(out), _rows(dout)
     at, args = _attention_args(q, k, v, plan, scale)
     _same(q, out, dout)
@@ -368,13 +368,21 @@ class _Linear(torch.autograd.Function):
         return dx, dw, db, None
 
 
+def _check_layer(x: torch.Tensor, layout: str):
+    if layout not in _LAYOUTS:
+        raise ValueError("layout is 'io' or 'oi'")
+    if x.dim() != 2:
+        raise ValueError(f"expected x [tokens, inner], got {tuple(x.shape)}")
+    _same(x)
+    _dtype(x)
+
+
 def checkpointed_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tensor | None = None,
                         layout: str = "oi") -> torch.Tensor:
     """A linear layer on x [tokens, inner] that keeps x in 8 bits for its weight
     gradient.  The products run in x's type, also under autocast (forward and
     backward); weights and their gradients may be fp32.  layout: "oi" for y = x W^T, "io" for y = x W."""
-    if layout not in _LAYOUTS:
-        raise ValueError("layout is 'io' or 'oi'")
+    _check_layer(x, layout)
     with torch.autocast("cuda", enabled=False):
         return _Linear.apply(x, weight, bias, layout)
 
@@ -428,7 +436,6 @@ def checkpointed_mlp(x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *
     W_out.  layout as in ``checkpointed_linear``, of all three matrices."""
     if act not in ("gelu", "swiglu") or (act == "swiglu") != (w_up is not None):
         raise ValueError("act is 'gelu', or 'swiglu' with w_up")
-    if layout not in _LAYOUTS:
-        raise ValueError("layout is 'io' or 'oi'")
+    _check_layer(x, layout)
     with torch.autocast("cuda", enabled=False):
         return _Mlp.apply(x, act, layout, w_in, b_in, w_up, w_out, b_out)

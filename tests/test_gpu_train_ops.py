@@ -805,3 +805,16 @@ def test_refusals(dev):
         T.checkpoint_pack(q.flatten(1).half())
     with pytest.raises(TypeError):
         T.checkpoint_unpack(c, torch.float16)
+
+
+def test_refusals_of_empty_heads_and_types(dev):
+    plan = T.AttentionPlan([20], True, dev)
+    empty = torch.empty(20, 2, 0, device=dev, dtype=BF16)
+    with pytest.raises(N.NormPreError) as e:
+        T.attention_forward(empty, empty, empty, plan)
+    assert e.value.code == N.NORMPRE_ERR_INVALID_ARG
+    x, w = torch.randn(20, 64, device=dev), torch.randn(32, 64, device=dev)
+    with torch.no_grad(), pytest.raises(TypeError):
+        T.checkpointed_linear(x.half(), w)
+    with torch.no_grad(), pytest.raises(TypeError):
+        T.checkpointed_mlp(x.double(), w, w.t())

@@ -213,3 +213,26 @@ def test_models_that_the_operators_do_not_compute_are_refused():
     for over in ({"activation_function": "relu"}, {"activation_function": "gelu"}, {"add_cross_attention": True}):
         with pytest.raises(ValueError):
             E.use_train_ops(_small_gpt2(**over), E.Packing("cpu"))
+
+
+def test_front_end_refusals_of_shapes():
+    from paper_2609_36692_amd import train_ops as T
+    plan = T.AttentionPlan([4], device="cpu")
+    q, flat = torch.randn(4, 2, 64), torch.randn(4, 128)
+    for args in ((flat, q, q), (q, flat, q), (q, q, flat), (q[0, 0], q, q)):
+        with pytest.raises(ValueError, match="tokens, heads, dim"):
+            T.attention_forward(*args, plan)
+    with pytest.raises(ValueError):
+        T.attention_backward(q, q, flat, q, q, torch.zeros(2, 4), plan)
+    # Layers, also with nothing to train: no result from anything but the kernels.
+    w = torch.randn(64, 128)
+    with pytest.raises(ValueError, match="GPU"):
+        T.checkpointed_linear(flat, w)
+    with pytest.raises(ValueError, match="GPU"):
+        T.checkpointed_mlp(flat, w, w.t())
+    with pytest.raises(ValueError, match="tokens, inner"):
+        T.checkpointed_linear(flat[None], w)
+    with pytest.raises(ValueError, match="tokens, inner"):
+        T.checkpointed_mlp(flat[None], w, w.t())
+    with pytest.raises(ValueError, match="layout"):
+        T.checkpointed_linear(flat, w, layout="xy")
