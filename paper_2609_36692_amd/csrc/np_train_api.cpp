@@ -68,10 +68,11 @@ int check_operand(const char* name, const normpre_heads& o, int64_t tokens, int6
         return fail(NORMPRE_ERR_UNSUPPORTED, "a stride of %s exceeds 2^40", name);
     if (written) {
         // Rows of one token side by side, or rows of one head (a stride that
-        // is never taken does not matter).
+        // is never taken does not matter).  heads < 2^23 and strides to 2^40 keep the
+        // first product within 64 bits, 2^31 tokens would not the second.
         const int64_t t = tokens > 1 ? o.token_stride : 0, h = heads > 1 ? o.head_stride : 0;
         const bool by_token = (heads == 1 || h >= dim) && (tokens == 1 || t >= (heads - 1) * h + dim);
-        const bool by_head = (tokens == 1 || t >= dim) && (heads == 1 || h >= (tokens - 1) * t + dim);
+        const bool by_head = (tokens == 1 || t >= dim) && (heads == 1 || (h >= dim && (tokens == 1 || (h - dim) / (tokens - 1) >= t)));
         if (!by_token && !by_head) return fail(NORMPRE_ERR_INVALID_ARG, "rows of %s overlap", name);
     }
     return NORMPRE_OK;

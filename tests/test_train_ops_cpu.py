@@ -105,6 +105,16 @@ def test_attention_forward_output_must_not_overlap(lib):
         assert "overlap" in N.normpre_last_error()
 
 
+def test_attention_overlap_of_far_rows(lib):
+    # (tokens - 1) * stride past 64 bits: heads 32 elements apart overlap all the same.
+    sizes = dict(heads=2, kv_heads=2, tokens=(1 << 23) + 1, num_tiles=(1 << 16) + 1, workspace_bytes=1 << 62)
+    for name in ("out", "dq", "dk", "dv"):
+        a = _block(**sizes, **{name: H(P, 1 << 40, 32)})
+        call = lib.normpre_attention_forward if name == "out" else lib.normpre_attention_backward
+        assert call(ctypes.byref(a), None) == INVALID, name
+        assert "overlap" in N.normpre_last_error()
+
+
 def test_attention_null_block_and_empty_batch(lib):
     assert lib.normpre_attention_forward(None, None) == INVALID
     empty = _block(tokens=0, num_tiles=0, q=H(None, 0, 0), plan=None)
