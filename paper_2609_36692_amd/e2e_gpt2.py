@@ -106,7 +106,9 @@ def use_train_ops(model, packing: Packing, dtype=torch.float32):
 
 def document_lengths(total, count, longest, gen):
     """`count` or more random lengths from 1 to `longest` with the sum `total`."""
-    cuts = (torch.rand(count - 1, generator=gen) * (total - 1)).long() + 1
+    if not 1 <= count <= total:
+        raise ValueError(f"{count} documents of {total} tokens")
+    cuts = torch.randperm(total - 1, generator=gen)[:count - 1] + 1
     ends = sorted(set(cuts.tolist()) | set(range(longest, total, longest)) | {total})
     return [b - a for a, b in zip([0] + ends[:-1], ends)]
 
@@ -158,7 +160,8 @@ def main(argv=None):
     for it in range(a.warmup + a.steps):
         tokens = torch.randint(0, 50257, (a.batch, a.seq), generator=gen, device=dev)
         if a.train_ops:
-            lens = document_lengths(a.batch * a.seq, a.documents or a.batch, a.seq, host_gen)
+            lens = document_lengths(a.batch * a.seq, a.batch if a.documents is None else a.documents, a.seq,
+                                    host_gen)
         torch.cuda.synchronize()
         t0 = time.perf_counter()
         if a.train_ops:

@@ -246,3 +246,15 @@ def test_front_end_refusals_of_shapes():
         T.checkpointed_mlp(flat[None], w, w.t())
     with pytest.raises(ValueError, match="layout"):
         T.checkpointed_linear(flat, w, layout="xy")
+
+
+@pytest.mark.parametrize("total,count,longest", [(1, 1, 1), (8, 8, 8), (64, 60, 16), (4096, 24, 1024), (100, 1, 30)])
+def test_document_lengths(total, count, longest):
+    from paper_2609_36692_amd import e2e_gpt2 as E
+    gen = torch.Generator().manual_seed(5)
+    for _ in range(20):
+        lens = E.document_lengths(total, count, longest, gen)
+        assert sum(lens) == total and len(lens) >= count and 1 <= min(lens) and max(lens) <= longest
+    for bad in (0, -1, total + 1):
+        with pytest.raises(ValueError):
+            E.document_lengths(total, bad, longest, gen)
