@@ -347,13 +347,13 @@ def _back(dy: torch.Tensor, w: torch.Tensor, layout: str) -> torch.Tensor:
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, layout):
+    def forward(ctx, x, weight, bias, layout, keep):
         w = weight.to(x.dtype)
         y = _times(x, w, layout)
         if bias is not None:
             y += bias.to(y.dtype)
         ctx.layout, ctx.bias, ctx.cols = layout, None if bias is None else bias.dtype, x.shape[1]
-        c = checkpoint_pack(x) if ctx.needs_input_grad[1] else None
+        c = checkpoint_pack(x) if keep else None
         ctx.save_for_backward(weight, *(() if c is None else (c.codes, c.exps)))
         return y
 
@@ -365,7 +365,13 @@ class _Linear(torch.autograd.Function):
         if held:
             dw = checkpoint_weight_grad(Checkpoint(*held, ctx.cols), dy, ctx.layout).to(weight.dtype)
         db = dy.sum(0, dtype=torch.float32).to(ctx.bias) if ctx.needs_input_grad[2] else None
-        return dx, dw, db, None
+        return dx, dw, db, None, None
+
+
+def _trained(*weights: torch.Tensor | None) -> bool:
+    """Whether a weight gradient may be asked for later, so that x is kept for it
+    (inside an autograd function's forward pass the grad mode is always off)."""
+    return torch.is_grad_enabled() and any(w is not None and w.requires_grad for w in weights)
 
 
 def _check_layer(x: torch.Tensor, layout: str):
@@ -384,12 +390,12 @@ def checkpointed_linear(x: torch.Tensor, weight: torch.Tensor, bias: torch.Tenso
     backward); weights and their gradients may be fp32.  layout: "oi" for y = x W^T, "io" for y = x W."""
     _check_layer(x, layout)
     with torch.autocast("cuda", enabled=False):
-        return _Linear.apply(x, weight, bias, layout)
+        return _Linear.apply(x, weight, bias, layout, _trained(weight))
 
 
 class _Mlp(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, act, layout, w_in, b_in, w_up, w_out, b_out):
+    def forward(ctx, x, act, layout, w_in, b_in, w_up, w_out, b_out, keep):
         u = _times(x, w_in.to(x.dtype), layout)
         if b_in is not None:
             u += b_in.to(u.dtype)
@@ -398,7 +404,7 @@ class _Mlp(torch.autograd.Function):
         y = _times(h, w_out.to(h.dtype), layout)
         if b_out is not None:
             y += b_out.to(y.dtype)
-        cx = checkpoint_pack(x)
+        cx = checkpoint_pack(x) if keep else Checkpoint(None, None, 0)
         ctx.act, ctx.layout, ctx.cols = act, layout, (x.shape[1], u.shape[1])
         ctx.bias = tuple(None if b is None else b.dtype for b in (b_in, b_out))
         held = [cx, cu, ch] + ([] if cup is None else [cup])
@@ -424,7 +430,7 @@ class _Mlp(torch.autograd.Function):
                 dx += _back(dup, w_up.to(dup.dtype), ctx.layout)
         b_in = du.sum(0, dtype=torch.float32).to(ctx.bias[0]) if need[4] else None
         b_out = dy.sum(0, dtype=torch.float32).to(ctx.bias[1]) if need[7] else None
-        return dx, None, None, d_in, b_in, d_up, d_out, b_out
+        return dx, None, None, d_in, b_in, d_up, d_out, b_out, None
 
 
 def checkpointed_mlp(x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *, act: str = "gelu",
@@ -438,4 +444,4 @@ def checkpointed_mlp(x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *
         raise ValueError("act is 'gelu', or 'swiglu' with w_up")
     _check_layer(x, layout)
     with torch.autocast("cuda", enabled=False):
-        return _Mlp.apply(x, act, layout, w_in, b_in, w_up, w_out, b_out)
+        return _Mlp.apply(x, act, layout, w_in, b_in, w_up, w_out, b_out, _trained(w_in, w_up))

@@ -695,6 +695,29 @@ def test_checkpointed_layers_backward_under_autocast(dev, act, dtype):
         assert torch.equal(a, b)
 
 
+def test_checkpointed_layers_keep_x_for_training_only(dev, monkeypatch):
+    packed = []
+    pack = T.checkpoint_pack
+    monkeypatch.setattr(T, "checkpoint_pack", lambda x: packed.append(x.shape) or pack(x))
+    x = torch.randn(40, 64, device=dev)
+    w1, w2, w3 = (torch.randn(128, 64, device=dev).requires_grad_() for _ in range(3))
+    layers = [lambda a, b, c: T.checkpointed_linear(x, a), lambda a, b, c: T.checkpointed_mlp(x, a, b.t()),
+              lambda a, b, c: T.checkpointed_mlp(x, a, b.t(), act="swiglu", w_up=c)]
+    trained = [f(w1, w2, w3).detach() for f in layers]
+    assert packed == [x.shape] * 3
+    with torch.no_grad():
+        for f, y in zip(layers, trained):
+            assert torch.equal(f(w1, w2, w3), y)
+    # Frozen in part: x is not needed for w_out's gradient.
+    f1, f3 = w1.detach(), w3.detach()
+    for f in layers[1:]:
+        f(f1, w2, f3).sum().backward()
+        assert w2.grad is not None
+    assert packed == [x.shape] * 3
+    T.checkpointed_mlp(x, f1, w2.t(), act="swiglu", w_up=w3).sum().backward()
+    assert packed == [x.shape] * 4 and w3.grad is not None and w1.grad is None
+
+
 def test_checkpointed_layers_keep_8_bits(dev):
     x = torch.randn(256, 128, device=dev).requires_grad_()
     w = torch.randn(512, 128, device=dev).requires_grad_()
