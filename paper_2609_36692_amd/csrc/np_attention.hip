@@ -45,6 +45,7 @@
 // over 6000 rows 1.04e-6 / 0.43e-6 of their norm, of out 0.35e-6 / 0.23e-6.
 #include "np_train.h"
 
+#include <cmath>
 #include <type_traits>
 
 namespace np {
@@ -535,7 +536,9 @@ __device__ __forceinline__ bool any_nonfinite(const f32x16 (&acc)[NT]) {
 // that are not finite, rows that must not see them come out as NaN.  Rows of
 // the tiled passes that are not finite are therefore done again here, by one
 // wave each, over the places that they see and no others: lanes first along
-// the other side (64 scores at a time), then along the features.
+// the other side (64 scores at a time), then along the features.  The forward
+// pass also sums o before it divides by l, with weights of up to 2^8, so values
+// above 2^120 / l may pass fp32's range on the way; here o is a mean at every step.
 template <class T>
 __device__ __forceinline__ float dot(const T* a, const T* b, int dim) {
     float s = 0.f;
@@ -563,12 +566,14 @@ __device__ void forward_row(const AttnArgs& a, const Where& w, int qi, int lane)
         const float t = lane < n ? dot(q, row_of<T>(a.k, w, k0 + lane, w.kv), a.dim) * c2 : -INFINITY;
         const float mn = fmaxf(m, wave_max(t)), mu = mn == -INFINITY ? 0.f : mn;
         const float p = exp2_fast(t - mu), f = exp2_fast(m - mu);
-        l = l * f + wave_sum(p);
+        const float before = l * f;
+        l = before + wave_sum(p);
         m = mn;
-        o[0] *= f;
-        o[1] *= f;
+        const float r = l > 0.f ? 1.f / l : 0.f;
+        o[0] *= before * r;
+        o[1] *= before * r;
         for (int j = 0; j < n; ++j) {
-            const float pj = __shfl(p, j, 64);
+            const float pj = __shfl(p, j, 64) * r;
             const T* v = row_of<T>(a.v, w, k0 + j, w.kv);
 #pragma unroll
             for (int x = 0; x < 2; ++x)
@@ -578,7 +583,7 @@ __device__ void forward_row(const AttnArgs& a, const Where& w, int qi, int lane)
     T* out = row_of<T>(a.out, w, qi, w.head);
 #pragma unroll
     for (int x = 0; x < 2; ++x)
-        if (lane + 64 * x < a.dim) out[lane + 64 * x] = (T)(o[x] / l);
+        if (lane + 64 * x < a.dim) out[lane + 64 * x] = (T)(l > 0.f ? o[x] : NAN);
     if (lane == 0) a.lse[w.head * a.tokens + w.start + qi] = m * kLn2 + logf(l);
 }
 

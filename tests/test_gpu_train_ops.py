@@ -132,6 +132,19 @@ def test_attention_fp32_magnitudes(dev, d, fq, fk, fv, fdout):
     _check(fq * q, fk * k, fv * v, fdout * dout, [150, 40], True)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attention_of_the_largest_values(dev, dtype, d):
+    # A mean of values near the end of the range, of one sign or both, is in range.
+    lens = [300, 40]
+    q, k, v, _ = _qkv(dev, 26, sum(lens), 2, 1, d, dtype)
+    v = (3e38 * torch.sign(v)).to(dtype)
+    v[:300, :, 3] = 3e38
+    out, _ = T.attention_forward(q, k, v, T.AttentionPlan(lens, True, dev))
+    want, tol = attention_reference(q, k, v, lens, True, 1 / math.sqrt(d))
+    assert_within("out", out, want["out"], tol["out"][1 if dtype == BF16 else 0])
+
+
 def test_attention_fp32_products(dev):
     # One token a sequence, one feature: the log-sum-exp is the product q k.  The
     # split may leave out 8 u of it, the sum of the terms' products may cut off 2 u,
