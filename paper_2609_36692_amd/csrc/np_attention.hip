@@ -534,15 +534,36 @@ __device__ __forceinline__ bool any_nonfinite(const f32x16 (&acc)[NT]) {
 // A matrix product multiplies the zero weight of a masked place with the
 // value there, and 0 * inf is NaN: where a tile on the diagonal holds values
 // that are not finite, rows that must not see them come out as NaN.  Rows of
-// the tiled passes that are not finite are therefore done again here, by one
-// wave each, over the places that they see and no others: lanes first along
-// the other side (64 scores at a time), then along the features.  The forward
-// pass also sums o before it divides by l, with weights of up to 2^8, so values
-// above 2^120 / l may pass fp32's range on the way; here o is a mean at every step.
+// the tiled passes that are not finite, unless that is their answer (odd_rows),
+// are therefore done again here, by one wave each, over the places that they see
+// and no others: lanes first along the other side (64 scores at a time), then along
+// the features, up to the point where every feature is NaN.  The forward pass also
+// sums o before it divides by l, with weights of up to 2^8, so values above 2^120 / l
+// may pass fp32's range on the way; here o is a mean at every step.
+template <class T, int N>
+__device__ __forceinline__ void dot_step(float& s, const T* a, const T* b) {      // N pieces of 16 bytes, at any element
+    constexpr int E = 16 / sizeof(T);
+    typedef u32x4 u32x4_any __attribute__((aligned(2)));
+    u32x4 x[N], y[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[i] = *reinterpret_cast<const u32x4_any*>(a + i * E);
+        y[i] = *reinterpret_cast<const u32x4_any*>(b + i * E);
+    }
+    T u[N * E], v[N * E];
+    __builtin_memcpy(u, x, 16 * N);
+    __builtin_memcpy(v, y, 16 * N);
+#pragma unroll
+    for (int i = 0; i < N * E; ++i) s = __builtin_fmaf((float)u[i], (float)v[i], s);
+}
 template <class T>
 __device__ __forceinline__ float dot(const T* a, const T* b, int dim) {
+    constexpr int E = 16 / sizeof(T);
     float s = 0.f;
-    for (int d = 0; d < dim; ++d) s = __builtin_fmaf((float)a[d], (float)b[d], s);
+    int d = 0;
+    for (; d + 4 * E <= dim; d += 4 * E) dot_step<T, 4>(s, a + d, b + d);
+    for (; d + E <= dim; d += E) dot_step<T, 1>(s, a + d, b + d);
+    for (; d < dim; ++d) s = __builtin_fmaf((float)a[d], (float)b[d], s);
     return s;
 }
 
@@ -555,8 +576,34 @@ __device__ __forceinline__ T* row_of(const AttnOperand& o, const Where& w, int r
     return static_cast<T*>(o.p) + (int64_t)(w.start + row) * o.tok + (int64_t)head * o.head;
 }
 
+// acc += sum_j w_j row_j over rows r0 .. r0 + n - 1 of o; w_j: lane j's w; acc[x]: feature
+// lane + 64 x (past the last one: not used).  Eight rows are loaded at a time.
 template <class T>
-__device__ void forward_row(const AttnArgs& a, const Where& w, int qi, int lane) {
+__device__ __forceinline__ void add_rows(float (&acc)[2], float w, const AttnOperand& o, const Where& at, int head,
+                                         int r0, int n, int dim, int lane) {
+    for (int j0 = 0; j0 < n; j0 += 8) {
+        float v[8][2];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const T* row = row_of<T>(o, at, r0 + min(j0 + u, n - 1), head);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) v[u][x] = (float)row[min(lane + 64 * x, dim - 1)];
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const float f = __shfl(w, j0 + u, 64);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) acc[x] = j0 + u < n ? __builtin_fmaf(f, v[u][x], acc[x]) : acc[x];
+        }
+    }
+}
+
+__device__ __forceinline__ bool all_nan(const float (&g)[2], int lane, int dim) {
+    return __all((lane >= dim || g[0] != g[0]) && (lane + 64 >= dim || g[1] != g[1]));
+}
+
+template <class T>
+__device__ void forward_row(const AttnArgs& a, const Where& w, int qi, bool has_lse, int lane) {
     const T* q = row_of<T>(a.q, w, qi, w.head);
     const int end = a.causal ? qi + 1 : w.len;
     const float c2 = a.scale * kLog2e;
@@ -569,22 +616,18 @@ __device__ void forward_row(const AttnArgs& a, const Where& w, int qi, int lane)
         const float before = l * f;
         l = before + wave_sum(p);
         m = mn;
+        if (l != l) break;                           // so is every feature
         const float r = l > 0.f ? 1.f / l : 0.f;
         o[0] *= before * r;
         o[1] *= before * r;
-        for (int j = 0; j < n; ++j) {
-            const float pj = __shfl(p, j, 64) * r;
-            const T* v = row_of<T>(a.v, w, k0 + j, w.kv);
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-                if (lane + 64 * x < a.dim) o[x] = __builtin_fmaf(pj, (float)v[lane + 64 * x], o[x]);
-        }
+        add_rows<T>(o, p * r, a.v, w, w.kv, k0, n, a.dim, lane);
+        if (has_lse && all_nan(o, lane, a.dim)) break;
     }
     T* out = row_of<T>(a.out, w, qi, w.head);
 #pragma unroll
     for (int x = 0; x < 2; ++x)
         if (lane + 64 * x < a.dim) out[lane + 64 * x] = (T)(l > 0.f ? o[x] : NAN);
-    if (lane == 0) a.lse[w.head * a.tokens + w.start + qi] = m * kLn2 + logf(l);
+    if (lane == 0 && !has_lse) a.lse[w.head * a.tokens + w.start + qi] = m * kLn2 + logf(l);
 }
 
 // sum_j p dp of one row.
@@ -612,13 +655,8 @@ __device__ void dq_row(const AttnArgs& a, const Where& w, int qi, float delta, i
             const float p = exp2_fast(dot(q, row_of<T>(a.k, w, k0 + lane, w.kv), a.dim) * c2 - lse2);
             ds = p * (dot(dout, row_of<T>(a.v, w, k0 + lane, w.kv), a.dim) - delta);
         }
-        for (int j = 0; j < n; ++j) {
-            const float dj = __shfl(ds, j, 64);
-            const T* k = row_of<T>(a.k, w, k0 + j, w.kv);
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-                if (lane + 64 * x < a.dim) g[x] = __builtin_fmaf(dj, (float)k[lane + 64 * x], g[x]);
-        }
+        add_rows<T>(g, ds, a.k, w, w.kv, k0, n, a.dim, lane);
+        if (all_nan(g, lane, a.dim)) break;
     }
     T* dq = row_of<T>(a.dq, w, qi, w.head);
 #pragma unroll
@@ -632,8 +670,9 @@ __device__ void dkv_row(const AttnArgs& a, const Where& w, int ki, int lane) {
     const int beg = a.causal ? ki : 0, group = a.heads / a.kv_heads;
     const float c2 = a.scale * kLog2e;
     float gk[2] = {0.f, 0.f}, gv[2] = {0.f, 0.f};
-    for (int h = w.kv * group; h < (w.kv + 1) * group; ++h)
-        for (int q0 = beg; q0 < w.len; q0 += 64) {
+    bool lost = false;
+    for (int h = w.kv * group; h < (w.kv + 1) * group && !lost; ++h)
+        for (int q0 = beg; q0 < w.len && !lost; q0 += 64) {
             const int n = min(64, w.len - q0);
             float p = 0.f, ds = 0.f;
             if (lane < n) {
@@ -641,16 +680,9 @@ __device__ void dkv_row(const AttnArgs& a, const Where& w, int ki, int lane) {
                 p = exp2_fast(dot(row_of<T>(a.q, w, q0 + lane, h), k, a.dim) * c2 - a.lse[at] * kLog2e);
                 ds = p * (dot(row_of<T>(a.dout, w, q0 + lane, h), v, a.dim) - a.delta[at]);
             }
-            for (int j = 0; j < n; ++j) {
-                const float pj = __shfl(p, j, 64), dj = __shfl(ds, j, 64);
-                const T *q = row_of<T>(a.q, w, q0 + j, h), *dout = row_of<T>(a.dout, w, q0 + j, h);
-#pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    if (lane + 64 * x < a.dim) {
-                        gk[x] = __builtin_fmaf(dj, (float)q[lane + 64 * x], gk[x]);
-                        gv[x] = __builtin_fmaf(pj, (float)dout[lane + 64 * x], gv[x]);
-                    }
-            }
+            add_rows<T>(gk, ds, a.q, w, h, q0, n, a.dim, lane);
+            add_rows<T>(gv, p, a.dout, w, h, q0, n, a.dim, lane);
+            lost = all_nan(gk, lane, a.dim) && all_nan(gv, lane, a.dim);
         }
     T *dk = row_of<T>(a.dk, w, ki, w.kv), *dv = row_of<T>(a.dv, w, ki, w.kv);
 #pragma unroll
@@ -661,10 +693,100 @@ __device__ void dkv_row(const AttnArgs& a, const Where& w, int ki, int lane) {
         }
 }
 
-// Owned rows (bit r: row r of the wave's 32) that any lane calls bad.
+// Owned rows (bit r: row r of the wave's 32) that any lane calls bad.  Not to be asked
+// with x < INFINITY alone: the compiler's ballot makes x != INFINITY of that, which
+// holds for NaN.
 __device__ __forceinline__ uint32_t bad_rows(bool bad) {
     const uint64_t b = __ballot(bad);
     return (uint32_t)b | (uint32_t)(b >> 32);
+}
+
+// Most rows that are not finite are right as the tiled passes made them: what they
+// see is not finite either, and a NaN early in a long sequence would otherwise send
+// every later row here (one NaN in k or v, 4096 tokens, 4 heads of 64: forward 32 ms,
+// backward 58, where the tiled passes take 0.07 and 0.13).  What a wave made is wrong
+// only
+//   - where a place that a row does not see held a value that is not finite: those
+//     places lie in the 32 to 64 rows of the tile on the diagonal, and behind the
+//     sequence's end, where its last row stands again;
+//   - where terms and copies made NaN of an infinity: fp32, and heads that leave a
+//     part of the tile to copies (Direct), if an operand holds one;
+//   - (forward) where finite values passed the range.
+// So the operands' rows are searched, by a wave that has such rows: 16 lanes a row.
+struct Odd {
+    bool inf, any;                               // an infinity, any value not finite
+    int first, last;                             // row
+};
+template <class T>
+__device__ Odd odd_rows(const AttnOperand& o, const Where& w, int head, int from, int to, int dim, int lane) {
+    bool inf = false, any = false;
+    int first = INT32_MAX, last = -1;
+    for (int r = from + (lane >> 4); r < to; r += 4) {
+        const T* x = row_of<T>(o, w, r, head);
+        bool i = false, n = false;
+        for (int d = lane & 15; d < dim; d += 16) {
+            const float v = (float)x[d];
+            i |= __builtin_fabsf(v) == INFINITY;
+            n |= !(__builtin_fabsf(v) < INFINITY);
+        }
+        inf |= i;
+        any |= n;
+        if (n) {
+            first = min(first, r);
+            last = r;
+        }
+    }
+#pragma unroll
+    for (int s = 32; s >= 1; s >>= 1) {
+        first = min(first, __shfl_xor(first, s, 64));
+        last = max(last, __shfl_xor(last, s, 64));
+    }
+    return {(bool)__any(inf), (bool)__any(any), first, last};
+}
+// Whether what the tiled passes make of visible values is the formula's.
+template <class T, int DP, bool VEC>
+__device__ __forceinline__ bool faithful(const AttnArgs& a) { return kTerms<T> == 1 && (!VEC || a.dim == DP); }
+
+// The query passes: the highest of the wave's rows, from row qw on, that x (v, or
+// k) spoils although it does not see the place, or INT_MAX: all of them.  Rows before
+// `done` were multiplied.
+template <class T>
+__device__ int spoiled_queries(const AttnArgs& a, const Where& w, const AttnOperand& x, int qw, int done, int lane) {
+    const Odd o = odd_rows<T>(x, w, w.kv, a.causal ? qw : w.len - 1, min(done, w.len), a.dim, lane);
+    return a.causal ? o.last : done > w.len && o.inf ? INT32_MAX : -1;
+}
+
+// dk and dv: the keys above the one that this returns, of 32 from row kw on, are spoiled
+// by queries that do not see them; INT_MAX: none, -1: all.
+template <class T>
+__device__ int spoiled_keys(const AttnArgs& a, const Where& w, int kw, bool right, int lane) {
+    const int group = a.heads / a.kv_heads;
+    // A query that every key of the wave sees and that has no log-sum-exp: all NaN.
+    const int sure = a.causal ? min(kw + 31, w.len - 1) : 0;
+    bool lost = false;
+    for (int h = w.kv * group; h < (w.kv + 1) * group; ++h)
+        for (int i = sure + lane; i < w.len; i += 64) {
+            const float l = a.lse[h * a.tokens + w.start + i];
+            lost |= l != l;
+        }
+    if (__any(lost)) return INT32_MAX;
+    if (!right) {
+        bool inf = odd_rows<T>(a.k, w, w.kv, kw, min(kw + 32, w.len), a.dim, lane).inf ||
+                   odd_rows<T>(a.v, w, w.kv, kw, min(kw + 32, w.len), a.dim, lane).inf;
+        for (int h = w.kv * group; h < (w.kv + 1) * group && !inf; ++h)
+            inf = odd_rows<T>(a.q, w, h, a.causal ? kw : 0, w.len, a.dim, lane).inf ||
+                  odd_rows<T>(a.dout, w, h, a.causal ? kw : 0, w.len, a.dim, lane).inf;
+        if (inf) return -1;
+    }
+    const bool copies = w.len % 32 != 0;
+    int low = INT32_MAX;
+    for (int h = w.kv * group; h < (w.kv + 1) * group; ++h)
+        for (int x = 0; x < 2; ++x) {
+            const AttnOperand& o = x ? a.dout : a.q;
+            if (a.causal) low = min(low, odd_rows<T>(o, w, h, kw, min(kw + 32, w.len), a.dim, lane).first);
+            if (copies && odd_rows<T>(o, w, h, w.len - 1, w.len, a.dim, lane).inf) return -1;
+        }
+    return low;
 }
 
 // ---------------------------------------------------------------- passes ---
@@ -817,11 +939,29 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
         m = mx;
     }
     uint32_t bad = bad_rows(live && (any_nonfinite(o) || !(l < INFINITY)));
+    const uint32_t lost = bad_rows(l != l);          // all NaN, of a visible score
+    if (bad) {
+        const int sees = a.causal ? qw + 1 : w.len;  // keys that every row of the wave sees
+        bool right = faithful<T, DP, VEC>(a);
+        if (!right)
+            right = !odd_rows<T>(a.q, w, head, qw, min(qw + 32, w.len), a.dim, lane).inf &&
+                    !odd_rows<T>(a.k, w, kv, 0, end, a.dim, lane).inf && !odd_rows<T>(a.v, w, kv, 0, end, a.dim, lane).inf;
+        if (right) {
+            bad &= ~lost;
+            if (bad) {
+                const int top = odd_rows<T>(a.v, w, kv, 0, sees, a.dim, lane).any
+                              ? spoiled_queries<T>(a, w, a.v, qw, ((a.causal ? min(end, qw + 32) : end) + BN - 1) / BN * BN, lane) : INT32_MAX;
+                bad &= bad_rows(qi <= top);
+            }
+        }
+    }
     store_rows<T, DP, VEC>(mine, row_of<T>(a.out, w, qw, head), a.out.tok, o, 1.f / l,
                            a.dim, live_rows(qw, w.len) & ~bad, lane);
-    if (live && half == 0 && !(bad >> lane & 1))
+    // A sum that is not NaN stands: every place it takes in is seen.
+    if (live && half == 0 && !(bad & lost & 1u << lane))
         a.lse[head * a.tokens + w.start + qi] = m * fabsf(a.scale) + logf(l);
-    for (; bad; bad &= bad - 1) forward_row<T>(a, w, qw + __builtin_ctz(bad), lane);
+    for (; bad; bad &= bad - 1)
+        forward_row<T>(a, w, qw + __builtin_ctz(bad), !(lost >> __builtin_ctz(bad) & 1), lane);
 }
 
 // dq, and delta and the base-2 log-sum-exp for the dk/dv pass: the forward pass's
@@ -950,6 +1090,15 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
         }
     if (live && half == 0) a.lse2[at] = lse2;
     if (live && half == 0) a.delta[at] = delta;
+    bad &= ~bad_rows(lse2 != lse2 || delta != delta);          // all NaN
+    if (bad) {
+        bool right = faithful<T, DP, VEC>(a);
+        if (!right)
+            right = !odd_rows<T>(a.q, w, head, qw, min(qw + 32, w.len), a.dim, lane).inf &&
+                    !odd_rows<T>(a.dout, w, head, qw, min(qw + 32, w.len), a.dim, lane).inf &&
+                    !odd_rows<T>(a.k, w, kv, 0, end, a.dim, lane).inf && !odd_rows<T>(a.v, w, kv, 0, end, a.dim, lane).inf;
+        if (right) bad &= bad_rows(qi <= spoiled_queries<T>(a, w, a.k, qw, ((a.causal ? min(end, qw + 32) : end) + 31) / 32 * 32, lane));
+    }
     store_rows<T, DP, VEC>(mine, row_of<T>(a.dq, w, qw, head), a.dq.tok, g,
                            a.scale, a.dim, live_rows(qw, w.len) & ~bad, lane);
     for (; bad; bad &= bad - 1) {
@@ -1100,10 +1249,31 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : kTerms<T> == 3 ? 1 : wav
         store_rows<float, DP, true>(mine, part + one, DP, gv, 1.f, a.dim, keep, lane);
         return;
     }
-    uint32_t bad = bad_rows(live && (any_nonfinite(gk) || any_nonfinite(gv)));
-    store_rows<T, DP, VEC>(mine, row_of<T>(a.dk, w, kw, kv), a.dk.tok, gk, a.scale, a.dim, keep & ~bad, lane);
-    store_rows<T, DP, VEC>(mine, row_of<T>(a.dv, w, kw, kv), a.dv.tok, gv, 1.f, a.dim, keep & ~bad, lane);
-    for (; bad; bad &= bad - 1) dkv_row<T>(a, w, kw + __builtin_ctz(bad), lane);
+    const uint32_t bad = bad_rows(live && (any_nonfinite(gk) || any_nonfinite(gv)));
+    if (lane == 0) a.odd[blockIdx.x * 4 + wave] = bad;
+    store_rows<T, DP, VEC>(mine, row_of<T>(a.dk, w, kw, kv), a.dk.tok, gk, a.scale, a.dim, keep, lane);
+    store_rows<T, DP, VEC>(mine, row_of<T>(a.dv, w, kw, kv), a.dv.tok, gv, 1.f, a.dim, keep, lane);
+}
+
+// Rows of dk and dv that attn_dkv_kernel found not finite: a wave for 32 of them.  In a
+// launch of its own (2 us), since in the kernel above their addresses would take scalar
+// registers that it has not: kept in vector registers, they slow it by a fifth
+// (packed 16418 tokens, 16/8 heads of 128, forward and backward 1097 us / 1235).
+template <class T, int DP, bool VEC>
+__global__ void __launch_bounds__(kThreads) attn_odd_keys_kernel(AttnArgs a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const AttnTile tile = a.tiles[a.num_tiles + blockIdx.x / a.kv_heads];
+    const int kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads;
+    int kw;
+    if (!locate(a, tile, wave * 32, kw)) return;
+    uint32_t bad = a.odd[blockIdx.x * 4 + wave];
+    if (!bad) return;
+    const Where w{tile.start, tile.len, kv * group, kv};
+    const int above = spoiled_keys<T>(a, w, kw, faithful<T, DP, VEC>(a), lane);
+    for (; bad; bad &= bad - 1) {
+        const int ki = kw + __builtin_ctz(bad);
+        if (ki > above) dkv_row<T>(a, w, ki, lane);
+    }
 }
 
 // Adds the shares of dk and dv, in their order: four features a thread, the rows
@@ -1136,7 +1306,8 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a) {
     // Rows that are not finite, of this wave: one by one.
     const uint64_t bad = __ballot(live && !(t == 0.f));
     constexpr uint64_t row_lanes = LR == 16 ? 0xffffull : 0xffffffffull;
-    const bool redo = bad >> (lane / LR * LR) & row_lanes;
+    const int above = bad ? spoiled_keys<T>(a, w, (ki - lane / LR) / 32 * 32, faithful<T, DP, true>(a), lane) : 0;
+    const bool redo = (bad >> (lane / LR * LR) & row_lanes) && ki > above;
     if (live && !redo) {
         T *dk = row_of<T>(a.dk, w, ki, kv), *dv = row_of<T>(a.dv, w, ki, kv);
 #pragma unroll
@@ -1147,7 +1318,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a) {
             }
     }
     for (int k = 0; k < 64 / LR; ++k)
-        if (bad >> (k * LR) & row_lanes) dkv_row<T>(a, w, ki - lane / LR + k, lane);
+        if ((bad >> (k * LR) & row_lanes) && ki - lane / LR + k > above) dkv_row<T>(a, w, ki - lane / LR + k, lane);
 }
 
 // -------------------------------------------------------------- launches ---
@@ -1195,8 +1366,9 @@ hipError_t run(const AttnArgs& a, bool backward, hipStream_t s) {
         attn_dkv_kernel<T, DP, VEC, can_hold><<<keys, kThreads, 0, s>>>(a);
     else attn_dkv_kernel<T, DP, VEC, false><<<keys, kThreads, 0, s>>>(a);
     e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    attn_join_kernel<T, DP><<<dim3((unsigned)a.num_tiles * a.kv_heads, DP / 8), kThreads, 0, s>>>(a);
+    if (e != hipSuccess) return e;
+    if (a.splits == 1) attn_odd_keys_kernel<T, DP, VEC><<<keys, kThreads, 0, s>>>(a);
+    else attn_join_kernel<T, DP><<<dim3((unsigned)a.num_tiles * a.kv_heads, DP / 8), kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -1223,7 +1395,8 @@ int attention_splits(int64_t num_tiles, int kv_heads) {
 
 int64_t attention_workspace(const AttnArgs& a) {
     const int64_t rows = 2 * (int64_t)a.heads * a.tokens, pitch = a.dim <= 64 ? 64 : 128;
-    return (rows + 3) / 4 * 4 + (a.splits > 1 ? 2 * a.splits * (int64_t)a.kv_heads * a.tokens * pitch : 0);
+    return (rows + 3) / 4 * 4 + (a.splits > 1 ? 2 * a.splits * (int64_t)a.kv_heads * a.tokens * pitch
+                                              : (int64_t)kAttnRows / 32 * a.num_tiles * a.kv_heads);
 }
 
 hipError_t launch_attention_forward(DType t, const AttnArgs& a, hipStream_t s) {

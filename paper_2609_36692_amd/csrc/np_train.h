@@ -31,6 +31,8 @@ struct AttnArgs {
     float* lse2;                // backward workspace, [heads][tokens] each: lse in
     float* delta;               // base 2, and delta
     float* partial;             // [splits][2][kv_heads][tokens][64 or 128], splits > 1
+    uint32_t* odd;              // splits = 1: rows of dk and dv that are not finite, a
+                                // bit each, [num_tiles][kv_heads][4], in its place
     int splits;                 // shares of a key's queries (dk/dv pass)
     const AttnTile* tiles;      // query tiles, then as many key tiles
     int num_tiles;
@@ -40,7 +42,7 @@ struct AttnArgs {
 };
 
 // Shares into which the dk/dv pass cuts the queries of a key, and the floats of
-// workspace that a backward call needs (lse2 and delta, then the partial sums).
+// workspace that a backward call needs (lse2 and delta, then the partial sums or odd).
 int attention_splits(int64_t num_tiles, int kv_heads);
 int64_t attention_workspace(const AttnArgs& a);
 hipError_t launch_attention_forward(DType t, const AttnArgs& a, hipStream_t s);

@@ -157,6 +157,7 @@ int attention(const normpre_attention* a, bool backward, void* stream) {
     k.lse2 = ws;
     k.delta = ws + rows;
     k.partial = ws + (2 * rows + 3) / 4 * 4;
+    k.odd = reinterpret_cast<uint32_t*>(k.partial);
     return launched(launch_attention_backward(dt, k, (hipStream_t)stream));
 }
 

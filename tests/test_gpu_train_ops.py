@@ -204,6 +204,65 @@ def test_attention_nonfinite_in_the_last_features(dev, dtype, d, value, where, s
     _check(**x, lens=lens, causal=True)
 
 
+@pytest.mark.parametrize("dtype,hq,hk,d,crowd", [(BF16, 4, 2, 64, 0), (BF16, 2, 2, 128, 300), (F32, 2, 1, 64, 0),
+                                                 (F32, 2, 1, 128, 600), (BF16, 2, 1, 96, 0)])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("where", ["q", "k", "v", "dout"])
+@pytest.mark.parametrize("values", ["nan", "inf", "both", "all", "last", "first"])
+def test_attention_nonfinite_in_long_sequences(dev, dtype, hq, hk, d, causal, crowd, where, values):
+    # Rows far behind a value that is not finite, rows beside it, whole operands, the
+    # ends of a sequence; batches whose keys' queries are shared out and not.
+    lens = [203, 70] + [1] * crowd
+    x = dict(zip(("q", "k", "v", "dout"), _qkv(dev, 45, sum(lens), hq, hk, d, dtype)))
+    y, nan, inf = x[where], float("nan"), float("inf")
+    if values == "all":
+        y[:203] = nan
+    elif values in ("last", "first"):
+        y[202 if values == "last" else 0, 0, 1] = inf
+        y[272 if values == "last" else 203, 0, d - 1] = nan
+    else:
+        if values != "inf":
+            y[60, 0, 3] = nan
+        if values != "nan":
+            y[75, -1, 2], y[230, 0, 4] = inf, -inf
+    _check(**x, lens=lens, causal=causal)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("where", ["one k", "all q", "all k", "all v", "all dout"])
+def test_attention_nan_costs_no_second_pass(dev, dtype, where):
+    # Results that are NaN by the formula are not computed again: 25 times the time
+    # of finite operands is far above what the search for them takes, and far below
+    # that of a second, scalar pass (100 to 500 times).
+    n = 4096
+    q, k, v, dout = _qkv(dev, 46, n, 4, 4, 64, dtype)
+    plan = T.AttentionPlan([n], True, dev)
+
+    def least():
+        times = []
+        for _ in range(5):
+            ends = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
+            ends[0].record()
+            out, lse = T.attention_forward(q, k, v, plan)
+            ends[1].record()
+            grads = T.attention_backward(dout, q, k, v, out, lse, plan)
+            ends[2].record()
+            ends[2].synchronize()
+            times.append([a.elapsed_time(b) for a, b in zip(ends, ends[1:])])
+        return [min(t) for t in zip(*times)], (out, *grads)
+
+    finite, _ = least()
+    count, name = where.split()
+    x = {"q": q, "k": k, "v": v, "dout": dout}[name]
+    x[n // 2 if count == "one" else slice(None)] = float("nan")
+    got, (out, dq, dk, dv) = least()
+    print(f"finite {finite} ms, {where} NaN {got} ms")
+    assert got[0] <= 25 * finite[0] and got[1] <= 25 * finite[1]
+    first = n // 2 if count == "one" else 0
+    assert torch.isnan(dq[first:]).all() and torch.isnan(dk[first:]).all()
+    assert torch.isnan(out[first:]).all() or name == "dout"
+
+
 def test_attention_all_scores_minus_infinity(dev):
     # Formula of a row whose scores are all -inf: 0 / 0.
     q = torch.ones(4, 1, 64, device=dev)
