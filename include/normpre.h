@@ -514,7 +514,10 @@ int normpre_attention_workspace(const normpre_attention* a, int64_t* bytes);
  * The backward call takes q, k, v, out and lse of the forward call and
  * d loss / d out, and writes d loss / d q, k, v (of a shared key head: summed
  * over its query heads).  bf16 operands: p and ds are rounded to bf16 for
- * their products.
+ * their products, and sum_j p_ij (do_i . v_j) of a query that sees more than 128
+ * keys is taken as do_i . out_i, with out as rounded to bf16: where one key has
+ * nearly all weight, so that the gradients of its scores vanish, they keep an error of
+ * up to 2^-8 |do_i| |out_i|.
  * Errors: INVALID_ARG (null or misaligned pointers, unknown dtype, heads not
  * a multiple of kv_heads, head_dim < 1, negative strides, an output whose
  * rows overlap, a non-finite scale, num_tiles < 0, causal not 0 or 1, tokens

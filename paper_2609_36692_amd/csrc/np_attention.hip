@@ -404,7 +404,8 @@ __device__ __forceinline__ bf16x8 columns(const bf16_t* lds, int r0, int t, int 
 // acc[t] (features 32 t .. of the result, by owned row) += tile^T weights,
 // over streamed rows [base, base + 32); w in the layout of scores().  The
 // weights of bf16 operands are rounded to bf16, as matrix instructions take
-// them: relative error 2^-9 each, below the rounding of the bf16 result.  fp32
+// them: relative error up to 2^-8 each, as that of the bf16 result, but of random
+// sign along a sum.  fp32
 // tiles are summed apart and then added, so that a long sum rounds once a tile at
 // its full size: half the error of dk and dv over 6000 rows for 1% of the time.
 template <class T, int DP>
@@ -1030,11 +1031,15 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
     };
     // Whether some row of the wave sees block b of the tile from k0 on.
     auto seen = [&](int k0, int b) { return k0 + 32 * b < end && (!a.causal || k0 + 32 * b <= qw + 31); };
-    // delta = do . o carries the rounding of o.  Where a row sees few keys, o
-    // is as large as a value and that error as large as the other ones, so
+    // delta = do . o carries the rounding of o to its type.  Where a row sees few
+    // keys, o is as large as a value and that error as large as the other ones, so
     // blocks with up to kAttnRows keys first sum delta = sum_j p dp from the
-    // scores; with more keys o averages out (error under a fifth of a
-    // rounding of ds) and a second pass over them would cost 2/3 of the first.
+    // scores.  With more keys and weights spread over them o averages out (error
+    // under a fifth of a rounding of ds), and a second pass over them would cost 2/3
+    // of the first.  Not so where one weight is near 1: then the row's ds are near 0
+    // and carry an error of up to 2^-8 |do . o| in bf16, small beside the gradients of
+    // other rows but not beside their own (600 keys, a weight of 0.98 on
+    // one key: dq and dk off by 5% of their norm, 0.3% in blocks of up to 128 keys).
     const int rounds = (steps + TEAMS - 1) / TEAMS;
     if (end <= kAttnRows) {
         float sum = 0.f;

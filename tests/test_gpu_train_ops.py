@@ -123,6 +123,26 @@ def test_attention_extreme_scores(dev):
     _check(8 * q, 8 * k, v, dout, [140], True)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention_with_one_dominating_score(dev, dtype):
+    # Small whole numbers, so every score is exact; each row has nearly all weight on
+    # one key, and the gradients of its scores almost vanish.  The bounds allow for
+    # the rounding of out in delta; where delta is summed from the scores (blocks
+    # of up to 128 keys) dq must do without: an error of 2 H (its operand's and its own
+    # rounding; the terms of a row's sum are few) of the norm.  fp32: what a weight
+    # lacks to 1 is 5e-3 or more, so u of out is at most some 1e-4 of the norm.
+    n, d = 600, 64
+    g = _gen(dev, 28)
+    k = torch.randint(-1, 2, (n, 1, d), generator=g, device=dev).to(dtype)
+    at = (torch.rand(n, generator=g, device=dev) * (torch.arange(n, device=dev) + 1)).long()
+    v, dout = (torch.randn(n, 1, d, generator=g, device=dev).to(dtype) for _ in range(2))
+    dq = _check(2 * k[at], k, v, dout, [n], True)[2]
+    want = attention_reference(2 * k[at], k, v, [n], True, 1 / math.sqrt(d), dout)[0]["dq"]
+    end = 128 if dtype == BF16 else n
+    off = np.linalg.norm(dq.double().cpu().numpy()[:end] - want[:end]) / np.linalg.norm(want[:end])
+    assert off <= (2 * H if dtype == BF16 else 1e-3)
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("fq,fk,fv,fdout", [(2.0 ** 50, 2.0 ** -50, 2.0 ** -60, 2.0 ** 30),
                                             (2.0 ** -45, 2.0 ** 45, 2.0 ** 60, 2.0 ** -70)])
