@@ -824,8 +824,7 @@ constexpr int query_waves(int ops) {
 // number of key heads is a multiple of 8; the plan's tiles, longest first,
 // slowest.
 __device__ __forceinline__ bool locate(const AttnArgs& a, const AttnTile& t, int within, int& row0) {
-    row0 = t.tile * kAttnRows + within;
-    return t.start >= 0 && t.len > 0 && t.tile >= 0 && row0 < t.len && (int64_t)t.start + t.len <= a.tokens;
+    return tile_row(t, a.tokens, within, row0);
 }
 
 // Forward: blocks of 32 WR queries of one head, TEAMS of waves that take the key

@@ -3,6 +3,8 @@
 // (np_train_api.cpp) and their kernels.  Not part of the public ABI.
 #pragma once
 
+#include "np_attn_tile.h"
+
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -11,13 +13,7 @@ namespace np {
 enum class DType { F32 = 0, BF16 = 1 };
 
 // ----------------------------------------------------------- attention ---
-// Rows of a block: queries in the forward and the dq pass, keys in the dk/dv
-// pass.  One entry of a plan covers that many rows of one sequence.
-constexpr int kAttnRows = 128;
 constexpr int kAttnMaxDim = 128;
-
-// {first token, length of the sequence, tile within it, 0}
-struct AttnTile { int32_t start, len, tile, zero; };
 
 // One [tokens, heads, dim] operand; strides in elements, dim contiguous.
 struct AttnOperand {
