@@ -28,15 +28,16 @@
 //
 // Measured (one MI355X, where a library product of 8192^3 reaches 1263 TFLOP/s in
 // bf16, 154 in fp32), causal, flops of the visible pairs:
-//   16384 tokens, 16/8 heads of 128, bf16: forward 1110-1130 us, 985 TFLOP/s
+//   16384 tokens, 16/8 heads of 128, bf16: forward 1095-1165 us from card to card,
+//     940-1000 TFLOP/s
 //   packed 16418 tokens (lengths 3 to 4096), same heads: forward 245 us (860),
 //     dq 343 us, dk/dv 480-500 us
 //   16 x 1024 tokens, 12 heads of 64, bf16: forward 45 us (570), dq 58, dk/dv 77
-//   4 x 1024 tokens, 12 heads of 64, fp32: forward 52-54 us (122), backward 194
-// Of the forward pass's cycles at heads of 128 the matrix instructions take 48%,
-// the vector instructions 57%, LDS reads 49%: two waves per SIMD overlap them in
-// part.  At heads of 64 the vector instructions (an exponential for every pair)
-// bound it: 65%, the matrix instructions 26%.  fp32 takes six
+//   4 x 1024 tokens, 12 heads of 64, fp32: forward 52-56 us (122), backward 195
+// Of the forward pass's cycles at heads of 128 the matrix instructions take 49%,
+// the vector instructions 58%, LDS reads 50%: two waves per SIMD overlap them in
+// part.  At heads of 64 the vector instructions (an exponential for every pair) take
+// 63%, the matrix instructions 28%, mostly one after the other.  fp32 takes six
 // products for one, which is still 1.3 to 1.9 times as fast as the fp32 instructions
 // (a sixteenth of the bf16 rate), us with those / with bf16 terms: 4 x 1024 tokens, 12
 // heads of 64, forward 76 / 53, backward 255 / 194; 2948 tokens, 16/8 heads of 128,
@@ -1352,6 +1353,10 @@ hipError_t run(const AttnArgs& a, bool backward, hipStream_t s) {
     //   bf16, 128: 256: 47.0 39.0 42.1, 512: 55.4 49.3 84.5, 768: 68.0 78.8 130
     //   fp32, 64, (4, 1) and (2, 2): 96: 62 44, 384: 66 54, 768: 86 99, 1536: 159 187
     //   fp32, 128: 128: 127 73, 256: 263 158, 512: 275 297, 1024: 402 593
+    // Rows that do not start on 16 bytes take (4, 1) whatever the batch, so that two
+    // more forms of each pass need not be built.  Forward us of aligned rows, of others
+    // and of others by the rule above: bf16 heads of 64, 1024 tokens of 12 heads 13 30
+    // 22, 4 x 1024 20 37 31; fp32 42 62 43, 57 67 55; bf16 128, 2 x 1024 of 16/8 24 47 41.
     const int64_t blocks = (int64_t)a.num_tiles * a.heads;
     constexpr bool small = sizeof(T) == 2;
     if (!VEC || blocks > (small ? 512 : 448)) query_pass<T, DP, VEC, 4, 1>(a, backward, s);

@@ -197,11 +197,11 @@ __global__ void __launch_bounds__(kThreads) act_grad_kernel(CkptGradArgs a, int6
 // operands.  fp32 dy is split into three bf16 terms (8 mantissa bits each,
 // by truncation, so the split is exact for magnitudes from 2^-100 up) and takes
 // three products, which is still 2.4 times the rate of the fp32 instructions.
-// Measured: 16384 x 2048 x 6144 bf16 411-425 us (970-1000 TFLOP/s; a library
-// product of bf16 operands reaches 1263 at 8192^3), 4001 x 768 x 2304 fp32 59 us
-// (240; 154 for a library's fp32 product), 53 of them in the products: 216 blocks
-// of 32 steps, whose conversions and LDS traffic the one block of a CU hides in
-// part (matrix instructions 35% of the cycles).
+// Measured: 16384 x 2048 x 6144 bf16 410-430 us from card to card (960-1005 TFLOP/s;
+// a library product of bf16 operands reaches 1263 at 8192^3), 4001 x 768 x 2304 fp32
+// 58-64 us (220-245; 154 for a library's fp32 product), 53 of them in the products:
+// 216 blocks of 32 steps, whose conversions and LDS traffic the one block of a CU
+// hides in part (matrix instructions 36% of the cycles).
 __device__ __forceinline__ void lds_barrier() {
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_barrier();
@@ -534,9 +534,9 @@ hipError_t launch_ckpt_act_grad(DType t, Act act, const CkptGradArgs& a, hipStre
 // more block of 128 x 128 on a CU, a whole step for each more of fp32; 4 for the
 // launch that joins the shares, and their bytes written and read at 3 TB/s.
 // Estimated and measured with 1, 2, 4, 8 shares: bf16 8192 x 768 x 2304 108 71 55 73
-// and 108 65 58 67, 2048^3 32 47 - - and 37 42 52 71, 600 x 2048 x 1024 14 25 - - and
-// 18 25 26 36; fp32 4001 x 768 x 2304 164 95 65 83 and 168 95 63 74, 2048^3 83 68 91 -
-// and 92 70 82 107.
+// and 118 73 64 74, 2048^3 32 47 - - and 41 43 55 76, 600 x 2048 x 1024 14 25 - - and
+// 19 27 27 38; fp32 4001 x 768 x 2304 164 95 65 83 and 164 93 64 75, 2048^3 83 68 91 -
+// and 94 70 83 110.
 int wgrad_splits(DType t, int64_t tokens, int64_t inner, int64_t outer) {
     if (t == DType::BF16 && wgrad_large(inner, outer)) return 1;
     const bool f32 = t == DType::F32;

@@ -48,7 +48,7 @@ hipError_t launch_attention_backward(DType t, const AttnArgs& a, hipStream_t s);
 constexpr int kCkptGroup = 64;          // features that share an exponent
 inline int64_t ckpt_pitch(int64_t cols) { return (cols + kCkptGroup - 1) / kCkptGroup * kCkptGroup; }
 
-struct CkptOut { int8_t* codes; int8_t* exps; };        // null codes: not wanted
+struct CkptOut { int8_t* codes; int8_t* exps; };
 struct CkptIn { const int8_t* codes; const int8_t* exps; };
 
 enum class Act { None = 0, Gelu = 1, Swiglu = 2 };
