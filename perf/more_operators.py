@@ -1,0 +1,462 @@
+"""More operators of a training step whose speed this repository is held to.
+
+They stand before and after packed attention and before the optimizer step:
+
+  rope          norms of the query and key heads and the rotation of their positions, one pass
+  rope_train    the same with its backward pass: q, k, dq, dk and the norms' weight gradients
+  window        causal attention over packed sequences with a sliding window and a few first
+                tokens that stay visible
+  window_train  the same with its backward pass: out, dq, dk, dv
+  clip          the norm of all gradients together, and the gradients scaled down to a limit
+
+A case is a dict of plain values:
+  kind      one of the above
+  dtype     "bf16" or "f32": the type of the activations, or of the gradients ("mixed": in turn)
+  lens      sequence lengths, "1024*4,77": length times how many          (all but clip)
+  heads, kv_heads, dim                                                    (all but clip)
+  fused     q, k and v are views of one projection's output               (all but clip)
+  norm      whether heads are normed (fp32 weights), or only rotated      (rope, rope_train)
+  rotated   features of a head that turn; the others stay                 (rope, rope_train)
+  axes      axes of a position; pair i of a head turns by axis i mod axes (rope, rope_train)
+  adjacent  pairs are (2i, 2i + 1), or (i, i + rotated / 2)               (rope, rope_train)
+  base      pair i turns by base^(-2i / rotated) a step                   (rope, rope_train)
+  far       position of a sequence's first token                          (rope, rope_train)
+  window, sinks   query i sees keys j <= i with j > i - window or j < sinks   (window, window_train)
+  shapes    "768x2304*12,768": shapes of the gradients, times how many    (clip)
+  out       "same" or "f32": the type of the scaled gradients             (clip)
+  rms       root mean square of the gradients; the limit of the norm is 1 (clip)
+
+  norm:      n_d = x_d w_d / sqrt(mean_d x_d^2 + 1e-6)
+  rotation:  (a, b) -> (a cos t - b sin t, a sin t + b cos t), t = position * frequency
+  clip:      norm = sqrt(sum g^2), g c with c = 1 where norm <= limit, else limit / norm
+
+Widths, head counts and head sizes are those of GPT-2 Small (768, 12 heads of 64), of the
+LLaMA-1B-shaped stack (32 heads over 8 of 64) and of Qwen3-1.7B (2048, 16 heads over 8 of 128,
+6144), as the optimizer's workloads have them, or generic ones.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+
+DEVICE = "cuda:0"
+DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+EPS = 1e-6
+LIMIT = 1.0
+
+
+# ------------------------------------------------------------------- cases ---
+def listed():
+    gpt2 = "768x2304*12,768x768*12,768x3072*12,3072x768*12,50257x768,1024x768,768*74,2304*12,3072*12"
+    qwen3 = "2048x2048*56,2048x1024*56,2048x6144*56,6144x2048*28"
+    return [
+        # A few short documents: what a call costs when there is hardly any work.
+        {"name": "rope-lines", "kind": "rope", "dtype": "bf16", "lens": "1,2,3,5,9,17,33,40,21,1", "heads": 12,
+         "kv_heads": 12, "dim": 64, "fused": True, "norm": True, "rotated": 64, "axes": 1, "adjacent": False,
+         "base": 10000.0, "far": 0},
+        # Frames of a video in fp32: positions of time, height and width, heads of 80, no norms.
+        {"name": "rope-video-f32", "kind": "rope", "dtype": "f32", "lens": "4096,333,2501", "heads": 16, "kv_heads": 16,
+         "dim": 80, "fused": True, "norm": False, "rotated": 80, "axes": 3, "adjacent": False, "base": 10000.0,
+         "far": 0},
+        # A small packed batch at far positions, half of every head turning, adjacent pairs.
+        {"name": "rope_train-odd", "kind": "rope_train", "dtype": "bf16", "lens": "129,1,301,64,77", "heads": 32,
+         "kv_heads": 8, "dim": 64, "fused": False, "norm": True, "rotated": 32, "axes": 1, "adjacent": True,
+         "base": 500000.0, "far": 1000003},
+        # A training micro-batch of 16384 tokens with the heads of the Qwen3 stack.
+        {"name": "rope_train-qwen3", "kind": "rope_train", "dtype": "bf16", "lens": "4096*3,2500,1596", "heads": 16,
+         "kv_heads": 8, "dim": 128, "fused": True, "norm": True, "rotated": 128, "axes": 1, "adjacent": False,
+         "base": 1000000.0, "far": 0},
+        # Short documents and a short window.
+        {"name": "window-lines", "kind": "window", "dtype": "bf16", "lens": "1,2,3,5,9,17,33,40,21,1", "heads": 12,
+         "kv_heads": 12, "dim": 64, "fused": True, "window": 16, "sinks": 2},
+        # One long document beside short ones, grouped heads.
+        {"name": "window-long", "kind": "window", "dtype": "bf16", "lens": "16384,515,64,1", "heads": 16, "kv_heads": 8,
+         "dim": 128, "fused": False, "window": 1024, "sinks": 4},
+        # A small packed batch with odd lengths and a window that no tile fits.
+        {"name": "window_train-odd", "kind": "window_train", "dtype": "bf16", "lens": "129,1,301,64,777", "heads": 32,
+         "kv_heads": 8, "dim": 64, "fused": False, "window": 100, "sinks": 1},
+        # The end-to-end model's default batch in fp32, a window of a quarter, no sinks.
+        {"name": "window_train-gpt2-f32", "kind": "window_train", "dtype": "f32", "lens": "1024*4", "heads": 12,
+         "kv_heads": 12, "dim": 64, "fused": True, "window": 256, "sinks": 0},
+        # A packed training micro-batch of long documents, grouped heads of 128.
+        {"name": "window_train-packed", "kind": "window_train", "dtype": "bf16", "lens": "8192,4096,2500,3,1011,130",
+         "heads": 16, "kv_heads": 8, "dim": 128, "fused": False, "window": 1024, "sinks": 4},
+        # A handful of small gradients of odd sizes and both types: what a call costs.
+        {"name": "clip-odd", "kind": "clip", "dtype": "mixed", "shapes": "1,77,333x65,129,1000x3,2049", "out": "same",
+         "rms": 0.02},
+        # Every gradient of GPT-2 Small in fp32.
+        {"name": "clip-gpt2-f32", "kind": "clip", "dtype": "f32", "shapes": gpt2, "out": "same", "rms": 0.001},
+        # The hidden matrices of the Qwen3 stack: gradients in bf16, scaled ones in fp32 for the optimizer step.
+        {"name": "clip-qwen3", "kind": "clip", "dtype": "bf16", "shapes": qwen3, "out": "f32", "rms": 0.001},
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _documents(rng, total):
+    parts = rng.randint(1, max(1, min(24, total // 8)))
+    cuts = sorted(rng.sample(range(1, total), parts - 1)) if parts > 1 else []
+    return [b - a for a, b in zip([0] + cuts, cuts + [total])]
+
+
+def draw(rng):
+    kind = rng.choice(["rope", "rope_train", "window", "window_train", "clip"])
+    c = {"kind": kind, "dtype": "bf16" if rng.random() < 0.7 else "f32"}
+    if kind == "clip":
+        if rng.random() < 0.3:
+            c["dtype"] = "mixed"
+        total, count = _log_int(rng, 1000, 2 ** 28), _log_int(rng, 1, 320)
+        shapes = []
+        for _ in range(count):
+            n = _log_int(rng, 1, max(1, 2 * total // count))
+            rows = _log_int(rng, 1, n)
+            shapes.append(f"{rows}x{n // rows}" if rng.random() < 0.7 else f"{n}")
+        return c | {"shapes": ",".join(shapes), "out": rng.choice(["same", "f32"]),
+                    "rms": math.exp(rng.uniform(math.log(1e-7), math.log(10.0)))}
+    heads, kv, dim = rng.choice([(12, 12, 64), (32, 8, 64), (16, 8, 128), (16, 8, 128), (16, 16, 80), (6, 2, 96),
+                                 (5, 1, 51)])
+    c |= {"heads": heads, "kv_heads": kv, "dim": dim, "fused": rng.random() < 0.5}
+    if kind in ("rope", "rope_train"):
+        lens = _documents(rng, _log_int(rng, 50, 16384 if c["dtype"] == "bf16" else 8192))
+        rotated = rng.choice([dim // 2 * 2, dim // 2 * 2, dim // 4 * 2, 2 * rng.randint(1, dim // 2)])
+        return c | {"lens": ",".join(str(n) for n in lens), "norm": rng.random() < 0.7, "rotated": rotated,
+                    "axes": rng.choice([1, 1, 2, 3]), "adjacent": rng.random() < 0.3,
+                    "base": rng.choice([10000.0, 500000.0, 1000000.0]),
+                    "far": rng.choice([0, 0, _log_int(rng, 1, 2 ** 24)])}
+    lens = _documents(rng, _log_int(rng, 100, 8192))
+    # The plain form pads every sequence to the longest: bound what it holds.
+    while len(lens) * max(lens) * heads > 16 * 16384:
+        i = lens.index(max(lens))
+        lens[i] = max(1, lens[i] // 2)
+    return c | {"lens": ",".join(str(n) for n in lens), "window": _log_int(rng, 1, 2048),
+                "sinks": rng.choice([0, 1, 4, _log_int(rng, 1, 300)])}
+
+
+def _times(text):
+    """("a", n) of each part of "a*n,b"."""
+    for part in text.split(","):
+        what, _, times = part.partition("*")
+        yield what, int(times) if times else 1
+
+
+def _lens(case):
+    return [int(n) for n, times in _times(case["lens"]) for _ in range(times)]
+
+
+def _shapes(case):
+    return [tuple(int(n) for n in s.split("x")) for s, times in _times(case["shapes"]) for _ in range(times)]
+
+
+def _grad_types(case):
+    n = len(_shapes(case))
+    if case["dtype"] == "mixed":
+        return [DTYPES["bf16" if i % 2 else "f32"] for i in range(n)]
+    return [DTYPES[case["dtype"]]] * n
+
+
+def _pairs(case):
+    """(frequency, axis) of every pair of a head."""
+    n = case["rotated"] // 2
+    return [case["base"] ** (-i / n) for i in range(n)], [i % case["axes"] for i in range(n)]
+
+
+# ------------------------------------------------------------------ inputs ---
+def _gen(seed):
+    g = torch.Generator(device=DEVICE)
+    g.manual_seed(int(seed))
+    return g
+
+
+def _randn(gen, dtype, *shape):
+    return torch.randn(*shape, generator=gen, device=DEVICE, dtype=torch.float32).to(dtype)
+
+
+def _positions(case, lens):
+    """int32 [axes, tokens]: places in the sequence, or those of a grid of 16 columns (and 16 rows a frame)."""
+    at = torch.cat([torch.arange(n) for n in lens])
+    grid = {1: [at], 2: [at // 16, at % 16], 3: [at // 256, at // 16 % 16, at % 16]}[case["axes"]]
+    return (torch.stack(grid) + case["far"]).to(torch.int32).to(DEVICE)
+
+
+def prepare(case, seed):
+    gen, kind = _gen(seed), case["kind"]
+    s = {"case": case}
+    if kind == "clip":
+        shapes, types = _shapes(case), _grad_types(case)
+        s["grads"] = [_randn(gen, torch.float32, *shape).mul_(case["rms"]).to(dt) for shape, dt in zip(shapes, types)]
+        # The scaled gradients of a type side by side, as a program keeps them that hands them on to an optimizer.
+        outs = [torch.float32 if case["out"] == "f32" else dt for dt in types]
+        sizes = [g.numel() for g in s["grads"]]
+        s["flat"] = {dt: torch.empty(sum(n for n, d in zip(sizes, outs) if d == dt), device=DEVICE, dtype=dt)
+                     for dt in dict.fromkeys(outs)}
+        at, s["out"] = dict.fromkeys(s["flat"], 0), []
+        for shape, n, dt in zip(shapes, sizes, outs):
+            s["out"].append(s["flat"][dt][at[dt]:at[dt] + n].view(shape))
+            at[dt] += n
+        return s
+    dt, lens, hq, hk, d = DTYPES[case["dtype"]], _lens(case), case["heads"], case["kv_heads"], case["dim"]
+    t = sum(lens)
+    if case["fused"]:
+        qkv = _randn(gen, dt, t, (hq + 2 * hk) * d)
+        s["q"], s["k"], s["v"] = (x.unflatten(1, (-1, d)) for x in qkv.split([hq * d, hk * d, hk * d], dim=1))
+    else:
+        s["q"], s["k"], s["v"] = (_randn(gen, dt, t, h, d) for h in (hq, hk, hk))
+    if kind in ("rope", "rope_train"):
+        s["positions"] = _positions(case, lens)
+        s["wq"], s["wk"] = (1.0 + 0.2 * _randn(gen, torch.float32, d) if case["norm"] else None for _ in range(2))
+        if kind == "rope_train":
+            s["dq"], s["dk"] = (_randn(gen, dt, t, h, d) for h in (hq, hk))
+        freqs, axes = _pairs(case)
+        if own:
+            from paper_2609_36692_amd import train_ops
+            s["rotary"] = train_ops.Rotary(freqs, axes=axes, adjacent=case["adjacent"], device=DEVICE)
+        else:
+            s["freqs"] = torch.tensor(freqs, dtype=torch.float64, device=DEVICE)
+            s["axis"] = torch.tensor(axes, device=DEVICE)
+        return s
+    if kind == "window_train":
+        s["dout"] = _randn(gen, dt, t, hq, d)
+    # Kept for every layer of a step: which token each place of the padded batch holds (plain form),
+    # the plan of the packed batch (the framework's kernels).
+    if own:
+        from paper_2609_36692_amd import train_ops
+        s["plan"] = train_ops.AttentionPlan(lens, device=DEVICE, window=case["window"], sinks=case["sinks"])
+    else:
+        n = torch.tensor(lens, device=DEVICE)
+        at = torch.arange(max(lens), device=DEVICE)
+        s["valid"] = at[None, :] < n[:, None]
+        s["place"] = torch.where(s["valid"], (n.cumsum(0) - n)[:, None] + at[None, :], 0)
+    return s
+
+
+# ------------------------------------------------------------- plain forms ---
+def _angles(s):
+    """(cos, sin) [tokens, 1, pairs]: the angle in 64 bits, since far positions turn many times."""
+    t = s["positions"].double()[s["axis"]].t() * s["freqs"]
+    return torch.cos(t).float()[:, None], torch.sin(t).float()[:, None]
+
+
+def _halves(case, x):
+    """The two members of every pair of x [tokens, heads, dim] that turns, as views."""
+    r = case["rotated"]
+    return (x[..., 0:r:2], x[..., 1:r:2]) if case["adjacent"] else (x[..., :r // 2], x[..., r // 2:r])
+
+
+def _turn(case, x, cos, sin):
+    y = x.clone()
+    (a, b), (ya, yb) = _halves(case, x), _halves(case, y)
+    ya.copy_(a * cos - b * sin)
+    yb.copy_(a * sin + b * cos)
+    return y
+
+
+def _plain_rope(s, train):
+    case, dt = s["case"], s["q"].dtype
+    cos, sin = _angles(s)
+    out = {}
+    for n in "qk":
+        x, w = s[n].float(), s["w" + n]
+        if w is not None:
+            r = torch.rsqrt(x.square().mean(2, keepdim=True) + EPS)
+            x = x * r
+        out[n] = _turn(case, x if w is None else x * w, cos, sin).to(dt)
+        if not train:
+            continue
+        g = _turn(case, s["d" + n].float(), cos, -sin)
+        if w is not None:
+            out["dw" + n] = (g * x).sum((0, 1))
+            g = g * w
+            g = (g - x * (g * x).mean(2, keepdim=True)) * r
+        out["d" + n] = g.to(dt)
+    return out
+
+
+def _plain_window(s, train):
+    """Over sequences padded to the longest, a block of queries at a time: with the keys of its
+    windows and the first ones."""
+    case, dt = s["case"], s["q"].dtype
+    g, c, w, sinks = case["heads"] // case["kv_heads"], 1.0 / math.sqrt(case["dim"]), case["window"], case["sinks"]
+    place, valid = s["place"], s["valid"]
+    n = place.shape[1]
+
+    def padded(x, times=1):                            # [sequences, heads, longest, dim]
+        return x.float().repeat_interleave(times, dim=1)[place].transpose(1, 2).contiguous()
+
+    def packed(x):
+        return x.transpose(1, 2)[valid]
+
+    q, k, v = padded(s["q"]), padded(s["k"], g), padded(s["v"], g)
+    out = torch.empty_like(q)
+    if train:
+        do = padded(s["dout"]).mul_(valid[:, None, :, None])
+        dq, dk, dv = torch.empty_like(q), torch.zeros_like(k), torch.zeros_like(v)
+    place_in = torch.arange(n, device=DEVICE)
+    step = max(w, 256)
+    for a in range(0, n, step):
+        b, lo = min(n, a + step), max(0, a - w + 1)
+        keys = torch.cat([place_in[:min(sinks, lo)], place_in[lo:b]])
+        i, j = place_in[a:b, None], keys[None, :]
+        seen = ((j <= i) & ((j > i - w) | (j < sinks)))[None, None] & valid[:, None, None, keys]
+        qs, ks, vs = q[:, :, a:b], k[:, :, keys], v[:, :, keys]
+        p = torch.matmul(qs, ks.transpose(2, 3)).mul_(c).masked_fill_(~seen, -math.inf)
+        p.sub_(p.amax(3, keepdim=True).clamp_(min=-1e30)).exp_()      # rows of the padding see nothing
+        p.div_(p.sum(3, keepdim=True).clamp_(min=1e-30))
+        out[:, :, a:b] = torch.matmul(p, vs)
+        if train:
+            dos = do[:, :, a:b]
+            ds = torch.matmul(dos, vs.transpose(2, 3))
+            ds.sub_((p * ds).sum(3, keepdim=True)).mul_(p).mul_(c)
+            dq[:, :, a:b] = torch.matmul(ds, ks)
+            dk.index_add_(2, keys, torch.matmul(ds.transpose(2, 3), qs))
+            dv.index_add_(2, keys, torch.matmul(p.transpose(2, 3), dos))
+    res = {"out": packed(out).to(dt)}
+    if train:
+        dk, dv = (packed(x).unflatten(1, (-1, g)).sum(2) for x in (dk, dv))
+        res |= {"dq": packed(dq).to(dt), "dk": dk.to(dt), "dv": dv.to(dt)}
+    return res
+
+
+def _plain_clip(s):
+    total = torch.stack([g.float().square().sum(dtype=torch.float64) for g in s["grads"]]).sum().sqrt()
+    c = torch.where(total <= LIMIT, 1.0, LIMIT / total).float()
+    for g, o in zip(s["grads"], s["out"]):
+        o.copy_(g.float() * c)
+    return {"norm": total.float()} | {str(dt): x for dt, x in s["flat"].items()}
+
+
+# --------------------------------------------------------------------- run ---
+def _own_run(s):
+    from paper_2609_36692_amd import train_ops as T
+    kind = s["case"]["kind"]
+    if kind == "clip":
+        norm = T.clip_grads(s["grads"], LIMIT, out=s["out"])
+        return {"norm": norm} | {str(dt): x for dt, x in s["flat"].items()}
+    if kind in ("window", "window_train"):
+        out, lse = T.attention_forward(s["q"], s["k"], s["v"], s["plan"])
+        if kind == "window":
+            return {"out": out}
+        dq, dk, dv = T.attention_backward(s["dout"], s["q"], s["k"], s["v"], out, lse, s["plan"])
+        return {"out": out, "dq": dq, "dk": dk, "dv": dv}
+    args = {"norm": s["case"]["norm"], "q_weight": s["wq"], "k_weight": s["wk"], "eps": EPS}
+    q, k = T.qk_norm_rope_forward(s["q"], s["k"], s["positions"], s["rotary"], **args)
+    if kind == "rope":
+        return {"q": q, "k": k}
+    dq, dk, dwq, dwk = T.qk_norm_rope_backward(s["dq"], s["dk"], s["q"], s["k"], s["positions"], s["rotary"], **args)
+    return {"q": q, "k": k, "dq": dq, "dk": dk} | ({"dwq": dwq, "dwk": dwk} if s["case"]["norm"] else {})
+
+
+def run(state):
+    if own:
+        return _own_run(state)
+    kind = state["case"]["kind"]
+    if kind == "clip":
+        return _plain_clip(state)
+    return (_plain_rope if kind in ("rope", "rope_train") else _plain_window)(state, kind.endswith("_train"))
+
+
+# -------------------------------------------------------------------- work ---
+def _visible(n, w, sinks):
+    """Pairs that a sequence of n tokens has: for query i, min(i + 1, window) keys and the first ones before them."""
+    m = min(n, w)
+    pairs = m * (m + 1) // 2 + (n - m) * w
+    e = min(sinks, max(0, n - w))                        # before the windows of the queries from w on: 1, 2, .. keys
+    return pairs + e * (e + 1) // 2 + (max(0, n - w) - e) * e
+
+
+def work(case):
+    kind = case["kind"]
+    if kind == "clip":
+        b = [2 if dt == torch.bfloat16 else 4 for dt in _grad_types(case)]
+        n = [math.prod(shape) for shape in _shapes(case)]
+        return {"bytes": sum(x * (y + (4 if case["out"] == "f32" else y)) for x, y in zip(n, b)), "flops": 3 * sum(n)}
+    lens, hq, hk, d, b = _lens(case), case["heads"], case["kv_heads"], case["dim"], 2 if case["dtype"] == "bf16" else 4
+    t = sum(lens)
+    if kind in ("rope", "rope_train"):
+        n = t * (hq + hk) * d
+        one = 2 * n * b + 4 * t * case["axes"]
+        # dq and dk are read too, and the gradients of q and k are written.
+        return {"bytes": one, "flops": 8 * n} if kind == "rope" else {"bytes": one + 2 * n * b, "flops": 22 * n}
+    pairs = sum(_visible(n, case["window"], case["sinks"]) for n in lens)
+    one = t * (2 * hq + 2 * hk) * d * b                  # q, k, v, out
+    if kind == "window":
+        return {"bytes": one, "flops": 4 * d * hq * pairs}
+    return {"bytes": one + t * (2 * hq + 2 * hk) * d * b, "flops": 14 * d * hq * pairs}
+
+
+# ------------------------------------------------------------------- exact ---
+def _exact_rope(case, s):
+    """By complex numbers, the backward pass by automatic differentiation in 64 bits."""
+    freqs, axes = _pairs(case)
+    r, m = case["rotated"], case["rotated"] // 2
+    pos = s["positions"].double()
+    t = torch.stack([pos[a] * f for f, a in zip(freqs, axes)], dim=1)
+    turn = torch.polar(torch.ones_like(t), t)[:, None]
+    first = torch.arange(0, r, 2) if case["adjacent"] else torch.arange(m)
+    second = first + (1 if case["adjacent"] else m)
+    order = torch.cat([first, second, torch.arange(r, case["dim"])]).argsort().to(DEVICE)
+    first, second = first.to(DEVICE), second.to(DEVICE)
+    res = {}
+    for n in "qk":
+        x = s[n].double().requires_grad_()
+        w = None if s["w" + n] is None else s["w" + n].double().requires_grad_()
+        y = x if w is None else x / torch.sqrt((x * x).sum(2, keepdim=True) / case["dim"] + EPS) * w
+        z = torch.complex(y[..., first], y[..., second]) * turn
+        y = torch.cat([z.real, z.imag, y[..., r:]], dim=2)[..., order]
+        res[n] = y.detach()
+        if case["kind"] == "rope_train":
+            grads = torch.autograd.grad(y, [x] if w is None else [x, w], s["d" + n].double())
+            res |= dict(zip(["d" + n, "dw" + n], grads))
+    return res
+
+
+def _exact_window(case, s):
+    hq, d, w, sinks = case["heads"], case["dim"], case["window"], case["sinks"]
+    g, train = hq // case["kv_heads"], case["kind"] == "window_train"
+    q, k, v = (s[x].double() for x in "qkv")
+    res = {"out": torch.empty_like(q)}
+    if train:
+        do = s["dout"].double()
+        res |= {"dq": torch.empty_like(q), "dk": torch.zeros_like(k), "dv": torch.zeros_like(v)}
+    start = 0
+    for n in _lens(case):
+        for a in range(0, n, 2048):
+            i = torch.arange(a, min(n, a + 2048), device=DEVICE)
+            gap = i[:, None] - torch.arange(n, device=DEVICE)[None]
+            hidden = (gap < 0) | ((gap >= w) & (torch.arange(n, device=DEVICE) >= sinks)[None])
+            cols = (~hidden).any(0).nonzero()[:, 0]
+            hidden, rows, cols = hidden[:, cols], start + i, start + cols
+            for h in range(hq):
+                qi, ki, vi = q[rows, h], k[cols, h // g], v[cols, h // g]
+                p = torch.softmax((qi @ ki.T / math.sqrt(d)).masked_fill_(hidden, -math.inf), dim=1)
+                o = p @ vi
+                res["out"][rows, h] = o
+                if train:
+                    doi = do[rows, h]
+                    dp = p * (doi @ vi.T - (doi * o).sum(1, keepdim=True)) / math.sqrt(d)
+                    res["dq"][rows, h] = dp @ ki
+                    res["dk"][cols, h // g] += dp.T @ qi
+                    res["dv"][cols, h // g] += p.T @ doi
+        start += n
+    return res
+
+
+def _exact_clip(case, s):
+    total = math.sqrt(math.fsum(float(torch.linalg.vector_norm(g, dtype=torch.float64)) ** 2 for g in s["grads"]))
+    c = min(1.0, LIMIT / total) if total > 0 else 1.0
+    res = {}
+    for dt in s["flat"]:
+        parts = [g.double().flatten() * c for g, o in zip(s["grads"], s["out"]) if o.dtype == dt]
+        res[str(dt)] = torch.cat(parts)
+    return {"norm": total} | res
+
+
+def exact(case, seed):
+    s, kind = prepare(case, seed), case["kind"]
+    if kind == "clip":
+        return _exact_clip(case, s)
+    return (_exact_rope if kind in ("rope", "rope_train") else _exact_window)(case, s)
