@@ -602,6 +602,39 @@ int normpre_checkpoint_weight_grad(int dtype, int layout, int accumulate, int64_
                                    const void* dy, int64_t ld_dy, float* dw, int64_t ld_dw,
                                    void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---- gradient norm and clipping ------------------------------------------ */
+/*
+ * The norm of all gradients together, and the gradients scaled down to a limit,
+ * before normpre_step() takes them; contexts, streams, threads and results as for
+ * the operators above.
+ *   grad_norm:  *norm = n = sqrt(sum g^2) over the elements of all gradients
+ *   grad_clip:  the same, and out = c g with c = 1 where n <= max_norm, else
+ *               max_norm / n; a NaN among the gradients makes all outputs NaN, an
+ *               infinity makes them 0 (itself NaN)
+ * Squares are summed in 64 bits; *norm (device fp32) is rounded once.  out may be
+ * grad itself (of one type); gradients in place are not written where c is 1.
+ * Gradients of either type may stand in one list, and out may be of the other
+ * type.  grad_norm ignores out and out_dtype, and may be given a tensor twice.
+ * num_grads = 0, and gradients of no elements: a norm of 0.
+ * workspace: NORMPRE_GRAD_WORKSPACE_BYTES, 16-byte aligned.
+ * Errors: INVALID_ARG (null or misaligned pointers, unknown dtype, negative
+ * sizes, max_norm negative or NaN, too small a workspace; grad_clip: outputs that
+ * overlap each other or a gradient that is not scaled in place), UNSUPPORTED (more
+ * than 2^20 gradients or 2^40 elements), OOM, HIP.
+ */
+#define NORMPRE_GRAD_WORKSPACE_BYTES 65600
+typedef struct normpre_grad {
+    const void* grad;           /* dense                                         */
+    void*   out;                /* in the order of grad's elements in memory     */
+    int64_t count;              /* elements                                      */
+    int32_t dtype;              /* NORMPRE_DTYPE_*, of grad                      */
+    int32_t out_dtype;          /* and of out                                    */
+} normpre_grad;
+int normpre_grad_norm(int64_t num_grads, const normpre_grad* grads, float* norm, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+int normpre_grad_clip(int64_t num_grads, const normpre_grad* grads, double max_norm, float* norm, void* workspace,
+                      int64_t workspace_bytes, void* stream);
+
 /* Library version string (static storage). */
 const char* normpre_version(void);
 

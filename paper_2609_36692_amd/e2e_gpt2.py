@@ -7,7 +7,8 @@ dataset: uniform random token ids), forward + backward + optimizer step.  The
 The optimizer step is timed between device synchronizations, as in the
 paper's efficiency tables (Sec. 4.2); the model runs in fp32.
 
-Prints one JSON line: fwd+bwd and optimizer milliseconds per step, the
+Prints one JSON line: fwd+bwd and optimizer milliseconds per step (with
+``--clip`` the optimizer's include the clipping of the gradients), the
 optimizer's share of the step, tokens/s, and the descent alignment of the
 last step (App. A.3: mean over the hidden matrices of the cosine between the
 gradient and the update direction, weight decay excluded).
@@ -113,7 +114,7 @@ def document_lengths(total, count, longest, gen):
     return [b - a for a, b in zip([0] + ends[:-1], ends)]
 
 
-def make_optimizer(name, model, lr, wd):
+def make_optimizer(name, model, lr, wd, clip=None):
     hidden = [p for n, p in model.named_parameters() if n.endswith(HIDDEN_SUFFIXES)]
     hidden_ids = {id(p) for p in hidden}
     others = [p for p in model.parameters() if id(p) not in hidden_ids]
@@ -123,7 +124,7 @@ def make_optimizer(name, model, lr, wd):
     variant = {"normpre-g": "G", "normpre-l": "L", "muon": "MUON", "normalize-only": "NORM"}[name]
     groups = [{"params": hidden, "normpre": True, "lr": lr, "weight_decay": wd},
               {"params": others, "normpre": False, "lr": lr, "weight_decay": wd}]
-    return NormPreOptimizer(groups, lr=lr, variant=variant, weight_decay=wd), hidden
+    return NormPreOptimizer(groups, lr=lr, variant=variant, weight_decay=wd, max_grad_norm=clip), hidden
 
 
 def main(argv=None):
@@ -136,10 +137,13 @@ def main(argv=None):
     ap.add_argument("--warmup", type=int, default=3)
     ap.add_argument("--lr", type=float, default=6e-4)
     ap.add_argument("--weight-decay", type=float, default=0.1)
+    ap.add_argument("--clip", type=float, help="largest norm of the gradients (not with adamw)")
     ap.add_argument("--train-ops", action="store_true", help="blocks on the operators of train_ops, packed documents")
     ap.add_argument("--documents", type=int, help="documents of a packed batch (default: the batch size)")
     ap.add_argument("--dtype", default="fp32", choices=["fp32", "bf16"], help="activations, with --train-ops")
     a = ap.parse_args(argv)
+    if a.clip is not None and a.optimizer == "adamw":
+        ap.error("--clip is the NormPre optimizers'")
     if not torch.cuda.is_available():
         raise SystemExit("needs a GPU")
     dev = torch.device("cuda:0")
@@ -152,7 +156,7 @@ def main(argv=None):
         host_gen.manual_seed(1337)
     elif a.documents is not None or dtype != torch.float32:
         ap.error("--documents and --dtype need --train-ops")
-    opt, hidden = make_optimizer(a.optimizer, model, a.lr, a.weight_decay)
+    opt, hidden = make_optimizer(a.optimizer, model, a.lr, a.weight_decay, a.clip)
     gen = torch.Generator(device=dev)
     gen.manual_seed(1337)
     fb_ms, op_ms = [], []
@@ -203,6 +207,7 @@ def main(argv=None):
            "optimizer_share": round(op / (fb + op), 4),
            "tokens_per_s": round(a.batch * a.seq / ((fb + op) / 1e3), 1),
            "descent_alignment_last_step": None if align is None else round(align, 4),
+           **({"grad_norm_last_step": round(float(opt.grad_norm), 4)} if a.clip is not None else {}),
            **({"peak_memory_gib": round(torch.cuda.max_memory_allocated() / 2 ** 30, 2)} if a.train_ops else {}),
            "final_loss": round(float(loss.detach()), 4)}
     print(json.dumps(out), flush=True)

@@ -76,6 +76,7 @@ NORMPRE_ACT_GELU = 1
 NORMPRE_ACT_SWIGLU = 2
 NORMPRE_WEIGHT_INNER_OUTER = 0
 NORMPRE_WEIGHT_OUTER_INNER = 1
+NORMPRE_GRAD_WORKSPACE_BYTES = 65600
 
 
 class NormPreError(RuntimeError):
@@ -127,6 +128,11 @@ class normpre_attention(ctypes.Structure):
         ("workspace", ctypes.c_void_p),
         ("workspace_bytes", ctypes.c_int64),
     ]
+
+
+class normpre_grad(ctypes.Structure):
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -191,6 +197,8 @@ def load_library(path: str = LIB_PATH):
         "normpre_checkpoint_weight_grad": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64,
                                                           ctypes.c_int64, ctypes.c_int64, P, P, P, ctypes.c_int64,
                                                           P, ctypes.c_int64, P, ctypes.c_int64, P]),
+        "normpre_grad_norm": (ctypes.c_int, [ctypes.c_int64, P, P, P, ctypes.c_int64, P]),
+        "normpre_grad_clip": (ctypes.c_int, [ctypes.c_int64, P, ctypes.c_double, P, P, ctypes.c_int64, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -476,6 +484,20 @@ def normpre_checkpoint_weight_grad(dtype: int, layout: int, accumulate: bool, to
     code = load_library().normpre_checkpoint_weight_grad(dtype, layout, int(bool(accumulate)), tokens, inner, outer,
                                                          codes, exps, dy, ld_dy, dw, ld_dw, workspace,
                                                          workspace_bytes, _stream_handle(stream))
+    if code:
+        _check(code)
+
+
+def normpre_grad_norm(num_grads: int, grads, norm, workspace, workspace_bytes, stream=None) -> None:
+    """grads: the address of num_grads ``normpre_grad``."""
+    code = load_library().normpre_grad_norm(num_grads, grads, norm, workspace, workspace_bytes, _stream_handle(stream))
+    if code:
+        _check(code)
+
+
+def normpre_grad_clip(num_grads: int, grads, max_norm: float, norm, workspace, workspace_bytes, stream=None) -> None:
+    code = load_library().normpre_grad_clip(num_grads, grads, max_norm, norm, workspace, workspace_bytes,
+                                            _stream_handle(stream))
     if code:
         _check(code)
 

@@ -17,6 +17,7 @@ from __future__ import annotations
 import torch
 
 from . import normpre as N
+from .train_ops import clip_grads
 
 
 class NormPreOptimizer(torch.optim.Optimizer):
@@ -33,13 +34,16 @@ class NormPreOptimizer(torch.optim.Optimizer):
             "MUON" / "NORM" of the library.
         adamw_lr, adamw_betas, adamw_eps: AdamW for the other parameters
             (App. A.1 uses betas (0.9, 0.95) and the model's learning rate).
+        max_grad_norm: gradients of all groups together are first scaled down
+            to this norm, in place (``train_ops.clip_grads``: bf16 and fp32 on one
+            GPU); their norm before that is then ``grad_norm``, a tensor.
         Other keyword arguments are NormPre hyper-parameters (momentum,
         weight_decay, rank, oversample, power_iters, ns_iters, seed, flags...).
     """
 
     def __init__(self, params, lr: float = 6e-4, variant: str = "G", weight_decay: float = 0.1,
                  adamw_lr: float | None = None, adamw_betas=(0.9, 0.95), adamw_eps: float = 1e-8,
-                 matrix_filter=None, **hparams):
+                 matrix_filter=None, max_grad_norm: float | None = None, **hparams):
         params = list(params)
         if params and not isinstance(params[0], dict):
             keep = matrix_filter or (lambda p: p.dim() == 2)
@@ -55,6 +59,9 @@ class NormPreOptimizer(torch.optim.Optimizer):
         self.variant = variant.upper()
         self.hparams = dict(hparams)
         self.t = int(self.hparams.pop("step", 0))
+        if max_grad_norm is not None and not max_grad_norm >= 0:
+            raise ValueError(f"max_grad_norm is {max_grad_norm}")
+        self.max_grad_norm, self.grad_norm = max_grad_norm, None
         adam_groups = []
         for g in self.param_groups:
             if g["normpre"]:
@@ -79,6 +86,9 @@ class NormPreOptimizer(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        if self.max_grad_norm is not None:
+            self.grad_norm = clip_grads([p.grad for g in self.param_groups for p in g["params"] if p.grad is not None],
+                                        self.max_grad_norm)
         for g in self.param_groups:
             if not g["normpre"]:
                 continue

@@ -8,7 +8,9 @@ Between a model's loss and the gradients of its hidden matrices:
   ``checkpoint_act`` (an MLP's activation and the checkpoints its backward pass
   needs, in one pass), ``checkpoint_act_grad`` and ``checkpoint_weight_grad``
   (the gradients that read them), and the layers made of them:
-  ``checkpointed_linear`` and ``checkpointed_mlp``.
+  ``checkpointed_linear`` and ``checkpointed_mlp``;
+* ``grad_norm`` and ``clip_grads``: the norm of all gradients together, and the
+  gradients scaled down to a limit, for the optimizer step.
 
 Every operator runs in the gfx950 kernels of libnormpre.so on the current
 stream of its tensors' device, in bf16 or fp32; there is no fallback.  The
@@ -21,7 +23,8 @@ from __future__ import annotations
 import ctypes
 import math
 import struct
-from typing import NamedTuple, Sequence
+from array import array
+from typing import Iterable, NamedTuple, Sequence
 
 import torch
 
@@ -445,3 +448,93 @@ def checkpointed_mlp(x: torch.Tensor, w_in: torch.Tensor, w_out: torch.Tensor, *
     _check_layer(x, layout)
     with torch.autocast("cuda", enabled=False):
         return _Mlp.apply(x, act, layout, w_in, b_in, w_up, w_out, b_out, _trained(w_in, w_up))
+
+
+# ------------------------------------------------------------- gradients ---
+def _dense(x: torch.Tensor) -> bool:
+    """Whether x's elements fill a piece of memory, each place once."""
+    if x.is_contiguous():
+        return True
+    expected = 1
+    for stride, size in sorted((st, n) for st, n in zip(x.stride(), x.shape) if n != 1):
+        if stride != expected:
+            return False
+        expected *= size
+    return True
+
+
+def _grad_list(grads: Iterable[torch.Tensor]) -> list[torch.Tensor]:
+    return [grads] if isinstance(grads, torch.Tensor) else list(grads)
+
+
+def _grad_entries(grads, outs) -> tuple[int, array]:
+    """(device index, the C ABI's list of gradients)."""
+    if not grads[0].is_cuda:
+        raise ValueError("expected tensors on a GPU")
+    at, block = grads[0].get_device(), array("Q")
+    for g, o in zip(grads, outs):
+        if g.get_device() != at or o.get_device() != at:
+            raise ValueError(f"gradients lie on different devices: {g.device}, {o.device} and cuda:{at}")
+        block.extend((g.data_ptr(), o.data_ptr(), g.numel(), _dtype(g) | _dtype(o) << 32))
+    return at, block
+
+
+def _grad_workspace(like: torch.Tensor):
+    return like.new_empty((), dtype=torch.float32), like.new_empty(N.NORMPRE_GRAD_WORKSPACE_BYTES, dtype=torch.uint8)
+
+
+def grad_norm(grads: Iterable[torch.Tensor] | torch.Tensor) -> torch.Tensor:
+    """The 2-norm of all gradients together, as an fp32 tensor of no dimensions on
+    their device (0 on the CPU for an empty list); does not wait for the GPU.
+    Gradients in bf16 and fp32, mixed or not, of any strides (those that do not
+    fill a piece of memory are copied)."""
+    grads = [g if _dense(g) else g.contiguous() for g in _grad_list(grads)]
+    if not grads:
+        return torch.zeros(())
+    at, block = _grad_entries(grads, grads)
+    if _elsewhere(at):
+        with torch.cuda.device(at):
+            return grad_norm(grads)
+    norm, work = _grad_workspace(grads[0])
+    N.normpre_grad_norm(len(grads), block.buffer_info()[0], norm.data_ptr(), work.data_ptr(), work.numel(), _stream(at))
+    return norm
+
+
+def clip_grads(grads: Iterable[torch.Tensor] | torch.Tensor, max_norm: float,
+               out: Iterable[torch.Tensor] | torch.Tensor | None = None) -> torch.Tensor:
+    """Scales the gradients by max_norm / norm where their norm (``grad_norm``, which
+    is returned) exceeds max_norm: in place, or into ``out``, tensors of the same
+    shapes, bf16 or fp32, which are written in any case (bf16 gradients for an
+    optimizer that takes fp32 ones).  Does not wait for the GPU.  NaN or infinite
+    gradients follow the formula: a norm of NaN makes every gradient NaN, an
+    infinite one 0 or, where it was infinite, NaN."""
+    grads = _grad_list(grads)
+    if not max_norm >= 0:
+        raise ValueError(f"max_norm is {max_norm}")
+    outs = grads if out is None else _grad_list(out)
+    if len(outs) != len(grads) or any(o.shape != g.shape for g, o in zip(grads, outs)):
+        raise ValueError("out has the gradients' number and shapes")
+    if not grads:
+        return torch.zeros(())
+    sources, targets, back = [], [], []
+    for g, o in zip(grads, outs):
+        if not _dense(o) and any(st == 0 and n > 1 for st, n in zip(o.stride(), o.shape)):
+            raise ValueError("an output's elements share memory")
+        if _dense(g) and (g.stride() == o.stride() or (g.is_contiguous() and o.is_contiguous())):
+            sources.append(g)
+            targets.append(o)
+            continue
+        sources.append(g.contiguous())
+        targets.append(o if o.is_contiguous() else torch.empty_like(o, memory_format=torch.contiguous_format))
+        if not o.is_contiguous():
+            back.append((o, targets[-1]))
+    at, block = _grad_entries(sources, targets)
+    if _elsewhere(at):
+        with torch.cuda.device(at):
+            return clip_grads(grads, max_norm, out)
+    norm, work = _grad_workspace(grads[0])
+    N.normpre_grad_clip(len(grads), block.buffer_info()[0], float(max_norm), norm.data_ptr(), work.data_ptr(),
+                        work.numel(), _stream(at))
+    for o, t in back:
+        o.copy_(t)
+    return norm

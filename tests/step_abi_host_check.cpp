@@ -1,0 +1,118 @@
+// Driver for the sanitized build of the gradient operators' host code
+// (tests/test_step_abi_sanitized.py): the lists that launches get, and refusals,
+// with launchers that only look at what they are given.
+#include "../include/normpre.h"
+#include "../paper_2609_36692_amd/csrc/np_grads.h"
+
+#include <cstdio>
+#include <limits>
+#include <string>
+#include <vector>
+
+static int g_failures = 0;
+static std::string g_error;
+
+#define EXPECT(got, want)                                                                              \
+    do {                                                                                               \
+        const long long g_ = (long long)(got), w_ = (long long)(want);                                 \
+        if (g_ != w_) {                                                                                \
+            std::printf("line %d: %s is %lld, expected %lld (%s)\n", __LINE__, #got, g_, w_, g_error.c_str()); \
+            ++g_failures;                                                                              \
+        }                                                                                              \
+    } while (0)
+
+// What the launches of a call covered.
+static long long g_squares, g_scaled, g_partials, g_total_of, g_launches;
+static double* g_work;
+
+namespace np {
+int set_thread_error(int code, const char* msg) { g_error = msg; return code; }
+
+static long long elements(const GradList& l, int blocks) {
+    EXPECT(l.count >= 1 && l.count <= kGradList, 1);
+    EXPECT(l.first[0], 0);
+    long long n = 0;
+    for (int i = 0; i < l.count; ++i) {
+        const uint32_t size = l.size[i] & (kGradInBf16 - 1);
+        EXPECT(size >= 1 && size <= kGradMost, 1);
+        EXPECT(l.first[i + 1] - l.first[i], (size + kGradChunk - 1) / kGradChunk);
+        n += size;
+    }
+    EXPECT(blocks >= 1 && blocks <= kGradBlocks && (uint32_t)blocks <= l.first[l.count], 1);
+    ++g_launches;
+    return n;
+}
+hipError_t launch_grad_squares(const GradList& l, int blocks, double* partial, hipStream_t) {
+    g_squares += elements(l, blocks);
+    EXPECT(partial - g_work, kGradHead + g_partials);    // one block's behind the other's
+    g_partials += blocks;
+    EXPECT(g_partials <= kGradPartials, 1);
+    return hipSuccess;
+}
+hipError_t launch_grad_total(double* work, int partials, double, float*, hipStream_t) {
+    EXPECT(work == g_work, 1);
+    g_total_of = partials;
+    return hipSuccess;
+}
+hipError_t launch_grad_scale(const GradList& l, int blocks, const double*, hipStream_t) {
+    g_scaled += elements(l, blocks);
+    return hipSuccess;
+}
+}  // namespace np
+
+static void reset() { g_squares = g_scaled = g_partials = g_launches = 0; g_total_of = -1; }
+
+int main() {
+    const int64_t huge = std::numeric_limits<int64_t>::max();
+    alignas(16) static char mem[64];
+    char* const far = reinterpret_cast<char*>(uintptr_t(1) << 44);
+    float* norm = reinterpret_cast<float*>(mem);
+    g_work = reinterpret_cast<double*>(mem + 16);
+    const int64_t ws = NORMPRE_GRAD_WORKSPACE_BYTES;
+
+    // Tensors of one element, of several pieces, of none; more than a launch holds.
+    for (int64_t count : {0, 1, 151, 152, 153, 5000, 1 << 20}) {
+        std::vector<normpre_grad> g(count);
+        long long all = 0;
+        char* at = far;
+        for (int64_t i = 0; i < count; ++i) {
+            const int64_t n = i == 3 ? (int64_t(1) << 32) + 5 : i % 7 == 5 ? 0 : i % 100 + 1;
+            g[i] = {at, at, n, (int)(i % 2), (int)(i % 2)};
+            at += 4 * n;
+            all += n;
+        }
+        reset();
+        EXPECT(normpre_grad_norm(count, g.data(), norm, g_work, ws, nullptr), NORMPRE_OK);
+        EXPECT(g_squares, all);
+        EXPECT(g_total_of, g_partials);
+        EXPECT(g_scaled, 0);
+        reset();
+        EXPECT(normpre_grad_clip(count, g.data(), 1.0, norm, g_work, ws, nullptr), NORMPRE_OK);
+        EXPECT(g_squares, all);
+        EXPECT(g_scaled, all);
+        for (auto& x : g) x.out = nullptr;
+        reset();
+        EXPECT(normpre_grad_norm(count, g.data(), norm, g_work, ws, nullptr), NORMPRE_OK);
+    }
+    reset();
+    EXPECT(normpre_grad_norm(0, nullptr, norm, g_work, ws, nullptr), NORMPRE_OK);
+    EXPECT(g_total_of, 0);
+    // The largest call that is taken: 2^40 elements in all.
+    std::vector<normpre_grad> g(1 << 20, normpre_grad{far, nullptr, 1, 0, 0});
+    g[0].count = (int64_t(1) << 40) - (1 << 20) + 1;
+    reset();
+    EXPECT(normpre_grad_norm(1 << 20, g.data(), norm, g_work, ws, nullptr), NORMPRE_OK);
+    ++g[0].count;
+    reset();
+    EXPECT(normpre_grad_norm(1 << 20, g.data(), norm, g_work, ws, nullptr), NORMPRE_ERR_UNSUPPORTED);
+    g[0].count = huge;
+    EXPECT(normpre_grad_norm(1 << 20, g.data(), norm, g_work, ws, nullptr), NORMPRE_ERR_UNSUPPORTED);
+    EXPECT(normpre_grad_norm(huge, g.data(), norm, g_work, ws, nullptr), NORMPRE_ERR_UNSUPPORTED);
+    EXPECT(normpre_grad_norm(-huge, g.data(), norm, g_work, ws, nullptr), NORMPRE_ERR_INVALID_ARG);
+    g[0].count = -huge;
+    EXPECT(normpre_grad_norm(2, g.data(), norm, g_work, ws, nullptr), NORMPRE_ERR_INVALID_ARG);
+    EXPECT(g_launches, 0);
+
+    std::printf("%d failure(s)\n", g_failures);
+    return g_failures != 0;
+}
