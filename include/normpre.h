@@ -602,6 +602,62 @@ int normpre_checkpoint_weight_grad(int dtype, int layout, int accumulate, int64_
                                    const void* dy, int64_t ld_dy, float* dw, int64_t ld_dw,
                                    void* workspace, int64_t workspace_bytes, void* stream);
 
+/*
+ * Norms of the query and key heads and the rotation of their positions, between the
+ * projection and attention.  For a head x of head_dim features and the first
+ * 2 pairs of them, which turn:
+ *   n_d = x_d w_d / sqrt(mean_d x_d^2 + eps)              (norm 1; else n = x)
+ *   (a, b) -> (a cos t - b sin t, a sin t + b cos t),  t = position * freqs[i]
+ * for pair i: features (i, i + pairs), or (2i, 2i + 1) if adjacent; the others stay
+ * n_d.  Positions have one or several axes (time, height, width ..); pair i
+ * turns by the one of axes[i].
+ * The backward call takes the gradients of q_out and k_out in their place (and q and
+ * k where norm is 1) and writes dq, dk and, where wanted, the weights' gradients,
+ * summed over tokens and heads (zero for tokens = 0).
+ * Angles are reduced in 64 bits: at position p they are off by p freqs[i] 2^-52.
+ * Squares are summed in 64 bits, the rest is fp32, rounded once.
+ */
+typedef struct normpre_qk_rope {
+    int32_t dtype;              /* NORMPRE_DTYPE_*, of every operand             */
+    int32_t heads, kv_heads;    /* of q and of k, 1..2^16                        */
+    int32_t head_dim;           /* 1..256                                        */
+    int32_t pairs;              /* turning ones, 0..head_dim / 2                 */
+    int32_t adjacent;           /* 0 or 1                                        */
+    int32_t norm;               /* 0 or 1                                        */
+    int32_t weight_dtype;       /* NORMPRE_DTYPE_*, of q_weight and k_weight     */
+    int32_t num_axes;           /* rows of positions                             */
+    int32_t position_bytes;     /* 4 or 8: int32 or int64                        */
+    double  eps;                /* finite, >= 0                                  */
+    int64_t tokens;
+    const double*  freqs;       /* [pairs], radians a step                       */
+    const int32_t* axes;        /* [pairs], each below num_axes (larger ones are */
+                                /* taken for the last axis); null: all 0         */
+    const void* positions;      /* [num_axes][tokens]                            */
+    int64_t position_stride;    /* elements from one axis to the next            */
+    const void* q_weight;       /* [head_dim]; null: 1                           */
+    const void* k_weight;
+    normpre_heads q, k;         /* read (backward: with norm only)               */
+    normpre_heads q_out, k_out; /* forward: written; backward: their gradients   */
+    normpre_heads dq, dk;       /* backward: written                             */
+    float*  dq_weight;          /* backward, with norm: [head_dim], written;     */
+    float*  dk_weight;          /* null: not wanted                              */
+    void*   workspace;          /* backward: 16-byte aligned, of                 */
+    int64_t workspace_bytes;    /* normpre_qk_rope_workspace() bytes or more     */
+} normpre_qk_rope;
+
+/* Workspace bytes of a backward call (0 where no weight gradient is wanted); reads
+ * the sizes, norm, dq_weight and dk_weight of *a.  Host only. */
+int normpre_qk_rope_workspace(const normpre_qk_rope* a, int64_t* bytes);
+/*
+ * tokens = 0: nothing but zero weight gradients is written.
+ * Errors: INVALID_ARG (null or misaligned pointers, unknown dtypes, counts, flags or
+ * eps out of their ranges, negative strides, an output whose rows overlap, too small
+ * a workspace), UNSUPPORTED (head_dim > 256, more than 2^16 heads, 2^31 tokens,
+ * strides above 2^40), HIP.
+ */
+int normpre_qk_rope_forward(const normpre_qk_rope* a, void* stream);
+int normpre_qk_rope_backward(const normpre_qk_rope* a, void* stream);
+
 /* ---- gradient norm and clipping ------------------------------------------ */
 /*
  * The norm of all gradients together, and the gradients scaled down to a limit,

@@ -130,6 +130,26 @@ class normpre_attention(ctypes.Structure):
     ]
 
 
+class normpre_qk_rope(ctypes.Structure):
+    _fields_ = [
+        *((name, ctypes.c_int32) for name in ("dtype", "heads", "kv_heads", "head_dim", "pairs", "adjacent", "norm",
+                                              "weight_dtype", "num_axes", "position_bytes")),
+        ("eps", ctypes.c_double),
+        ("tokens", ctypes.c_int64),
+        ("freqs", ctypes.c_void_p),
+        ("axes", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p),
+        ("position_stride", ctypes.c_int64),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+        ("q", normpre_heads), ("k", normpre_heads),
+        ("q_out", normpre_heads), ("k_out", normpre_heads),
+        ("dq", normpre_heads), ("dk", normpre_heads),
+        ("dq_weight", ctypes.c_void_p), ("dk_weight", ctypes.c_void_p),
+        ("workspace", ctypes.c_void_p),
+        ("workspace_bytes", ctypes.c_int64),
+    ]
+
+
 class normpre_grad(ctypes.Structure):
     _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("count", ctypes.c_int64),
                 ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32)]
@@ -197,6 +217,9 @@ def load_library(path: str = LIB_PATH):
         "normpre_checkpoint_weight_grad": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64,
                                                           ctypes.c_int64, ctypes.c_int64, P, P, P, ctypes.c_int64,
                                                           P, ctypes.c_int64, P, ctypes.c_int64, P]),
+        "normpre_qk_rope_workspace": (ctypes.c_int, [ctypes.POINTER(normpre_qk_rope), i64p]),
+        "normpre_qk_rope_forward": (ctypes.c_int, [ctypes.POINTER(normpre_qk_rope), P]),
+        "normpre_qk_rope_backward": (ctypes.c_int, [ctypes.POINTER(normpre_qk_rope), P]),
         "normpre_grad_norm": (ctypes.c_int, [ctypes.c_int64, P, P, P, ctypes.c_int64, P]),
         "normpre_grad_clip": (ctypes.c_int, [ctypes.c_int64, P, ctypes.c_double, P, P, ctypes.c_int64, P]),
     }
@@ -484,6 +507,26 @@ def normpre_checkpoint_weight_grad(dtype: int, layout: int, accumulate: bool, to
     code = load_library().normpre_checkpoint_weight_grad(dtype, layout, int(bool(accumulate)), tokens, inner, outer,
                                                          codes, exps, dy, ld_dy, dw, ld_dw, workspace,
                                                          workspace_bytes, _stream_handle(stream))
+    if code:
+        _check(code)
+
+
+def normpre_qk_rope_workspace(args: normpre_qk_rope) -> int:
+    out = ctypes.c_int64()
+    code = load_library().normpre_qk_rope_workspace(args, out)
+    if code:
+        _check(code)
+    return out.value
+
+
+def normpre_qk_rope_forward(args: normpre_qk_rope, stream=None) -> None:
+    code = load_library().normpre_qk_rope_forward(args, _stream_handle(stream))
+    if code:
+        _check(code)
+
+
+def normpre_qk_rope_backward(args: normpre_qk_rope, stream=None) -> None:
+    code = load_library().normpre_qk_rope_backward(args, _stream_handle(stream))
     if code:
         _check(code)
 

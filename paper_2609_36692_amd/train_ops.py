@@ -2,6 +2,8 @@
 
 Between a model's loss and the gradients of its hidden matrices:
 
+* ``qk_norm_rope``: norms of the query and key heads and the rotation of their
+  positions (``Rotary``; positions of one or several axes), and its backward pass;
 * ``attention``: causal (or full) attention over packed sequences of different
   lengths with grouped heads, and its backward pass;
 * 8-bit activation checkpoints: ``checkpoint_pack`` / ``checkpoint_unpack``,
@@ -15,8 +17,8 @@ Between a model's loss and the gradients of its hidden matrices:
 Every operator runs in the gfx950 kernels of libnormpre.so on the current
 stream of its tensors' device, in bf16 or fp32; there is no fallback.  The
 ``*_forward``, ``*_backward`` and ``checkpoint_*`` functions are the kernels'
-calls and record nothing for autograd; ``attention``, ``checkpointed_linear``
-and ``checkpointed_mlp`` are differentiable.
+calls and record nothing for autograd; ``qk_norm_rope``, ``attention``,
+``checkpointed_linear`` and ``checkpointed_mlp`` are differentiable.
 """
 from __future__ import annotations
 
@@ -176,6 +178,144 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Attention
               scale: float | None = None) -> torch.Tensor:
     """Differentiable ``attention_forward``; returns out alone."""
     return _Attention.apply(q, k, v, plan, scale)
+
+
+# -------------------------------------------------------------- rotation ---
+class Rotary:
+    """How heads turn with their positions: made once, used by every layer.
+
+    freqs: radians a step of each turning pair of features (numbers, kept in 64
+    bits); the first 2 * len(freqs) features of a head turn, the others stay.
+    axes: the axis of positions that each pair turns by (default: all by the
+    first).  adjacent: pair i is features (2i, 2i + 1); else (i, i + len(freqs)).
+    """
+
+    def __init__(self, freqs: Sequence[float], axes: Sequence[int] | None = None, adjacent: bool = False,
+                 device="cuda"):
+        freqs = [float(f) for f in freqs]
+        self.pairs, self.adjacent, self.num_axes = len(freqs), bool(adjacent), 1
+        if axes is not None:
+            axes = [int(a) for a in axes]
+            if len(axes) != len(freqs) or any(a < 0 for a in axes):
+                raise ValueError("axes names an axis, 0 or above, for each frequency")
+            self.num_axes = max(axes, default=0) + 1
+        self.freqs = torch.tensor(freqs, dtype=torch.float64, device=device)
+        self.axes = None if axes is None or self.num_axes == 1 else torch.tensor(axes, dtype=torch.int32, device=device)
+
+    @staticmethod
+    def geometric(rotated: int, base: float = 10000.0) -> list[float]:
+        """Frequencies base^(-2i / rotated) of `rotated` / 2 pairs."""
+        if rotated < 0 or rotated % 2:
+            raise ValueError(f"{rotated} features do not make pairs")
+        return [base ** (-2 * i / rotated) for i in range(rotated // 2)]
+
+
+# normpre_qk_rope (include/normpre.h) in one piece, as for attention.
+_ROPE = struct.Struct("=10idq" + "3Qq" + "2Q" + "Q2q" * 6 + "2Q" + "Qq")
+
+
+def _rope_args(q, k, positions, rotary: Rotary | None, norm, q_weight, k_weight, eps):
+    """(device index, the fields up to k_weight); checks the operands."""
+    tokens, heads, dim = q.shape
+    if k.shape[0] != tokens or k.shape[2] != dim:
+        raise ValueError(f"expected q [tokens, heads, dim] and k [tokens, kv_heads, dim], got {tuple(q.shape)}, {tuple(k.shape)}")
+    at = _same(q, k)
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    if weights and not norm:
+        raise ValueError("weights are the norm's")
+    for w in weights:
+        if w.shape != (dim,) or w.dtype != weights[0].dtype or w.get_device() != at or not w.is_contiguous():
+            raise ValueError(f"a weight is a contiguous [{dim}] tensor on {q.device}, of the other's type")
+    turn = (0, 0, 0, 0)
+    if rotary is not None:
+        if positions is None or positions.dtype not in (torch.int32, torch.int64) or positions.get_device() != at \
+                or positions.shape not in ((rotary.num_axes, tokens), *(((tokens,),) if rotary.num_axes == 1 else ())):
+            raise ValueError(f"positions are int32 or int64 [{rotary.num_axes}, {tokens}] on {q.device}")
+        if rotary.freqs.get_device() != at:
+            raise ValueError("the rotary lies on another device")
+        turn = (rotary.freqs.data_ptr(), 0 if rotary.axes is None else rotary.axes.data_ptr(), positions.data_ptr(),
+                positions.stride(0) if positions.dim() == 2 else 0)
+    return at, (_dtype(q), heads, k.shape[1], dim, 0 if rotary is None else rotary.pairs,
+                int(rotary is not None and rotary.adjacent), int(bool(norm)), _dtype(weights[0]) if weights else 0,
+                1 if rotary is None else rotary.num_axes, 4 if positions is None else positions.element_size(),
+                float(eps), tokens, *turn, *(0 if w is None else w.data_ptr() for w in (q_weight, k_weight)))
+
+
+def _positions(positions: torch.Tensor | None) -> torch.Tensor | None:
+    """Positions with adjacent tokens."""
+    return positions if positions is None or positions.dim() not in (1, 2) or positions.stride(-1) == 1 else positions.contiguous()
+
+
+def qk_norm_rope_forward(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | None, rotary: Rotary | None, *,
+                         norm: bool = True, q_weight: torch.Tensor | None = None,
+                         k_weight: torch.Tensor | None = None, eps: float = 1e-6):
+    """(q, k) with their heads normed, x / sqrt(mean x^2 + eps) times the weight
+    [dim] if there is one (``norm``), and turned by ``rotary`` (None: not turned)
+    at ``positions``, int32 or int64 [tokens], or [axes, tokens] of several axes.
+    q [tokens, heads, dim], k [tokens, kv_heads, dim], dim up to 256, any strides;
+    weights fp32 or bf16."""
+    q, k, positions = _rows(q), _rows(k), _positions(positions)
+    at, args = _rope_args(q, k, positions, rotary, norm, q_weight, k_weight, eps)
+    if _elsewhere(at):
+        with torch.cuda.device(at):
+            return qk_norm_rope_forward(q, k, positions, rotary, norm=norm, q_weight=q_weight, k_weight=k_weight, eps=eps)
+    q_out, k_out = q.new_empty(q.shape), k.new_empty(k.shape)
+    block = _ROPE.pack(*args, *_heads(q), *_heads(k), *_heads(q_out), *_heads(k_out), *_NONE * 2, 0, 0, 0, 0)
+    N.normpre_qk_rope_forward(N.normpre_qk_rope.from_buffer_copy(block), _stream(at))
+    return q_out, k_out
+
+
+def qk_norm_rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                          positions: torch.Tensor | None, rotary: Rotary | None, *, norm: bool = True,
+                          q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
+                          eps: float = 1e-6):
+    """(dq, dk, dq_weight, dk_weight) from the gradients of ``qk_norm_rope_forward``'s
+    outputs and what that call took; the weights' in fp32, None where there is no
+    weight."""
+    if dq_out.shape != q.shape or dk_out.shape != k.shape:
+        raise ValueError("gradients have the shapes of q and k")
+    q, k, dq_out, dk_out, positions = _rows(q), _rows(k), _rows(dq_out), _rows(dk_out), _positions(positions)
+    at, args = _rope_args(q, k, positions, rotary, norm, q_weight, k_weight, eps)
+    _same(q, dq_out, dk_out)
+    if _elsewhere(at):
+        with torch.cuda.device(at):
+            return qk_norm_rope_backward(dq_out, dk_out, q, k, positions, rotary, norm=norm, q_weight=q_weight,
+                                         k_weight=k_weight, eps=eps)
+    dq, dk = q.new_empty(q.shape), k.new_empty(k.shape)
+    dw = [None if w is None else w.new_empty(w.shape, dtype=torch.float32) for w in (q_weight, k_weight)]
+    block = N.normpre_qk_rope.from_buffer_copy(_ROPE.pack(
+        *args, *_heads(q), *_heads(k), *_heads(dq_out), *_heads(dk_out), *_heads(dq), *_heads(dk),
+        *(0 if w is None else w.data_ptr() for w in dw), 0, 0))
+    if q_weight is not None or k_weight is not None:
+        block.workspace_bytes = N.normpre_qk_rope_workspace(block)
+        work = dq.new_empty(block.workspace_bytes, dtype=torch.uint8)
+        block.workspace = work.data_ptr()
+    N.normpre_qk_rope_backward(block, _stream(at))
+    return dq, dk, *dw
+
+
+class _QkNormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, positions, rotary, norm, q_weight, k_weight, eps):
+        ctx.save_for_backward(q, k, positions, q_weight, k_weight)
+        ctx.rotary, ctx.how = rotary, {"norm": norm, "eps": eps}
+        return qk_norm_rope_forward(q, k, positions, rotary, norm=norm, q_weight=q_weight, k_weight=k_weight, eps=eps)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dq_out, dk_out):
+        q, k, positions, *weights = ctx.saved_tensors
+        dq, dk, *dw = qk_norm_rope_backward(dq_out, dk_out, q, k, positions, ctx.rotary, q_weight=weights[0],
+                                            k_weight=weights[1], **ctx.how)
+        dwq, dwk = (d if d is None else d.to(w.dtype) for d, w in zip(dw, weights))
+        return dq, dk, None, None, None, dwq, dwk, None
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor | None, rotary: Rotary | None, *,
+                 norm: bool = True, q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
+                 eps: float = 1e-6) -> tuple[torch.Tensor, torch.Tensor]:
+    """Differentiable ``qk_norm_rope_forward``, with respect to q, k and the weights."""
+    return _QkNormRope.apply(q, k, positions, rotary, norm, q_weight, k_weight, eps)
 
 
 # ----------------------------------------------------------- checkpoints ---

@@ -1,8 +1,9 @@
-// Driver for the sanitized build of the gradient operators' host code
+// Driver for the sanitized build of the rotation's and the gradient operators' host code
 // (tests/test_step_abi_sanitized.py): the lists that launches get, and refusals,
 // with launchers that only look at what they are given.
 #include "../include/normpre.h"
 #include "../paper_2609_36692_amd/csrc/np_grads.h"
+#include "../paper_2609_36692_amd/csrc/np_rope.h"
 
 #include <cstdio>
 #include <limits>
@@ -58,7 +59,74 @@ hipError_t launch_grad_scale(const GradList& l, int blocks, const double*, hipSt
     g_scaled += elements(l, blocks);
     return hipSuccess;
 }
+
+int64_t rope_workspace(DType, const RopeArgs& a) { return rope_sums(a) ? 100 : 0; }
+hipError_t launch_rope(DType, const RopeArgs& a, bool backward, hipStream_t) {
+    ++g_launches;
+    EXPECT(a.partial != nullptr, backward && rope_sums(a));
+    return a.tokens == 77 ? hipErrorInvalidValue : hipSuccess;
+}
 }  // namespace np
+
+static void rope_calls(char* mem) {
+    const int64_t huge = std::numeric_limits<int64_t>::max();
+    const int32_t most = std::numeric_limits<int32_t>::max(), least = std::numeric_limits<int32_t>::min();
+    float* f = reinterpret_cast<float*>(mem);
+    normpre_qk_rope a{};
+    a.dtype = NORMPRE_DTYPE_BF16;
+    a.heads = 4;
+    a.kv_heads = 2;
+    a.head_dim = 64;
+    a.pairs = 32;
+    a.norm = 1;
+    a.num_axes = 1;
+    a.position_bytes = 8;
+    a.tokens = 100;
+    a.freqs = reinterpret_cast<double*>(mem);
+    a.positions = a.q_weight = a.k_weight = mem;
+    a.q = a.q_out = a.dq = {mem, 256, 64};
+    a.k = a.k_out = a.dk = {mem, 128, 64};
+    a.dq_weight = a.dk_weight = f;
+    a.workspace = mem;
+    g_launches = 0;
+    EXPECT(normpre_qk_rope_workspace(&a, &a.workspace_bytes), NORMPRE_OK);
+    EXPECT(a.workspace_bytes, 400);
+    EXPECT(normpre_qk_rope_forward(&a, nullptr), NORMPRE_OK);
+    EXPECT(normpre_qk_rope_backward(&a, nullptr), NORMPRE_OK);
+    EXPECT(g_launches, 2);
+    normpre_qk_rope b = a;
+    b.workspace_bytes = 399;
+    EXPECT(normpre_qk_rope_backward(&b, nullptr), NORMPRE_ERR_INVALID_ARG);
+    b.dq_weight = b.dk_weight = nullptr;
+    b.workspace = nullptr;
+    EXPECT(normpre_qk_rope_backward(&b, nullptr), NORMPRE_OK);
+    b = a;
+    b.tokens = 0;                                    // zero weight gradients
+    EXPECT(normpre_qk_rope_forward(&b, nullptr), NORMPRE_OK);
+    EXPECT(g_launches, 3);
+    EXPECT(normpre_qk_rope_backward(&b, nullptr), NORMPRE_OK);
+    EXPECT(g_launches, 4);
+    b.tokens = 77;
+    EXPECT(normpre_qk_rope_forward(&b, nullptr), NORMPRE_ERR_HIP);
+    b = a;
+    b.tokens = huge;
+    EXPECT(normpre_qk_rope_forward(&b, nullptr), NORMPRE_ERR_UNSUPPORTED);
+    b = a;
+    b.heads = most;
+    EXPECT(normpre_qk_rope_workspace(&b, &b.workspace_bytes), NORMPRE_ERR_UNSUPPORTED);
+    for (int32_t n : {least, -1, 33, most}) {
+        b = a;
+        b.pairs = n;
+        EXPECT(normpre_qk_rope_forward(&b, nullptr), NORMPRE_ERR_INVALID_ARG);
+    }
+    b = a;
+    b.tokens = most;
+    b.heads = b.kv_heads = np::kRopeMaxHeads;
+    b.q_out = {mem, int64_t(1) << 40, int64_t(1) << 40};
+    EXPECT(normpre_qk_rope_forward(&b, nullptr), NORMPRE_ERR_INVALID_ARG);
+    b.q_out = {mem, huge, 64};
+    EXPECT(normpre_qk_rope_forward(&b, nullptr), NORMPRE_ERR_UNSUPPORTED);
+}
 
 static void reset() { g_squares = g_scaled = g_partials = g_launches = 0; g_total_of = -1; }
 
@@ -112,6 +180,7 @@ int main() {
     g[0].count = -huge;
     EXPECT(normpre_grad_norm(2, g.data(), norm, g_work, ws, nullptr), NORMPRE_ERR_INVALID_ARG);
     EXPECT(g_launches, 0);
+    rope_calls(mem);
 
     std::printf("%d failure(s)\n", g_failures);
     return g_failures != 0;
