@@ -529,6 +529,35 @@ int normpre_attention_forward(const normpre_attention* a, void* stream);
 int normpre_attention_backward(const normpre_attention* a, void* stream);
 
 /*
+ * Attention with a sliding window: query i sees the keys j <= i of its sequence with
+ * j > i - window or j < sinks (the first tokens, which stay visible).  Everything
+ * else is as above, with plans of their own (causal is 1 in *a): window and sinks
+ * come from the caller (lengths beyond 2^31 mean the same as 2^31), sink_tiles and
+ * sink_pieces from normpre_window_attention_plan_sizes(), which every later call on
+ * the batch takes as they are.  A plan has 8 num_tiles + 8 sink_tiles +
+ * 4 sink_pieces int32.  Work and memory grow with tokens * (window + sinks); dk and
+ * dv of the first tokens are summed in pieces of their queries, in a fixed order, in
+ * the workspace.  bf16: delta is summed from the scores, as for few keys above, also
+ * where window + sinks is at most 128.
+ * Errors: as above, and INVALID_ARG (null window, window < 1, sinks < 0, causal not 1,
+ * sink_tiles and sink_pieces that no plan has).
+ */
+typedef struct normpre_window {
+    int64_t window;             /* keys of a query, itself among them; >= 1      */
+    int64_t sinks;              /* first tokens that stay visible; >= 0          */
+    int64_t sink_tiles;         /* of the plan                                   */
+    int64_t sink_pieces;
+} normpre_window;
+
+int normpre_window_attention_plan_sizes(int64_t num_seqs, const int64_t* lens, normpre_window* window,
+                                        int64_t* num_tiles);
+int normpre_window_attention_plan(int64_t num_seqs, const int64_t* lens, const normpre_window* window, int32_t* plan,
+                                  int64_t capacity);
+int normpre_window_attention_workspace(const normpre_attention* a, const normpre_window* window, int64_t* bytes);
+int normpre_window_attention_forward(const normpre_attention* a, const normpre_window* window, void* stream);
+int normpre_window_attention_backward(const normpre_attention* a, const normpre_window* window, void* stream);
+
+/*
  * 8-bit checkpoints.  The checkpoint of x [rows, cols] has groups of 64
  * consecutive features of a row (the last one of a row may be shorter).  With
  * amax the largest magnitude of a group, e is the smallest integer in

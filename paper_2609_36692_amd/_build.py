@@ -18,8 +18,9 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB = os.path.join(LIB_DIR, "libnormpre.so")
 OBJ_DIR = os.path.join(ROOT, "_build")
-SOURCES = ["np_gemm.hip", "np_elementwise.hip", "np_sketch.hip", "np_eigen.hip", "np_attention.hip", "np_checkpoint.hip",
-           "np_rope.hip", "np_grads.hip", "np_train_api.cpp", "np_rope_api.cpp", "np_grads_api.cpp", "normpre_api.cpp"]
+SOURCES = ["np_attn_window.hip", "np_attention.hip", "np_rope.hip", "np_gemm.hip", "np_elementwise.hip", "np_sketch.hip",
+           "np_eigen.hip", "np_checkpoint.hip", "np_grads.hip", "np_train_api.cpp", "np_window_api.cpp",
+           "np_rope_api.cpp", "np_grads_api.cpp", "normpre_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -5,6 +5,7 @@
 #include "np_internal.h"
 #include "np_train.h"
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdint>
 #include <cstdio>
@@ -65,6 +66,96 @@ inline AttnOperand operand(const normpre_heads& o) { return {o.data, o.token_str
         const int rc_ = (call);                   \
         if (rc_ != NORMPRE_OK) return rc_;        \
     } while (0)
+
+// ----------------------------------------------------------- attention ---
+// Number of tiles of 128 rows and of tokens.
+inline int count_tiles(int64_t num_seqs, const int64_t* lens, int64_t& tiles, int64_t& tokens) {
+    if (num_seqs < 0) return bad("num_seqs < 0");
+    if (num_seqs > 0 && !lens) return bad("lens is null");
+    tiles = tokens = 0;
+    for (int64_t i = 0; i < num_seqs; ++i) {
+        if (lens[i] < 0) return fail(NORMPRE_ERR_INVALID_ARG, "sequence %lld has a negative length", (long long)i);
+        if (lens[i] > kMaxTokens - tokens) return fail(NORMPRE_ERR_UNSUPPORTED, "2^31 tokens or more");
+        tokens += lens[i];
+        tiles += (lens[i] + kAttnRows - 1) / kAttnRows;
+    }
+    return NORMPRE_OK;
+}
+
+inline int check_attention_sizes(const normpre_attention* a) {
+    if (!a) return bad("the argument block is null");
+    if (!known(a->dtype)) return fail(NORMPRE_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
+    if (a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads)
+        return fail(NORMPRE_ERR_INVALID_ARG, "%d heads over %d key heads", a->heads, a->kv_heads);
+    if (a->head_dim < 1) return fail(NORMPRE_ERR_INVALID_ARG, "head_dim %d < 1", a->head_dim);
+    if (a->head_dim > kAttnMaxDim)
+        return fail(NORMPRE_ERR_UNSUPPORTED, "head_dim %d exceeds %d", a->head_dim, kAttnMaxDim);
+    if (a->causal != 0 && a->causal != 1) return bad("causal is neither 0 nor 1");
+    if (!std::isfinite(a->scale)) return bad("scale must be finite");
+    if (a->tokens < 0 || a->num_tiles < 0) return bad("tokens < 0 or num_tiles < 0");
+    if (a->tokens > kMaxTokens) return fail(NORMPRE_ERR_UNSUPPORTED, "2^31 tokens or more");
+    // Every token lies in one tile, and no tile is empty.
+    if (a->num_tiles > a->tokens || a->num_tiles * kAttnRows < a->tokens)
+        return fail(NORMPRE_ERR_INVALID_ARG, "%lld tiles cannot hold %lld tokens", (long long)a->num_tiles,
+                    (long long)a->tokens);
+    if (a->num_tiles * a->heads > kMaxBlocks) return fail(NORMPRE_ERR_UNSUPPORTED, "more than 2^23 - 1 blocks of 128 rows");
+    return NORMPRE_OK;
+}
+
+inline AttnArgs attention_sizes(const normpre_attention* a) {
+    AttnArgs k{};
+    k.num_tiles = (int)a->num_tiles;
+    k.tokens = a->tokens;
+    k.heads = a->heads;
+    k.kv_heads = a->kv_heads;
+    k.dim = a->head_dim;
+    return k;
+}
+
+// All but the workspace.
+inline int check_attention(const normpre_attention* a, bool backward) {
+    NP_CHECK(check_attention_sizes(a));
+    if (a->tokens == 0) return NORMPRE_OK;
+    if (!a->plan || !on(a->plan, 16)) return bad("plan is null or not 16-byte aligned");
+    if (!a->lse || !on(a->lse, 4)) return bad("lse is null or misaligned");
+    const int64_t t = a->tokens, hq = a->heads, hk = a->kv_heads, d = a->head_dim, e = size_of(a->dtype);
+    NP_CHECK(check_operand("q", a->q, t, hq, d, e, false));
+    NP_CHECK(check_operand("k", a->k, t, hk, d, e, false));
+    NP_CHECK(check_operand("v", a->v, t, hk, d, e, false));
+    NP_CHECK(check_operand("out", a->out, t, hq, d, e, !backward));
+    if (backward) {
+        NP_CHECK(check_operand("dout", a->dout, t, hq, d, e, false));
+        NP_CHECK(check_operand("dq", a->dq, t, hq, d, e, true));
+        NP_CHECK(check_operand("dk", a->dk, t, hk, d, e, true));
+        NP_CHECK(check_operand("dv", a->dv, t, hk, d, e, true));
+    }
+    return NORMPRE_OK;
+}
+
+inline void attention_operands(const normpre_attention* a, bool backward, AttnArgs& k) {
+    k.q = operand(a->q);
+    k.k = operand(a->k);
+    k.v = operand(a->v);
+    k.out = operand(a->out);
+    k.lse = a->lse;
+    k.tiles = reinterpret_cast<const AttnTile*>(a->plan);
+    k.causal = a->causal;
+    k.scale = a->scale;
+    if (!backward) return;
+    k.dout = operand(a->dout);
+    k.dq = operand(a->dq);
+    k.dk = operand(a->dk);
+    k.dv = operand(a->dv);
+}
+
+// The parts of a backward call's workspace.
+inline void attention_parts(float* ws, AttnArgs& k) {
+    const int64_t rows = (int64_t)k.heads * k.tokens;
+    k.lse2 = ws;
+    k.delta = ws + rows;
+    k.partial = ws + (2 * rows + 3) / 4 * 4;
+    k.odd = reinterpret_cast<uint32_t*>(k.partial);
+}
 
 }  // namespace
 }  // namespace np

@@ -35,6 +35,12 @@ struct AttnArgs {
     int64_t tokens;
     int heads, kv_heads, dim, causal;
     float scale;
+    // Sliding window (launch_window_*): query i sees keys j <= i with j > i - window or
+    // j < sinks.
+    int window, sinks;
+    int sink_tiles, sink_pieces;    // entries of the plan behind its tiles (AttnSink, AttnPiece)
+    int sink_rows;              // rows of a key tile that may be sinks, whole waves: 32 .. 128
+    float* first_keys;          // [sink_pieces + sink_tiles][2][kv_heads][sink_rows][64 or 128]
 };
 
 // Shares into which the dk/dv pass cuts the queries of a key, and the floats of
@@ -43,6 +49,12 @@ int attention_splits(int64_t num_tiles, int kv_heads);
 int64_t attention_workspace(const AttnArgs& a);
 hipError_t launch_attention_forward(DType t, const AttnArgs& a, hipStream_t s);
 hipError_t launch_attention_backward(DType t, const AttnArgs& a, hipStream_t s);
+
+// The same with a sliding window; the workspace is that of a call without one, then
+// first_keys.
+int window_splits(const AttnArgs& a);
+hipError_t launch_window_forward(DType t, const AttnArgs& a, hipStream_t s);
+hipError_t launch_window_backward(DType t, const AttnArgs& a, hipStream_t s);
 
 // --------------------------------------------------------- checkpoints ---
 constexpr int kCkptGroup = 64;          // features that share an exponent

@@ -4,7 +4,6 @@
 #include "np_checks.h"
 
 #include <algorithm>
-#include <cmath>
 #include <cstring>
 #include <new>
 #include <vector>
@@ -14,98 +13,24 @@ using namespace np;
 namespace {
 
 // ----------------------------------------------------------- attention ---
-// Number of tiles of 128 rows and of tokens; false: error set.
-int count(int64_t num_seqs, const int64_t* lens, int64_t& tiles, int64_t& tokens) {
-    if (num_seqs < 0) return bad("num_seqs < 0");
-    if (num_seqs > 0 && !lens) return bad("lens is null");
-    tiles = tokens = 0;
-    for (int64_t i = 0; i < num_seqs; ++i) {
-        if (lens[i] < 0) return fail(NORMPRE_ERR_INVALID_ARG, "sequence %lld has a negative length", (long long)i);
-        if (lens[i] > kMaxTokens - tokens) return fail(NORMPRE_ERR_UNSUPPORTED, "2^31 tokens or more");
-        tokens += lens[i];
-        tiles += (lens[i] + kAttnRows - 1) / kAttnRows;
-    }
-    return NORMPRE_OK;
-}
-
-int check_sizes(const normpre_attention* a) {
-    if (!a) return bad("the argument block is null");
-    if (!known(a->dtype)) return fail(NORMPRE_ERR_INVALID_ARG, "unknown dtype %d", a->dtype);
-    if (a->heads < 1 || a->kv_heads < 1 || a->heads % a->kv_heads)
-        return fail(NORMPRE_ERR_INVALID_ARG, "%d heads over %d key heads", a->heads, a->kv_heads);
-    if (a->head_dim < 1) return fail(NORMPRE_ERR_INVALID_ARG, "head_dim %d < 1", a->head_dim);
-    if (a->head_dim > kAttnMaxDim)
-        return fail(NORMPRE_ERR_UNSUPPORTED, "head_dim %d exceeds %d", a->head_dim, kAttnMaxDim);
-    if (a->causal != 0 && a->causal != 1) return bad("causal is neither 0 nor 1");
-    if (!std::isfinite(a->scale)) return bad("scale must be finite");
-    if (a->tokens < 0 || a->num_tiles < 0) return bad("tokens < 0 or num_tiles < 0");
-    if (a->tokens > kMaxTokens) return fail(NORMPRE_ERR_UNSUPPORTED, "2^31 tokens or more");
-    // Every token lies in one tile, and no tile is empty.
-    if (a->num_tiles > a->tokens || a->num_tiles * kAttnRows < a->tokens)
-        return fail(NORMPRE_ERR_INVALID_ARG, "%lld tiles cannot hold %lld tokens", (long long)a->num_tiles,
-                    (long long)a->tokens);
-    if (a->num_tiles * a->heads > kMaxBlocks) return fail(NORMPRE_ERR_UNSUPPORTED, "more than 2^23 - 1 blocks of 128 rows");
-    return NORMPRE_OK;
-}
-
 // The sizes alone, with what the backward pass makes of them.
 AttnArgs sizes(const normpre_attention* a) {
-    AttnArgs k{};
-    k.num_tiles = (int)a->num_tiles;
-    k.tokens = a->tokens;
-    k.heads = a->heads;
-    k.kv_heads = a->kv_heads;
-    k.dim = a->head_dim;
+    AttnArgs k = attention_sizes(a);
     k.splits = attention_splits(a->num_tiles, a->kv_heads);
     return k;
 }
 
 int attention(const normpre_attention* a, bool backward, void* stream) {
-    const int sized = check_sizes(a);
-    if (sized != NORMPRE_OK) return sized;
+    NP_CHECK(check_attention(a, backward));
     if (a->tokens == 0) return NORMPRE_OK;
-    if (!a->plan || !on(a->plan, 16)) return bad("plan is null or not 16-byte aligned");
-    if (!a->lse || !on(a->lse, 4)) return bad("lse is null or misaligned");
-    const int64_t t = a->tokens, hq = a->heads, hk = a->kv_heads, d = a->head_dim, e = size_of(a->dtype);
-    int rc = NORMPRE_OK;
-    auto operand_ok = [&](const char* n, const normpre_heads& o, int64_t h, bool w) {
-        if (rc == NORMPRE_OK) rc = check_operand(n, o, t, h, d, e, w);
-    };
-    operand_ok("q", a->q, hq, false);
-    operand_ok("k", a->k, hk, false);
-    operand_ok("v", a->v, hk, false);
-    operand_ok("out", a->out, hq, !backward);
-    if (backward) {
-        operand_ok("dout", a->dout, hq, false);
-        operand_ok("dq", a->dq, hq, true);
-        operand_ok("dk", a->dk, hk, true);
-        operand_ok("dv", a->dv, hk, true);
-    }
-    if (rc != NORMPRE_OK) return rc;
-
     AttnArgs k = sizes(a);
-    k.q = operand(a->q);
-    k.k = operand(a->k);
-    k.v = operand(a->v);
-    k.out = operand(a->out);
-    k.lse = a->lse;
-    k.tiles = reinterpret_cast<const AttnTile*>(a->plan);
-    k.causal = a->causal;
-    k.scale = a->scale;
+    attention_operands(a, backward, k);
     const DType dt = (DType)a->dtype;
     if (!backward) return launched(launch_attention_forward(dt, k, (hipStream_t)stream));
-    k.dout = operand(a->dout);
-    k.dq = operand(a->dq);
-    k.dk = operand(a->dk);
-    k.dv = operand(a->dv);
     float* ws = static_cast<float*>(a->workspace);
     if (!ws || !on(ws, 16) || a->workspace_bytes < 4 * attention_workspace(k))
         return bad("workspace is null, misaligned or too small");
-    const int64_t rows = (int64_t)a->heads * a->tokens;
-    k.lse2 = ws;
-    k.delta = ws + rows;
-    k.partial = ws + (2 * rows + 3) / 4 * 4;
-    k.odd = reinterpret_cast<uint32_t*>(k.partial);
+    attention_parts(ws, k);
     return launched(launch_attention_backward(dt, k, (hipStream_t)stream));
 }
 
@@ -139,14 +64,14 @@ extern "C" {
 int normpre_attention_plan_tiles(int64_t num_seqs, const int64_t* lens, int64_t* num_tiles) {
     if (!num_tiles) return bad("num_tiles is null");
     int64_t tiles, tokens;
-    NP_CHECK(count(num_seqs, lens, tiles, tokens));
+    NP_CHECK(count_tiles(num_seqs, lens, tiles, tokens));
     *num_tiles = tiles;
     return NORMPRE_OK;
 }
 
 int normpre_attention_plan(int64_t num_seqs, const int64_t* lens, int causal, int32_t* plan, int64_t capacity) {
     int64_t n, tokens;
-    NP_CHECK(count(num_seqs, lens, n, tokens));
+    NP_CHECK(count_tiles(num_seqs, lens, n, tokens));
     if (causal != 0 && causal != 1) return bad("causal is neither 0 nor 1");
     if (capacity < 8 * n) return bad("the plan does not fit");
     if (n == 0) return NORMPRE_OK;
@@ -183,7 +108,7 @@ int normpre_attention_plan(int64_t num_seqs, const int64_t* lens, int causal, in
 
 int normpre_attention_workspace(const normpre_attention* a, int64_t* bytes) {
     if (!bytes) return bad("bytes is null");
-    NP_CHECK(check_sizes(a));
+    NP_CHECK(check_attention_sizes(a));
     *bytes = 4 * attention_workspace(sizes(a));
     return NORMPRE_OK;
 }

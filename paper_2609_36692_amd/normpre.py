@@ -130,6 +130,11 @@ class normpre_attention(ctypes.Structure):
     ]
 
 
+class normpre_window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int64), ("sinks", ctypes.c_int64), ("sink_tiles", ctypes.c_int64),
+                ("sink_pieces", ctypes.c_int64)]
+
+
 class normpre_qk_rope(ctypes.Structure):
     _fields_ = [
         *((name, ctypes.c_int32) for name in ("dtype", "heads", "kv_heads", "head_dim", "pairs", "adjacent", "norm",
@@ -217,6 +222,16 @@ def load_library(path: str = LIB_PATH):
         "normpre_checkpoint_weight_grad": (ctypes.c_int, [ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int64,
                                                           ctypes.c_int64, ctypes.c_int64, P, P, P, ctypes.c_int64,
                                                           P, ctypes.c_int64, P, ctypes.c_int64, P]),
+        "normpre_window_attention_plan_sizes": (ctypes.c_int, [ctypes.c_int64, i64p, ctypes.POINTER(normpre_window),
+                                                               i64p]),
+        "normpre_window_attention_plan": (ctypes.c_int, [ctypes.c_int64, i64p, ctypes.POINTER(normpre_window), P,
+                                                         ctypes.c_int64]),
+        "normpre_window_attention_workspace": (ctypes.c_int, [ctypes.POINTER(normpre_attention),
+                                                              ctypes.POINTER(normpre_window), i64p]),
+        "normpre_window_attention_forward": (ctypes.c_int, [ctypes.POINTER(normpre_attention),
+                                                            ctypes.POINTER(normpre_window), P]),
+        "normpre_window_attention_backward": (ctypes.c_int, [ctypes.POINTER(normpre_attention),
+                                                             ctypes.POINTER(normpre_window), P]),
         "normpre_qk_rope_workspace": (ctypes.c_int, [ctypes.POINTER(normpre_qk_rope), i64p]),
         "normpre_qk_rope_forward": (ctypes.c_int, [ctypes.POINTER(normpre_qk_rope), P]),
         "normpre_qk_rope_backward": (ctypes.c_int, [ctypes.POINTER(normpre_qk_rope), P]),
@@ -507,6 +522,39 @@ def normpre_checkpoint_weight_grad(dtype: int, layout: int, accumulate: bool, to
     code = load_library().normpre_checkpoint_weight_grad(dtype, layout, int(bool(accumulate)), tokens, inner, outer,
                                                          codes, exps, dy, ld_dy, dw, ld_dw, workspace,
                                                          workspace_bytes, _stream_handle(stream))
+    if code:
+        _check(code)
+
+
+def normpre_window_attention_plan(lens, window: int, sinks: int):
+    """(plan of a packed batch as a host array int32 [n], its tiles, the window's
+    argument of every call on the batch)."""
+    n = len(lens)
+    arr = (ctypes.c_int64 * max(1, n))(*[int(v) for v in lens])
+    tiles, bounds = ctypes.c_int64(), normpre_window(window, sinks)
+    lib = load_library()
+    _check(lib.normpre_window_attention_plan_sizes(n, arr, bounds, tiles))
+    plan = np.zeros(8 * tiles.value + 8 * bounds.sink_tiles + 4 * bounds.sink_pieces, dtype=np.int32)
+    _check(lib.normpre_window_attention_plan(n, arr, bounds, plan.ctypes.data_as(ctypes.c_void_p), plan.size))
+    return plan, tiles.value, bounds
+
+
+def normpre_window_attention_workspace(args: normpre_attention, window: normpre_window) -> int:
+    out = ctypes.c_int64()
+    code = load_library().normpre_window_attention_workspace(args, window, out)
+    if code:
+        _check(code)
+    return out.value
+
+
+def normpre_window_attention_forward(args: normpre_attention, window: normpre_window, stream=None) -> None:
+    code = load_library().normpre_window_attention_forward(args, window, _stream_handle(stream))
+    if code:
+        _check(code)
+
+
+def normpre_window_attention_backward(args: normpre_attention, window: normpre_window, stream=None) -> None:
+    code = load_library().normpre_window_attention_backward(args, window, _stream_handle(stream))
     if code:
         _check(code)
 

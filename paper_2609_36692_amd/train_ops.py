@@ -5,7 +5,8 @@ Between a model's loss and the gradients of its hidden matrices:
 * ``qk_norm_rope``: norms of the query and key heads and the rotation of their
   positions (``Rotary``; positions of one or several axes), and its backward pass;
 * ``attention``: causal (or full) attention over packed sequences of different
-  lengths with grouped heads, and its backward pass;
+  lengths with grouped heads, with a sliding window where the plan has one, and its
+  backward pass;
 * 8-bit activation checkpoints: ``checkpoint_pack`` / ``checkpoint_unpack``,
   ``checkpoint_act`` (an MLP's activation and the checkpoints its backward pass
   needs, in one pass), ``checkpoint_act_grad`` and ``checkpoint_weight_grad``
@@ -72,14 +73,30 @@ class AttentionPlan:
 
     Sequence i holds ``lens[i]`` consecutive tokens, one sequence after the
     other; ``causal``: token t sees the tokens up to itself in its sequence.
+    ``window``: of these, the last ``window`` alone, itself among them, and the first
+    ``sinks`` tokens of its sequence, which stay visible.
     """
 
-    def __init__(self, lens: Sequence[int], causal: bool = True, device="cuda"):
+    def __init__(self, lens: Sequence[int], causal: bool = True, device="cuda", window: int | None = None,
+                 sinks: int = 0):
         self.lens = [int(n) for n in lens]
         self.causal = bool(causal)
-        plan = N.normpre_attention_plan(self.lens, self.causal)
+        self.window, self.sinks = None if window is None else int(window), int(sinks)
+        self.bounds = None                           # of plans with a window
+        if self.window is None:
+            if self.sinks:
+                raise ValueError("sinks are the first tokens before a window")
+        elif not self.causal:
+            raise ValueError("a window is causal")
+        elif self.window < 1 or self.sinks < 0:
+            raise ValueError(f"a window of {window} tokens and {sinks} first ones")
         self.tokens = sum(self.lens)
-        self.num_tiles = plan.shape[1]
+        # Where every query sees all keys before it, no window is looked at.
+        if self.window is None or self.window + self.sinks >= max(self.lens, default=0):
+            plan = N.normpre_attention_plan(self.lens, self.causal)
+            self.num_tiles = plan.shape[1]
+        else:
+            plan, self.num_tiles, self.bounds = N.normpre_window_attention_plan(self.lens, self.window, self.sinks)
         self.data = torch.from_numpy(plan).to(device)
 
 
@@ -130,7 +147,10 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: A
     out = q.new_empty((tokens, heads, dim))
     lse = q.new_empty((heads, tokens), dtype=torch.float32)
     block = _ARGS.pack(*args, out.data_ptr(), heads * dim, dim, lse.data_ptr(), *_NONE * 4, 0, 0)
-    N.normpre_attention_forward(N.normpre_attention.from_buffer_copy(block), _stream(at))
+    if plan.bounds is None:
+        N.normpre_attention_forward(N.normpre_attention.from_buffer_copy(block), _stream(at))
+    else:
+        N.normpre_window_attention_forward(N.normpre_attention.from_buffer_copy(block), plan.bounds, _stream(at))
     return out, lse
 
 
@@ -152,10 +172,15 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
     block = N.normpre_attention.from_buffer_copy(_ARGS.pack(
         *args, *_heads(out), lse.data_ptr(), *_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv), 0, 0))
-    block.workspace_bytes = N.normpre_attention_workspace(block)
+    bounds = plan.bounds
+    block.workspace_bytes = (N.normpre_attention_workspace(block) if bounds is None
+                             else N.normpre_window_attention_workspace(block, bounds))
     work = lse.new_empty(block.workspace_bytes, dtype=torch.uint8)
     block.workspace = work.data_ptr()
-    N.normpre_attention_backward(block, _stream(at))
+    if bounds is None:
+        N.normpre_attention_backward(block, _stream(at))
+    else:
+        N.normpre_window_attention_backward(block, bounds, _stream(at))
     return dq, dk, dv
 
 

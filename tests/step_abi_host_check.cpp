@@ -1,4 +1,4 @@
-// Driver for the sanitized build of the rotation's and the gradient operators' host code
+// Driver for the sanitized build of the rotation's, the windows' and the gradient operators' host code
 // (tests/test_step_abi_sanitized.py): the lists that launches get, and refusals,
 // with launchers that only look at what they are given.
 #include "../include/normpre.h"
@@ -66,7 +66,72 @@ hipError_t launch_rope(DType, const RopeArgs& a, bool backward, hipStream_t) {
     EXPECT(a.partial != nullptr, backward && rope_sums(a));
     return a.tokens == 77 ? hipErrorInvalidValue : hipSuccess;
 }
+
+int attention_splits(int64_t, int) { return 2; }
+int window_splits(const AttnArgs&) { return 2; }
+int64_t attention_workspace(const AttnArgs& a) { return 2 * (int64_t)a.heads * a.tokens + 1; }
+hipError_t launch_window_forward(DType, const AttnArgs&, hipStream_t) { ++g_launches; return hipSuccess; }
+hipError_t launch_window_backward(DType, const AttnArgs& a, hipStream_t) {
+    ++g_launches;
+    EXPECT((reinterpret_cast<uintptr_t>(a.first_keys) - reinterpret_cast<uintptr_t>(a.lse2)) % 16, 0);
+    return hipErrorInvalidValue;
+}
 }  // namespace np
+
+static void window_calls(char* mem) {
+    const int64_t huge = std::numeric_limits<int64_t>::max();
+    // Plans, into buffers of exactly their size.
+    for (const std::vector<int64_t>& lens : {std::vector<int64_t>{}, {0}, {1}, {128, 129, 0, 4000}, std::vector<int64_t>(999, 3), {100000}})
+        for (int64_t window : {(int64_t)1, (int64_t)100, (int64_t)3999, huge})
+            for (int64_t sinks : {(int64_t)0, (int64_t)1, (int64_t)130, huge}) {
+                normpre_window w{window, sinks, -1, -1};
+                int64_t n = -1;
+                EXPECT(normpre_window_attention_plan_sizes((int64_t)lens.size(), lens.data(), &w, &n), NORMPRE_OK);
+                const int64_t size = 8 * n + 8 * w.sink_tiles + 4 * w.sink_pieces;
+                std::vector<int32_t> plan(size);
+                EXPECT(normpre_window_attention_plan((int64_t)lens.size(), lens.data(), &w, plan.data(), size), NORMPRE_OK);
+                EXPECT(normpre_window_attention_plan((int64_t)lens.size(), lens.data(), &w, plan.data(), size - 1), NORMPRE_ERR_INVALID_ARG);
+            }
+    int64_t n = 0, bad[2] = {huge, huge}, long_one[1] = {std::numeric_limits<int32_t>::max()};
+    normpre_window w{1, huge, 0, 0};
+    EXPECT(normpre_window_attention_plan_sizes(2, bad, &w, &n), NORMPRE_ERR_UNSUPPORTED);
+    EXPECT(normpre_window_attention_plan_sizes(1, long_one, &w, &n), NORMPRE_OK);
+    EXPECT(w.sink_pieces <= w.sink_tiles + 512, 1);
+
+    normpre_attention a{};
+    a.dtype = NORMPRE_DTYPE_BF16;
+    a.heads = 4;
+    a.kv_heads = 2;
+    a.head_dim = 64;
+    a.causal = 1;
+    a.scale = 1.f;
+    a.tokens = 300;
+    a.plan = reinterpret_cast<int32_t*>(mem);
+    a.num_tiles = 3;
+    a.q = a.out = a.dout = a.dq = {mem, 256, 64};
+    a.k = a.v = a.dk = a.dv = {mem, 128, 64};
+    a.lse = reinterpret_cast<float*>(mem);
+    a.workspace = mem;
+    w = {5, 1, 1, 1};
+    g_launches = 0;
+    EXPECT(normpre_window_attention_workspace(&a, &w, &a.workspace_bytes), NORMPRE_OK);
+    EXPECT(a.workspace_bytes, 4 * ((2 * 4 * 300 + 1 + 3) / 4 * 4 + 2 * 2 * 2 * 32 * 64));
+    EXPECT(normpre_window_attention_forward(&a, &w, nullptr), NORMPRE_OK);
+    EXPECT(normpre_window_attention_backward(&a, &w, nullptr), NORMPRE_ERR_HIP);
+    EXPECT(g_launches, 2);
+    for (const normpre_window& x : {normpre_window{huge, huge, huge, huge}, {-huge, 0, 0, 0}, {1, -huge, 0, 0}, {1, 1, -huge, 0},
+                                    {1, 1, 1, huge}, {1, 1, 1, -huge}}) {
+        EXPECT(normpre_window_attention_backward(&a, &x, nullptr), NORMPRE_ERR_INVALID_ARG);
+        EXPECT(normpre_window_attention_workspace(&a, &x, &n), NORMPRE_ERR_INVALID_ARG);
+    }
+    normpre_attention b = a;
+    b.tokens = b.num_tiles = std::numeric_limits<int32_t>::max();
+    b.heads = b.kv_heads = 1;
+    EXPECT(normpre_window_attention_forward(&b, &w, nullptr), NORMPRE_ERR_UNSUPPORTED);
+    b.num_tiles = huge;
+    EXPECT(normpre_window_attention_forward(&b, &w, nullptr), NORMPRE_ERR_INVALID_ARG);
+    EXPECT(g_launches, 2);
+}
 
 static void rope_calls(char* mem) {
     const int64_t huge = std::numeric_limits<int64_t>::max();
@@ -181,6 +246,7 @@ int main() {
     EXPECT(normpre_grad_norm(2, g.data(), norm, g_work, ws, nullptr), NORMPRE_ERR_INVALID_ARG);
     EXPECT(g_launches, 0);
     rope_calls(mem);
+    window_calls(mem);
 
     std::printf("%d failure(s)\n", g_failures);
     return g_failures != 0;
