@@ -895,6 +895,20 @@ template <bool WIN>
 __device__ __forceinline__ bool past_windows(const AttnArgs& a, int k0, int n, int qw) {
     return WIN && k0 < qw + 31 - (a.window - 1) && k0 + n > a.sinks;
 }
+// Which keys a query does not see, as places behind key k: those from it back to the window's
+// start, and those of the first keys that lie before it, are seen.
+struct Bounds {
+    uint32_t from, span;
+    int few;
+    __device__ __forceinline__ Bounds(const AttnArgs& a, const Where& w, int qi, int k) {
+        const uint32_t start = (uint32_t)qi - (uint32_t)(a.window - 1);
+        from = start - (uint32_t)k;
+        span = (uint32_t)min(qi, w.len - 1) - start;
+        few = min(a.sinks - k, (int)from);
+    }
+    __device__ __forceinline__ bool hides(int j) const { return (uint32_t)j - from > span; }
+    __device__ __forceinline__ bool hides_with_sinks(int j) const { return hides(j) & (j >= few); }
+};
 // The keys of [from, to) and, WIN, the first ones: of `from` = 0, those of the tiles.
 template <class T, bool WIN>
 __device__ Odd odd_keys(const AttnArgs& a, const Where& w, const AttnOperand& x, int from, int to, const KeyWalk& walk,
@@ -955,19 +969,30 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
             float mx = m;
             const bool far = past_windows<WIN>(a, k0, BN, qw);
             const bool edge = far || k0 + BN > w.len || (a.causal && k0 + BN - 1 > qw);
-            // WIN: keys before `first` are seen up to `few`.
-            const int first = WIN ? qi - (a.window - 1) - k0 - 4 * half : 0, few = WIN ? a.sinks - k0 - 4 * half : 0;
             const int last = (a.causal ? min(qi, w.len - 1) : w.len - 1) - k0 - 4 * half;
+            const Bounds bounds(a, w, qi, k0 + 4 * half);    // WIN
 #pragma unroll
             for (int b = 0; b < NB; ++b) s[b] = scores<T, DP>(ks, 32 * b, q, lane);
-            if (edge) {
+            // Selects, not branches, in WIN: a branch for each place is slow, and the compiler of
+            // ROCm 7.2 lost the first place's value on its way out of one.
+            auto mask = [&](float value) {
+                auto all = [&](auto hidden) {
+#pragma unroll
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) s[b][r] = hidden(32 * b + 8 * (r / 4) + r % 4) ? value : s[b][r];
+                };
+                if (k0 < a.sinks) all([&](int j) { return bounds.hides_with_sinks(j); });
+                else all([&](int j) { return bounds.hides(j); });
+            };
+            if constexpr (WIN) {
+                if (edge) mask(-INFINITY);
+            } else if (edge) {
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = 32 * b + 8 * (r / 4) + r % 4;
-                        if (j > last || (WIN && j < first && j >= few)) s[b][r] = -INFINITY;
-                    }
+                    for (int r = 0; r < 16; ++r)
+                        if (32 * b + 8 * (r / 4) + r % 4 > last) s[b][r] = -INFINITY;
             }
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -986,14 +1011,14 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[b][r] = exp2_fast(__builtin_fmaf(s[b][r], c2, -mu));
-            if (edge) {                              // also where c is 0
+            if constexpr (WIN) {
+                if (edge && c2 == 0.f) mask(0.f);
+            } else if (edge) {                       // also where c is 0
 #pragma unroll
                 for (int b = 0; b < NB; ++b)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = 32 * b + 8 * (r / 4) + r % 4;
-                        if (j > last || (WIN && j < first && j >= few)) s[b][r] = 0.f;
-                    }
+                    for (int r = 0; r < 16; ++r)
+                        if (32 * b + 8 * (r / 4) + r % 4 > last) s[b][r] = 0.f;
             }
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -1118,12 +1143,14 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
         for (int r = 0; r < 16; ++r) s[0][r] = exp2_fast(__builtin_fmaf(s[0][r], c2, -lse2)) * (s[1][r] - de);
         if (k0 + 32 * b + 32 > w.len || (a.causal && k0 + 32 * b + 31 > qw) || past_windows<WIN>(a, k0 + 32 * b, 32, qw)) {
             const int last = (a.causal ? min(qi, w.len - 1) : w.len - 1) - k0 - 32 * b - 4 * half;
-            const int first = WIN ? qi - (a.window - 1) - k0 - 32 * b - 4 * half : 0, few = WIN ? a.sinks - k0 - 32 * b - 4 * half : 0;
+            const Bounds bounds(a, w, qi, k0 + 32 * b + 4 * half);    // WIN
+            auto mask = [&](auto hidden) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int j = 8 * (r / 4) + r % 4;
-                s[0][r] = j > last || (WIN && j < first && j >= few) ? 0.f : s[0][r];
-            }
+                for (int r = 0; r < 16; ++r) s[0][r] = hidden(8 * (r / 4) + r % 4) ? 0.f : s[0][r];
+            };
+            if constexpr (!WIN) mask([&](int j) { return j > last; });
+            else if (k0 + 32 * b < a.sinks) mask([&](int j) { return bounds.hides_with_sinks(j); });
+            else mask([&](int j) { return bounds.hides(j); });
         }
         return s[0];
     };
@@ -1253,13 +1280,12 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : kTerms<T> == 3 ? 1 : wav
     AttnPiece piece{};
     int pieces = 1, slot = -1;
     if (past) {
-        if (blockIdx.y > 0) return;
         piece = sink_piece(a, blockIdx.x / a.kv_heads);
         const AttnSink sink = sink_tile(a, piece.sink);
         if (!sink_slots(a, sink) || piece.piece < 0 || piece.piece >= sink.pieces || piece.slot != sink.tile.zero + piece.piece) return;
         tile = sink.tile;
-        pieces = sink.pieces;
-        slot = piece.slot;
+        pieces = sink.pieces * a.splits;
+        slot = piece.slot * a.splits + blockIdx.y;
     } else {
         tile = a.tiles[a.num_tiles + block / a.kv_heads];
         if (WIN && a.splits == 1 && tile.zero > 0) {
@@ -1291,13 +1317,16 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : kTerms<T> == 3 ? 1 : wav
     const int all = per * group;
     int beg = (int)((int64_t)all * share / a.splits), steps = (int)((int64_t)all * (share + 1) / a.splits);
     if (past) {
-        const PieceSteps p = piece_steps(tile, a.window, pieces, piece.piece, group, BM);
+        const PieceSteps p = piece_steps(tile, a.window, pieces, piece.piece * a.splits + share, group, BM);
         first = p.first;
         per = p.per;
         beg = p.from;
         steps = p.to;
     }
     const float c2 = a.scale * kLog2e;
+    // WIN: the lane's key is seen by `reach` queries of this block from `base` on.
+    const int base = past ? ki + min(a.window, w.len - ki) : ki;
+    const uint32_t reach = !live ? 0 : past ? (ki < a.sinks ? w.len - base : 0) : min(a.window, w.len - ki);
 
     f32x16 gk[DT] = {}, gv[DT] = {};
     // A step's queries, their log-sum-exps and deltas; fp32: the tile on its way.
@@ -1364,14 +1393,12 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : kTerms<T> == 3 ? 1 : wav
             if (WIN) edge |= past ? qb - (kw + 31) < a.window || kw + 31 >= a.sinks : qb + 31 - kw >= a.window;
             const int from = a.causal ? ki : 0;
             auto hidden = [&](int row) {
-                if constexpr (WIN)
-                    return row >= w.len || (past ? row - ki < a.window || ki >= a.sinks : row < ki || row - ki >= a.window);
+                if constexpr (WIN) return (uint32_t)(row - base) >= reach;
                 return row < from || row >= w.len;
             };
             if (edge) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (hidden(qb + 8 * (r / 4) + 4 * half + r % 4)) p[r] = 0.f;
+                for (int r = 0; r < 16; ++r) p[r] = hidden(qb + 8 * (r / 4) + 4 * half + r % 4) ? 0.f : p[r];
             }
             accumulate<T, DP>(gv, ds, 32 * b, p, ln);
             if constexpr (HELD) {
@@ -1387,8 +1414,7 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : kTerms<T> == 3 ? 1 : wav
             }
             if (edge) {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (hidden(qb + 8 * (r / 4) + 4 * half + r % 4)) dp[r] = 0.f;
+                for (int r = 0; r < 16; ++r) dp[r] = hidden(qb + 8 * (r / 4) + 4 * half + r % 4) ? 0.f : dp[r];
             }
             accumulate<T, DP>(gk, qs, 32 * b, dp, ln);
         }
@@ -1399,7 +1425,7 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : kTerms<T> == 3 ? 1 : wav
     if (WIN && slot >= 0 && (past || kw < a.sinks)) {
         if (kw < a.sinks) {
             const int64_t one = (int64_t)a.kv_heads * a.sink_rows * DP;
-            float* part = a.first_keys + 2 * slot * one + ((int64_t)kv * a.sink_rows + kw - kt) * DP;
+            float* part = a.first_keys + 2 * (int64_t)slot * one + ((int64_t)kv * a.sink_rows + kw - kt) * DP;
             store_rows<float, DP, true>(mine, part, DP, gk, a.scale, a.dim, keep, lane);
             store_rows<float, DP, true>(mine, part + one, DP, gv, 1.f, a.dim, keep, lane);
         }
@@ -1483,14 +1509,14 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a) {
         }
         if (WIN && has_sinks && ki / 32 * 32 < a.sinks) {
             const int64_t many = (int64_t)a.kv_heads * a.sink_rows * DP;
-            const float* part = a.first_keys + 2 * sink.tile.zero * many + ((int64_t)kv * a.sink_rows + ki - kt) * DP + d;
+            const float* part = a.first_keys + 2 * (int64_t)sink.tile.zero * a.splits * many + ((int64_t)kv * a.sink_rows + ki - kt) * DP + d;
             if (sinks_only) {
                 gk = *reinterpret_cast<const f32x4*>(part + 2 * sink.pieces * many);
                 gv = *reinterpret_cast<const f32x4*>(part + (2 * sink.pieces + 1) * many);
             }
             if (ki < a.sinks)
 #pragma unroll 4
-                for (int s = 0; s < sink.pieces; ++s) {
+                for (int s = 0; s < sink.pieces * a.splits; ++s) {
                     gk += *reinterpret_cast<const f32x4*>(part + 2 * s * many);
                     gv += *reinterpret_cast<const f32x4*>(part + (2 * s + 1) * many);
                 }

@@ -38,7 +38,8 @@ constexpr KeyWalk key_walk(int q0, int end, int window, int sinks, int bn) {
 // With a window, what follows a plan's 2 x tiles entries: for each key tile with keys that
 // queries past their windows see (sinks) an AttnSink, and for each piece of those queries
 // an AttnPiece.  The key tile's own entry then has 1 + the number of its AttnSink for zero.
-// Sums of a piece go to its slot; those of the tile's windows to the slot behind its last.
+// Sums of a piece go to its slot (each share of it, as of any block, to one of its own); those of
+// the tile's windows to the slot behind its last, where there is one share.
 struct AttnSink { AttnTile tile; int32_t pieces, zero[3]; };      // tile.zero: the first piece's slot
 struct AttnPiece { int32_t sink, piece, slot, zero; };
 

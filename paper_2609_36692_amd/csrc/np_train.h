@@ -40,7 +40,7 @@ struct AttnArgs {
     int window, sinks;
     int sink_tiles, sink_pieces;    // entries of the plan behind its tiles (AttnSink, AttnPiece)
     int sink_rows;              // rows of a key tile that may be sinks, whole waves: 32 .. 128
-    float* first_keys;          // [sink_pieces + sink_tiles][2][kv_heads][sink_rows][64 or 128]
+    float* first_keys;          // [sink_pieces + sink_tiles][splits][2][kv_heads][sink_rows][64 or 128]
 };
 
 // Shares into which the dk/dv pass cuts the queries of a key, and the floats of
@@ -52,7 +52,7 @@ hipError_t launch_attention_backward(DType t, const AttnArgs& a, hipStream_t s);
 
 // The same with a sliding window; the workspace is that of a call without one, then
 // first_keys.
-int window_splits(const AttnArgs& a);
+int window_splits(DType t, const AttnArgs& a);
 hipError_t launch_window_forward(DType t, const AttnArgs& a, hipStream_t s);
 hipError_t launch_window_backward(DType t, const AttnArgs& a, hipStream_t s);
 

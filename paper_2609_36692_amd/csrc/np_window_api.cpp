@@ -36,7 +36,7 @@ int64_t piece_length(int64_t num_seqs, const int64_t* lens, int window, int sink
     int64_t all = 0;
     for (int64_t i = 0; i < num_seqs; ++i)
         for (int64_t k = 0; k * kAttnRows < std::min<int64_t>(lens[i], sinks); ++k) all += past(lens[i], k, window, sinks);
-    return std::max<int64_t>({(int64_t)window + kAttnRows, 512, (all + kMostPieces - 1) / kMostPieces});
+    return std::max<int64_t>({(int64_t)window + kAttnRows, 256, (all + kMostPieces - 1) / kMostPieces});
 }
 
 // f(first token, length, tile, pieces) of every sink tile.
@@ -66,19 +66,20 @@ int check_block(const normpre_attention* a, const normpre_window* w) {
 
 AttnArgs sizes(const normpre_attention* a, const normpre_window* w) {
     AttnArgs k = attention_sizes(a);
-    k.window = clipped(w->window);
-    k.sinks = clipped(w->sinks);
+    // No sequence is longer: larger numbers mean the same.
+    k.window = (int)std::clamp<int64_t>(w->window, 1, std::max<int64_t>(a->tokens, 1));
+    k.sinks = (int)std::min(w->sinks, a->tokens);
     k.sink_tiles = (int)w->sink_tiles;
     k.sink_pieces = (int)w->sink_pieces;
     k.sink_rows = sink_rows(k.sinks);
-    k.splits = window_splits(k);
+    k.splits = window_splits((DType)a->dtype, k);
     return k;
 }
 
 // Floats in front of first_keys, and of it.
 int64_t before(const AttnArgs& k) { return (attention_workspace(k) + 3) / 4 * 4; }
 int64_t first_keys(const AttnArgs& k) {
-    return 2 * ((int64_t)k.sink_pieces + k.sink_tiles) * k.kv_heads * k.sink_rows * (k.dim <= 64 ? 64 : 128);
+    return 2 * ((int64_t)k.sink_pieces + k.sink_tiles) * k.splits * k.kv_heads * k.sink_rows * (k.dim <= 64 ? 64 : 128);
 }
 
 int attention(const normpre_attention* a, const normpre_window* w, bool backward, void* stream) {

@@ -68,7 +68,7 @@ hipError_t launch_rope(DType, const RopeArgs& a, bool backward, hipStream_t) {
 }
 
 int attention_splits(int64_t, int) { return 2; }
-int window_splits(const AttnArgs&) { return 2; }
+int window_splits(DType, const AttnArgs&) { return 2; }
 int64_t attention_workspace(const AttnArgs& a) { return 2 * (int64_t)a.heads * a.tokens + 1; }
 hipError_t launch_window_forward(DType, const AttnArgs&, hipStream_t) { ++g_launches; return hipSuccess; }
 hipError_t launch_window_backward(DType, const AttnArgs& a, hipStream_t) {
@@ -115,7 +115,7 @@ static void window_calls(char* mem) {
     w = {5, 1, 1, 1};
     g_launches = 0;
     EXPECT(normpre_window_attention_workspace(&a, &w, &a.workspace_bytes), NORMPRE_OK);
-    EXPECT(a.workspace_bytes, 4 * ((2 * 4 * 300 + 1 + 3) / 4 * 4 + 2 * 2 * 2 * 32 * 64));
+    EXPECT(a.workspace_bytes, 4 * ((2 * 4 * 300 + 1 + 3) / 4 * 4 + 2 * 2 * 2 * 2 * 32 * 64));
     EXPECT(normpre_window_attention_forward(&a, &w, nullptr), NORMPRE_OK);
     EXPECT(normpre_window_attention_backward(&a, &w, nullptr), NORMPRE_ERR_HIP);
     EXPECT(g_launches, 2);

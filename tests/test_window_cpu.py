@@ -79,13 +79,13 @@ def test_plan_refusals(lib):
     assert sizes(2, (ctypes.c_int64 * 2)(1, -1), W(5, 5), n) == INVALID
     assert sizes(2, (ctypes.c_int64 * 2)(2 ** 31 - 1, 1), W(5, 5), n) == UNSUPPORTED
     w = W(5, 5)
-    assert sizes(2, ok, w, n) == 0 and (n.value, w.sink_tiles, w.sink_pieces) == (4, 2, 2)
+    assert sizes(2, ok, w, n) == 0 and (n.value, w.sink_tiles, w.sink_pieces) == (4, 2, 3)
     buf = (ctypes.c_int32 * 100)()
     plan = lib.normpre_window_attention_plan
-    need = 8 * 4 + 8 * 2 + 4 * 2
+    need = 8 * 4 + 8 * 2 + 4 * 3
     assert plan(2, ok, w, buf, need) == 0
     assert plan(2, ok, w, buf, need - 1) == INVALID and plan(2, ok, w, None, need) == INVALID
-    assert plan(2, ok, W(5, 5, 1, 1), buf, need) == INVALID and plan(2, ok, W(0, 5, 2, 2), buf, need) == INVALID
+    assert plan(2, ok, W(5, 5, 1, 1), buf, need) == INVALID and plan(2, ok, W(0, 5, 2, 3), buf, need) == INVALID
     assert plan(2, ok, None, buf, need) == INVALID
     assert plan(1, ok, w, buf, need) == INVALID      # another batch's
 
@@ -122,8 +122,8 @@ def test_backward_refusals_and_workspace(lib):
     w, n = W(5, 1, 1, 1), ctypes.c_int64()
     assert lib.normpre_window_attention_workspace(_block(), w, n) == 0
     need = n.value
-    # Statistics, four shares of dk and dv, and the sums of two slots of 32 rows.
-    assert need == 4 * (2 * 4 * 300 + 2 * 4 * 2 * 300 * 64 + 2 * 2 * 2 * 32 * 64)
+    # Statistics, four shares of dk and dv, and the sums of two slots of 32 rows, four shares each.
+    assert need == 4 * (2 * 4 * 300 + 2 * 4 * 2 * 300 * 64 + 2 * 4 * 2 * 2 * 32 * 64)
     assert lib.normpre_window_attention_workspace(_block(), None, n) == INVALID
     assert lib.normpre_window_attention_workspace(None, w, n) == INVALID
     assert lib.normpre_window_attention_workspace(_block(), w, None) == INVALID
