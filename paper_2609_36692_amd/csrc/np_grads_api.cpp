@@ -69,7 +69,7 @@ int check_apart(int64_t num, const normpre_grad* g) {
 // f(list) for every launch's list of tensors; the number of launches (at most
 // 2^40 / 2^29 + 2^20 pieces of tensors: fewer than there are partial sums).
 template <class F>
-int64_t lists(int64_t num, const normpre_grad* g, bool scale, F f) {
+int64_t lists(int64_t num, const normpre_grad* g, bool scale, uint32_t chunk, F f) {
     GradList l;
     int64_t launches = 0;
     l.count = 0;
@@ -88,7 +88,7 @@ int64_t lists(int64_t num, const normpre_grad* g, bool scale, F f) {
                         (g[i].out_dtype == NORMPRE_DTYPE_BF16 ? kGradOutBf16 : 0);
             l.in[k] = static_cast<const char*>(g[i].grad) + at * size_of(g[i].dtype);
             l.out[k] = scale ? static_cast<char*>(g[i].out) + at * size_of(g[i].out_dtype) : nullptr;
-            l.first[k + 1] = l.first[k] + (n + kGradChunk - 1) / kGradChunk;
+            l.first[k + 1] = l.first[k] + (n + chunk - 1) / chunk;
             if (l.count == kGradList) flush();
         }
     flush();
@@ -107,21 +107,34 @@ int grads(int64_t num, const normpre_grad* g, bool scale, double max_norm, float
     } catch (const std::bad_alloc&) {
         return fail(NORMPRE_ERR_OOM, "no memory to check the gradients");
     }
+    if (!scale) max_norm = INFINITY;
+    // Few elements: one launch of one block instead of three.
+    int64_t few = 0;
+    bool some = false;
+    for (int64_t i = 0; i < num && few <= kGradSmallChunks; ++i) {
+        few += std::min<int64_t>((g[i].count + kGradSmallChunk - 1) / kGradSmallChunk, kGradSmallChunks + 1);
+        some |= g[i].count > 0;
+    }
+    if (few <= kGradSmallChunks && some) {
+        hipError_t e = hipSuccess;
+        lists(num, g, scale, kGradSmallChunk, [&](const GradList& l) { e = launch_grad_small(l, max_norm, norm, scale, stream); });
+        return launched(e);
+    }
     double* work = static_cast<double*>(workspace);
     // Blocks of a launch: all of them hold a partial sum.
-    const int64_t launches = lists(num, g, scale, [](const GradList&) {});
+    const int64_t launches = lists(num, g, scale, kGradChunk, [](const GradList&) {});
     const int most = (int)std::min<int64_t>(kGradBlocks, kGradPartials / std::max<int64_t>(launches, 1));
     auto blocks = [&](const GradList& l) { return (int)std::min<int64_t>(l.first[l.count], most); };
     int partials = 0;
     hipError_t e = hipSuccess;
-    lists(num, g, scale, [&](const GradList& l) {
+    lists(num, g, scale, kGradChunk, [&](const GradList& l) {
         if (e != hipSuccess) return;
         e = launch_grad_squares(l, blocks(l), work + kGradHead + partials, stream);
         partials += blocks(l);
     });
-    if (e == hipSuccess) e = launch_grad_total(work, partials, scale ? max_norm : INFINITY, norm, stream);
+    if (e == hipSuccess) e = launch_grad_total(work, partials, max_norm, norm, stream);
     if (scale)
-        lists(num, g, scale, [&](const GradList& l) {
+        lists(num, g, scale, kGradChunk, [&](const GradList& l) {
             if (e == hipSuccess) e = launch_grad_scale(l, blocks(l), work, stream);
         });
     return launched(e);

@@ -633,15 +633,22 @@ def _grad_list(grads: Iterable[torch.Tensor]) -> list[torch.Tensor]:
 
 
 def _grad_entries(grads, outs) -> tuple[int, array]:
-    """(device index, the C ABI's list of gradients)."""
-    if not grads[0].is_cuda:
+    """(device index, the C ABI's list of gradients).  Hundreds of tensors a step: a
+    pass over them for each thing that is asked of them."""
+    at = grads[0].get_device()
+    if at < 0:
         raise ValueError("expected tensors on a GPU")
-    at, block = grads[0].get_device(), array("Q")
-    for g, o in zip(grads, outs):
-        if g.get_device() != at or o.get_device() != at:
-            raise ValueError(f"gradients lie on different devices: {g.device}, {o.device} and cuda:{at}")
-        block.extend((g.data_ptr(), o.data_ptr(), g.numel(), _dtype(g) | _dtype(o) << 32))
-    return at, block
+    kinds, places, sizes = [_DTYPES.get(g.dtype) for g in grads], [g.data_ptr() for g in grads], [g.numel() for g in grads]
+    devices = {g.get_device() for g in grads}
+    to, into = kinds, places
+    if outs is not grads:
+        to, into = [_DTYPES.get(o.dtype) for o in outs], [o.data_ptr() for o in outs]
+        devices |= {o.get_device() for o in outs}
+    if devices != {at}:
+        raise ValueError("gradients lie on different devices")
+    if None in kinds or None in to:
+        raise TypeError("expected bfloat16 or float32 gradients")
+    return at, array("Q", [x for e in zip(places, into, sizes, [a | b << 32 for a, b in zip(kinds, to)]) for x in e])
 
 
 def _grad_workspace(like: torch.Tensor):
@@ -665,6 +672,24 @@ def grad_norm(grads: Iterable[torch.Tensor] | torch.Tensor) -> torch.Tensor:
     return norm
 
 
+def _in_one_order(grads, outs):
+    """(gradients, outputs, pairs to copy afterwards), each gradient's elements in its
+    output's order in memory."""
+    sources, targets, back = [], [], []
+    for g, o in zip(grads, outs):
+        if not _dense(o) and any(st == 0 and n > 1 for st, n in zip(o.stride(), o.shape)):
+            raise ValueError("an output's elements share memory")
+        if _dense(g) and (g.stride() == o.stride() or (g.is_contiguous() and o.is_contiguous())):
+            sources.append(g)
+            targets.append(o)
+            continue
+        sources.append(g.contiguous())
+        targets.append(o if o.is_contiguous() else torch.empty_like(o, memory_format=torch.contiguous_format))
+        if not o.is_contiguous():
+            back.append((o, targets[-1]))
+    return sources, targets, back
+
+
 def clip_grads(grads: Iterable[torch.Tensor] | torch.Tensor, max_norm: float,
                out: Iterable[torch.Tensor] | torch.Tensor | None = None) -> torch.Tensor:
     """Scales the gradients by max_norm / norm where their norm (``grad_norm``, which
@@ -681,18 +706,9 @@ def clip_grads(grads: Iterable[torch.Tensor] | torch.Tensor, max_norm: float,
         raise ValueError("out has the gradients' number and shapes")
     if not grads:
         return torch.zeros(())
-    sources, targets, back = [], [], []
-    for g, o in zip(grads, outs):
-        if not _dense(o) and any(st == 0 and n > 1 for st, n in zip(o.stride(), o.shape)):
-            raise ValueError("an output's elements share memory")
-        if _dense(g) and (g.stride() == o.stride() or (g.is_contiguous() and o.is_contiguous())):
-            sources.append(g)
-            targets.append(o)
-            continue
-        sources.append(g.contiguous())
-        targets.append(o if o.is_contiguous() else torch.empty_like(o, memory_format=torch.contiguous_format))
-        if not o.is_contiguous():
-            back.append((o, targets[-1]))
+    sources, targets, back = grads, outs, []
+    if not (all(g.is_contiguous() for g in grads) and (out is None or all(o.is_contiguous() for o in outs))):
+        sources, targets, back = _in_one_order(grads, outs)
     at, block = _grad_entries(sources, targets)
     if _elsewhere(at):
         with torch.cuda.device(at):

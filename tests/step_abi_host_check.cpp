@@ -29,22 +29,30 @@ static double* g_work;
 namespace np {
 int set_thread_error(int code, const char* msg) { g_error = msg; return code; }
 
-static long long elements(const GradList& l, int blocks) {
+static long long elements(const GradList& l, int blocks, uint32_t chunk) {
     EXPECT(l.count >= 1 && l.count <= kGradList, 1);
     EXPECT(l.first[0], 0);
     long long n = 0;
     for (int i = 0; i < l.count; ++i) {
         const uint32_t size = l.size[i] & (kGradInBf16 - 1);
         EXPECT(size >= 1 && size <= kGradMost, 1);
-        EXPECT(l.first[i + 1] - l.first[i], (size + kGradChunk - 1) / kGradChunk);
+        EXPECT(l.first[i + 1] - l.first[i], (size + chunk - 1) / chunk);
         n += size;
     }
     EXPECT(blocks >= 1 && blocks <= kGradBlocks && (uint32_t)blocks <= l.first[l.count], 1);
     ++g_launches;
     return n;
 }
+hipError_t launch_grad_small(const GradList& l, double, float*, bool scale, hipStream_t) {
+    const long long n = elements(l, 1, kGradSmallChunk);
+    EXPECT(l.first[l.count] <= kGradSmallChunks, 1);
+    g_squares += n;
+    if (scale) g_scaled += n;
+    g_total_of = g_partials;
+    return hipSuccess;
+}
 hipError_t launch_grad_squares(const GradList& l, int blocks, double* partial, hipStream_t) {
-    g_squares += elements(l, blocks);
+    g_squares += elements(l, blocks, kGradChunk);
     EXPECT(partial - g_work, kGradHead + g_partials);    // one block's behind the other's
     g_partials += blocks;
     EXPECT(g_partials <= kGradPartials, 1);
@@ -56,7 +64,7 @@ hipError_t launch_grad_total(double* work, int partials, double, float*, hipStre
     return hipSuccess;
 }
 hipError_t launch_grad_scale(const GradList& l, int blocks, const double*, hipStream_t) {
-    g_scaled += elements(l, blocks);
+    g_scaled += elements(l, blocks, kGradChunk);
     return hipSuccess;
 }
 
@@ -204,12 +212,12 @@ int main() {
     const int64_t ws = NORMPRE_GRAD_WORKSPACE_BYTES;
 
     // Tensors of one element, of several pieces, of none; more than a launch holds.
-    for (int64_t count : {0, 1, 151, 152, 153, 5000, 1 << 20}) {
+    for (int64_t count : {0, 1, 3, 40, 60, 151, 152, 153, 5000, 1 << 20}) {
         std::vector<normpre_grad> g(count);
         long long all = 0;
         char* at = far;
         for (int64_t i = 0; i < count; ++i) {
-            const int64_t n = i == 3 ? (int64_t(1) << 32) + 5 : i % 7 == 5 ? 0 : i % 100 + 1;
+            const int64_t n = i == 3 && count != 40 ? (int64_t(1) << 32) + 5 : i % 7 == 5 ? 0 : i % 100 + 1;
             g[i] = {at, at, n, (int)(i % 2), (int)(i % 2)};
             at += 4 * n;
             all += n;
