@@ -654,7 +654,7 @@ typedef struct normpre_qk_rope {
     int32_t adjacent;           /* 0 or 1                                        */
     int32_t norm;               /* 0 or 1                                        */
     int32_t weight_dtype;       /* NORMPRE_DTYPE_*, of q_weight and k_weight     */
-    int32_t num_axes;           /* rows of positions                             */
+    int32_t num_axes;           /* rows of positions, up to 256                  */
     int32_t position_bytes;     /* 4 or 8: int32 or int64                        */
     double  eps;                /* finite, >= 0                                  */
     int64_t tokens;
@@ -674,15 +674,16 @@ typedef struct normpre_qk_rope {
     int64_t workspace_bytes;    /* normpre_qk_rope_workspace() bytes or more     */
 } normpre_qk_rope;
 
-/* Workspace bytes of a backward call (0 where no weight gradient is wanted); reads
- * the sizes, norm, dq_weight and dk_weight of *a.  Host only. */
+/* Workspace bytes of a backward call: 0 where no weight gradient is wanted, and never
+ * more than 4096 head_dim.  Reads the sizes, norm, axes, dq_weight and dk_weight of *a.
+ * Host only. */
 int normpre_qk_rope_workspace(const normpre_qk_rope* a, int64_t* bytes);
 /*
  * tokens = 0: nothing but zero weight gradients is written.
  * Errors: INVALID_ARG (null or misaligned pointers, unknown dtypes, counts, flags or
  * eps out of their ranges, negative strides, an output whose rows overlap, too small
- * a workspace), UNSUPPORTED (head_dim > 256, more than 2^16 heads, 2^31 tokens,
- * strides above 2^40), HIP.
+ * a workspace), UNSUPPORTED (head_dim > 256, more than 2^16 heads or 256 axes, 2^31
+ * tokens, strides above 2^40), HIP.
  */
 int normpre_qk_rope_forward(const normpre_qk_rope* a, void* stream);
 int normpre_qk_rope_backward(const normpre_qk_rope* a, void* stream);

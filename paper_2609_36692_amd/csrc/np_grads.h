@@ -13,7 +13,7 @@ namespace np {
 // and a captured launch keeps its own.  Chunks first[i] .. first[i + 1] - 1 are those
 // of tensor i; size: elements, at most kGradMost, and the two flags below.
 constexpr int kGradList = 152;
-constexpr uint32_t kGradChunk = 8192, kGradSmallChunk = 2048;
+constexpr uint32_t kGradChunk = 4096, kGradScaleChunk = 8192, kGradSmallChunk = 2048;
 constexpr uint32_t kGradMost = 1u << 29;            // a multiple of the chunk
 constexpr uint32_t kGradInBf16 = 1u << 30, kGradOutBf16 = 1u << 31;
 

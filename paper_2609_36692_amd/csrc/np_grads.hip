@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kTotalThreads) grad_total_kernel(double* work,
 __global__ void __launch_bounds__(kThreads) grad_scale_kernel(GradList l, const double* work) {
     const uint32_t all = l.first[l.count];
     const double f = work[0];
-    for (uint32_t c = blockIdx.x; c < all; c += gridDim.x) scale_of<kThreads, kGradChunk>(l, all - 1 - c, f);
+    for (uint32_t c = blockIdx.x; c < all; c += gridDim.x) scale_of<kThreads, kGradScaleChunk>(l, all - 1 - c, f);
 }
 
 // Norm and scaling of few elements in one block: chunks go to its waves in turn.

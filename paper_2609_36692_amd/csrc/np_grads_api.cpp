@@ -134,7 +134,7 @@ int grads(int64_t num, const normpre_grad* g, bool scale, double max_norm, float
     });
     if (e == hipSuccess) e = launch_grad_total(work, partials, max_norm, norm, stream);
     if (scale)
-        lists(num, g, scale, kGradChunk, [&](const GradList& l) {
+        lists(num, g, scale, kGradScaleChunk, [&](const GradList& l) {
             if (e == hipSuccess) e = launch_grad_scale(l, blocks(l), work, stream);
         });
     return launched(e);

@@ -8,6 +8,7 @@ namespace np {
 
 constexpr int kRopeMaxDim = 256;
 constexpr int kRopeMaxHeads = 1 << 16;
+constexpr int kRopeMaxAxes = 256;
 
 struct RopeArgs {                  // [2]: queries, keys
     AttnOperand x[2];              // forward, and backward with norm: read
@@ -27,7 +28,9 @@ struct RopeArgs {                  // [2]: queries, keys
     float* partial;                // [blocks][2][dim], where dw is wanted
 };
 
-// Floats of workspace that a backward call needs: where weight gradients are wanted.
+// Floats of workspace that a backward call needs: where weight gradients are wanted, 2 dim
+// for each of up to kRopeMostSums blocks.
+constexpr int kRopeMostSums = 512;
 int64_t rope_workspace(DType t, const RopeArgs& a);
 inline bool rope_sums(const RopeArgs& a) { return a.norm && (a.dw[0] || a.dw[1]); }
 hipError_t launch_rope(DType t, const RopeArgs& a, bool backward, hipStream_t s);

@@ -39,10 +39,13 @@ RopeArgs sizes(const normpre_qk_rope* a) {
     k.weight_bf16 = a->weight_dtype == NORMPRE_DTYPE_BF16;
     k.eps = a->eps;
     k.tokens = a->tokens;
+    k.axis = a->pairs > 0 ? a->axes : nullptr;
     k.dw[0] = a->dq_weight;
     k.dw[1] = a->dk_weight;
     return k;
 }
+
+static_assert(4 * 2 * kRopeMostSums == 4096, "the header's bound");
 
 int rope(const normpre_qk_rope* a, bool backward, void* stream) {
     NP_CHECK(check_sizes(a));
@@ -57,6 +60,7 @@ int rope(const normpre_qk_rope* a, bool backward, void* stream) {
             if (!a->freqs || !on(a->freqs, 8)) return bad("freqs is null or misaligned");
             if (a->axes && !on(a->axes, 4)) return bad("axes is misaligned");
             if (a->num_axes < 1) return bad("num_axes < 1");
+            if (a->num_axes > kRopeMaxAxes) return fail(NORMPRE_ERR_UNSUPPORTED, "more than %d axes", kRopeMaxAxes);
             if (a->position_bytes != 4 && a->position_bytes != 8) return bad("positions have 4 or 8 bytes");
             if (!a->positions || !on(a->positions, a->position_bytes)) return bad("positions is null or misaligned");
             if (a->position_stride < 0) return bad("position_stride < 0");
@@ -88,7 +92,6 @@ int rope(const normpre_qk_rope* a, bool backward, void* stream) {
         k.w[1] = a->k_weight;
     }
     k.freqs = a->freqs;
-    k.axis = a->axes;
     k.axes = a->num_axes;
     k.positions = a->positions;
     k.positions_64 = a->position_bytes == 8;

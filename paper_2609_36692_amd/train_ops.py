@@ -239,31 +239,41 @@ class Rotary:
 _ROPE = struct.Struct("=10idq" + "3Qq" + "2Q" + "Q2q" * 6 + "2Q" + "Qq")
 
 
+def _norm_weight(w: torch.Tensor, dim: int, at: int) -> int:
+    if w.shape != (dim,) or w.get_device() != at or not w.is_contiguous():
+        raise ValueError(f"a weight is a contiguous [{dim}] tensor on cuda:{at}, got {tuple(w.shape)} on {w.device}")
+    return _dtype(w)
+
+
 def _rope_args(q, k, positions, rotary: Rotary | None, norm, q_weight, k_weight, eps):
     """(device index, the fields up to k_weight); checks the operands."""
     tokens, heads, dim = q.shape
-    if k.shape[0] != tokens or k.shape[2] != dim:
-        raise ValueError(f"expected q [tokens, heads, dim] and k [tokens, kv_heads, dim], got {tuple(q.shape)}, {tuple(k.shape)}")
+    ks = k.shape
+    if ks[0] != tokens or ks[2] != dim:
+        raise ValueError(f"expected q [tokens, heads, dim] and k [tokens, kv_heads, dim], got {tuple(q.shape)}, {tuple(ks)}")
     at = _same(q, k)
-    weights = [w for w in (q_weight, k_weight) if w is not None]
-    if weights and not norm:
+    kind = qw = kw = 0
+    if q_weight is not None:
+        kind, qw = _norm_weight(q_weight, dim, at), q_weight.data_ptr()
+    if k_weight is not None:
+        other, kw = _norm_weight(k_weight, dim, at), k_weight.data_ptr()
+        if q_weight is not None and other != kind:
+            raise ValueError("the weights have one type")
+        kind = other
+    if (qw or kw) and not norm:
         raise ValueError("weights are the norm's")
-    for w in weights:
-        if w.shape != (dim,) or w.dtype != weights[0].dtype or w.get_device() != at or not w.is_contiguous():
-            raise ValueError(f"a weight is a contiguous [{dim}] tensor on {q.device}, of the other's type")
-    turn = (0, 0, 0, 0)
-    if rotary is not None:
-        if positions is None or positions.dtype not in (torch.int32, torch.int64) or positions.get_device() != at \
-                or positions.shape not in ((rotary.num_axes, tokens), *(((tokens,),) if rotary.num_axes == 1 else ())):
-            raise ValueError(f"positions are int32 or int64 [{rotary.num_axes}, {tokens}] on {q.device}")
-        if rotary.freqs.get_device() != at:
-            raise ValueError("the rotary lies on another device")
-        turn = (rotary.freqs.data_ptr(), 0 if rotary.axes is None else rotary.axes.data_ptr(), positions.data_ptr(),
-                positions.stride(0) if positions.dim() == 2 else 0)
-    return at, (_dtype(q), heads, k.shape[1], dim, 0 if rotary is None else rotary.pairs,
-                int(rotary is not None and rotary.adjacent), int(bool(norm)), _dtype(weights[0]) if weights else 0,
-                1 if rotary is None else rotary.num_axes, 4 if positions is None else positions.element_size(),
-                float(eps), tokens, *turn, *(0 if w is None else w.data_ptr() for w in (q_weight, k_weight)))
+    if rotary is None:
+        return at, (_dtype(q), heads, ks[1], dim, 0, 0, int(bool(norm)), kind, 1, 4, float(eps), tokens, 0, 0, 0, 0, qw, kw)
+    axes = rotary.num_axes
+    if positions is None or positions.dtype not in (torch.int32, torch.int64) or positions.get_device() != at \
+            or not (positions.shape == (axes, tokens) or (axes == 1 and positions.shape == (tokens,))):
+        raise ValueError(f"positions are int32 or int64 [{axes}, {tokens}] on {q.device}")
+    if rotary.freqs.get_device() != at:
+        raise ValueError("the rotary lies on another device")
+    return at, (_dtype(q), heads, ks[1], dim, rotary.pairs, int(rotary.adjacent), int(bool(norm)), kind, axes,
+                positions.element_size(), float(eps), tokens, rotary.freqs.data_ptr(),
+                0 if rotary.axes is None else rotary.axes.data_ptr(), positions.data_ptr(),
+                positions.stride(0) if axes > 1 else 0, qw, kw)
 
 
 def _positions(positions: torch.Tensor | None) -> torch.Tensor | None:
@@ -307,16 +317,17 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.T
             return qk_norm_rope_backward(dq_out, dk_out, q, k, positions, rotary, norm=norm, q_weight=q_weight,
                                          k_weight=k_weight, eps=eps)
     dq, dk = q.new_empty(q.shape), k.new_empty(k.shape)
-    dw = [None if w is None else w.new_empty(w.shape, dtype=torch.float32) for w in (q_weight, k_weight)]
-    block = N.normpre_qk_rope.from_buffer_copy(_ROPE.pack(
-        *args, *_heads(q), *_heads(k), *_heads(dq_out), *_heads(dk_out), *_heads(dq), *_heads(dk),
-        *(0 if w is None else w.data_ptr() for w in dw), 0, 0))
+    dwq = dwk = None
+    ends = (0, 0, 0, 0)
     if q_weight is not None or k_weight is not None:
-        block.workspace_bytes = N.normpre_qk_rope_workspace(block)
-        work = dq.new_empty(block.workspace_bytes, dtype=torch.uint8)
-        block.workspace = work.data_ptr()
-    N.normpre_qk_rope_backward(block, _stream(at))
-    return dq, dk, *dw
+        dim = q.shape[2]
+        work = q.new_empty(1024 * dim, dtype=torch.float32)      # the bound: the size itself is not worth a call
+        dwq = None if q_weight is None else work.new_empty(dim)
+        dwk = None if k_weight is None else work.new_empty(dim)
+        ends = (0 if dwq is None else dwq.data_ptr(), 0 if dwk is None else dwk.data_ptr(), work.data_ptr(), 4096 * dim)
+    N.normpre_qk_rope_backward(N.normpre_qk_rope.from_buffer_copy(_ROPE.pack(
+        *args, *_heads(q), *_heads(k), *_heads(dq_out), *_heads(dk_out), *_heads(dq), *_heads(dk), *ends)), _stream(at))
+    return dq, dk, dwq, dwk
 
 
 class _QkNormRope(torch.autograd.Function):

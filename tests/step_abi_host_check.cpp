@@ -64,7 +64,7 @@ hipError_t launch_grad_total(double* work, int partials, double, float*, hipStre
     return hipSuccess;
 }
 hipError_t launch_grad_scale(const GradList& l, int blocks, const double*, hipStream_t) {
-    g_scaled += elements(l, blocks, kGradChunk);
+    g_scaled += elements(l, blocks, kGradScaleChunk);
     return hipSuccess;
 }
 

@@ -42,7 +42,7 @@ def _block(**over):
     (True, {"norm": 2}, INVALID), (True, {"weight_dtype": 7}, INVALID), (True, {"eps": -1e-9}, INVALID),
     (True, {"eps": float("nan")}, INVALID), (True, {"eps": float("inf")}, INVALID), (True, {"tokens": -1}, INVALID),
     (True, {"tokens": 1 << 31}, UNSUPPORTED), (True, {"freqs": None}, INVALID), (True, {"freqs": P + 4}, INVALID),
-    (True, {"axes": P + 2}, INVALID), (True, {"num_axes": 0}, INVALID), (True, {"position_bytes": 2}, INVALID),
+    (True, {"axes": P + 2}, INVALID), (True, {"num_axes": 0}, INVALID), (True, {"num_axes": 257}, UNSUPPORTED), (True, {"position_bytes": 2}, INVALID),
     (True, {"positions": None}, INVALID), (True, {"positions": P + 4, "position_bytes": 8}, INVALID),
     (True, {"position_stride": -1}, INVALID), (True, {"position_stride": 1 << 41}, UNSUPPORTED),
     (True, {"q": H(None, 256, 64)}, INVALID), (True, {"k": H(P + 1, 128, 64)}, INVALID), (True, {"k": H(P, -1, 64)}, INVALID),
