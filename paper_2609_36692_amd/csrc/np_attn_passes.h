@@ -26,6 +26,8 @@
 // that every result is summed by one wave in one order, without atomics and
 // without an array of partial dq.
 //
+// WIN: with a sliding window and first tokens that stay visible (np_attn_window.hip).
+//
 // Measured (one MI355X, where a library product of 8192^3 reaches 1263 TFLOP/s in
 // bf16, 154 in fp32), causal, flops of the visible pairs:
 //   16384 tokens, 16/8 heads of 128, bf16: forward 1095-1165 us from card to card,

@@ -1,5 +1,18 @@
 // Packed attention with a sliding window and first tokens that stay visible (sinks):
-// which form of the passes (np_attn_passes.h) a call takes.
+// query i sees the keys j <= i of its sequence with j > i - window or j < sinks.  The
+// passes are those without a window (np_attn_passes.h, WIN): blocks of 128 queries go
+// through the tiles of the first keys and then those from their first query's window on,
+// blocks of 128 keys through the queries whose windows reach them, so that work grows with
+// tokens x (window + sinks).  A block meets up to 127 rows more than each of its rows sees,
+// and masks them on both sides.
+//
+// Measured (bf16, 16/8 heads of 128, window 1024, 4 first tokens; flops of the visible
+// pairs): forward, 16964 tokens, 187-200 us (675-720 TFLOP/s); packed 15932 tokens: forward 165 us
+// (700), dq 228 (760), dk/dv 357 (650).  Matrix instructions take 31 to 38% of the cycles, vector ones
+// 41 to 56%.  What is lost against long causal rows (940-1000): the masked 11% of the pairs,
+// each block's start and end over 19 tiles instead of a hundred, and the last round of
+// blocks (2160 on 512 places; dk/dv: 1112, 2.2 rounds that take three).
+// 4 x 1024 tokens, fp32, 12 heads of 64, window 256: forward 40 us, dq 55, dk/dv 91.
 #include "np_attn_passes.h"
 
 namespace np {

@@ -7,12 +7,13 @@
 
 namespace np {
 
-// Tensors of one launch, cut into chunks of kGradChunk (or
-// kGradSmallChunk) elements; the list travels as
-// the kernel's argument (4 KB with what the compiler adds), so no table is copied to the device
-// and a captured launch keeps its own.  Chunks first[i] .. first[i + 1] - 1 are those
+// Tensors of one launch, cut into chunks; the list travels as the kernel's argument (4 KB
+// with what the compiler adds), so no table is copied to the device and a captured launch
+// keeps its own.  Chunks first[i] .. first[i + 1] - 1 are those
 // of tensor i; size: elements, at most kGradMost, and the two flags below.
 constexpr int kGradList = 152;
+// us with chunks of 8192 / 4096 / 2048 for the sum (scaling: 8192): 124 M fp32 elements 285 / 269 / 275, 1.41 G
+// bf16 2134 / 2060 / 2267; scaling in chunks of 16384: 265, 2197.
 constexpr uint32_t kGradChunk = 4096, kGradScaleChunk = 8192, kGradSmallChunk = 2048;
 constexpr uint32_t kGradMost = 1u << 29;            // a multiple of the chunk
 constexpr uint32_t kGradInBf16 = 1u << 30, kGradOutBf16 = 1u << 31;

@@ -209,8 +209,9 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: Attention
 class Rotary:
     """How heads turn with their positions: made once, used by every layer.
 
-    freqs: radians a step of each turning pair of features (numbers, kept in 64
-    bits); the first 2 * len(freqs) features of a head turn, the others stay.
+    freqs: radians a step of each turning pair of features (finite numbers, kept in
+    64 bits); the first 2 * len(freqs) features of a head turn, the others stay.
+    Angles (position * frequency) are exact to 2^-52 of their size, for up to 2^51.
     axes: the axis of positions that each pair turns by (default: all by the
     first).  adjacent: pair i is features (2i, 2i + 1); else (i, i + len(freqs)).
     """
@@ -218,6 +219,8 @@ class Rotary:
     def __init__(self, freqs: Sequence[float], axes: Sequence[int] | None = None, adjacent: bool = False,
                  device="cuda"):
         freqs = [float(f) for f in freqs]
+        if not all(map(math.isfinite, freqs)):
+            raise ValueError("a frequency is not finite")
         self.pairs, self.adjacent, self.num_axes = len(freqs), bool(adjacent), 1
         if axes is not None:
             axes = [int(a) for a in axes]
@@ -305,8 +308,8 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.T
                           q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None,
                           eps: float = 1e-6):
     """(dq, dk, dq_weight, dk_weight) from the gradients of ``qk_norm_rope_forward``'s
-    outputs and what that call took; the weights' in fp32, None where there is no
-    weight."""
+    outputs and what that call took (without ``norm`` the shapes of q and k alone); the
+    weights' in fp32, None where there is no weight."""
     if dq_out.shape != q.shape or dk_out.shape != k.shape:
         raise ValueError("gradients have the shapes of q and k")
     q, k, dq_out, dk_out, positions = _rows(q), _rows(k), _rows(dq_out), _rows(dk_out), _positions(positions)
@@ -333,7 +336,8 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.T
 class _QkNormRope(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, positions, rotary, norm, q_weight, k_weight, eps):
-        ctx.save_for_backward(q, k, positions, q_weight, k_weight)
+        # Without norms the gradients need nothing of q and k.
+        ctx.save_for_backward(q if norm else None, k if norm else None, positions, q_weight, k_weight)
         ctx.rotary, ctx.how = rotary, {"norm": norm, "eps": eps}
         return qk_norm_rope_forward(q, k, positions, rotary, norm=norm, q_weight=q_weight, k_weight=k_weight, eps=eps)
 
@@ -341,6 +345,8 @@ class _QkNormRope(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dq_out, dk_out):
         q, k, positions, *weights = ctx.saved_tensors
+        if q is None:
+            q, k = dq_out, dk_out
         dq, dk, *dw = qk_norm_rope_backward(dq_out, dk_out, q, k, positions, ctx.rotary, q_weight=weights[0],
                                             k_weight=weights[1], **ctx.how)
         dwq, dwk = (d if d is None else d.to(w.dtype) for d, w in zip(dw, weights))
@@ -727,6 +733,7 @@ def clip_grads(grads: Iterable[torch.Tensor] | torch.Tensor, max_norm: float,
     norm, work = _grad_workspace(grads[0])
     N.normpre_grad_clip(len(grads), block.buffer_info()[0], float(max_norm), norm.data_ptr(), work.data_ptr(),
                         work.numel(), _stream(at))
-    for o, t in back:
-        o.copy_(t)
+    with torch.no_grad():
+        for o, t in back:
+            o.copy_(t)
     return norm

@@ -283,6 +283,13 @@ def test_autograd_matches_calls(dev):
     want = T.qk_norm_rope_backward(dq, dk, q, k, pos, rotary, q_weight=wq, k_weight=wk.bfloat16().float())
     for x, y in zip(leaves, want):
         assert x.grad.dtype == x.dtype and torch.equal(x.grad, y.to(x.dtype))
+    # Without norms: nothing of q and k is kept.
+    x = [q.clone().requires_grad_(), k.clone().requires_grad_()]
+    out = T.qk_norm_rope(x[0], x[1], pos, rotary, norm=False)
+    assert all(t is None or t.dtype == torch.int64 for t in out[0].grad_fn.saved_tensors)
+    torch.autograd.backward(out, (dq, dk))
+    turned = T.qk_norm_rope_backward(dq, dk, q, k, pos, rotary, norm=False)
+    assert torch.equal(x[0].grad, turned[0]) and torch.equal(x[1].grad, turned[1])
     # One output unused; frozen weights.
     x = q.clone().requires_grad_()
     T.qk_norm_rope(x, k, pos, rotary, q_weight=wq, k_weight=wk)[0].backward(dq)

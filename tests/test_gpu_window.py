@@ -110,7 +110,7 @@ def test_long_rows(dev, dtype, window, sinks):
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("crowd", [0, 130, 250, 600, 1100])
+@pytest.mark.parametrize("crowd", [0, 90, 130, 250, 600, 1100])
 @pytest.mark.parametrize("nonfinite", [False, True])
 def test_in_a_crowd(dev, dtype, d, crowd, nonfinite):
     # How blocks share their work goes by the size of the batch: the same long

@@ -97,7 +97,8 @@ def test_rotary():
     assert T.Rotary([], device="cpu").pairs == 0
     assert T.Rotary.geometric(4, 100.0) == [1.0, 0.1]
     assert T.Rotary.geometric(0) == []
-    for bad in (lambda: T.Rotary([1.0], [0, 1], device="cpu"), lambda: T.Rotary([1.0], [-1], device="cpu"),
+    for bad in (lambda: T.Rotary([1.0, float("inf")], device="cpu"), lambda: T.Rotary([float("nan")], device="cpu"),
+                lambda: T.Rotary([1.0], [0, 1], device="cpu"), lambda: T.Rotary([1.0], [-1], device="cpu"),
                 lambda: T.Rotary.geometric(5), lambda: T.Rotary.geometric(-2)):
         with pytest.raises(ValueError):
             bad()
