@@ -107,6 +107,11 @@ def _rows(x: torch.Tensor) -> torch.Tensor:
     return x if x.stride(2) == 1 or x.shape[2] == 1 else x.contiguous()
 
 
+def _fresh(x: torch.Tensor) -> torch.Tensor:
+    """A contiguous tensor like x (2 us of host work less than by its shape)."""
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 # normpre_attention (include/normpre.h) in one piece: filling a ctypes structure
 # field by field takes as long as the launch itself.
 _ARGS = struct.Struct("=5if3q" + "Q2q" * 4 + "Q" + "Q2q" * 4 + "Qq")
@@ -144,7 +149,7 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: A
         with torch.cuda.device(at):
             return attention_forward(q, k, v, plan, scale)
     tokens, heads, dim = q.shape
-    out = q.new_empty((tokens, heads, dim))
+    out = _fresh(q)
     lse = q.new_empty((heads, tokens), dtype=torch.float32)
     block = _ARGS.pack(*args, out.data_ptr(), heads * dim, dim, lse.data_ptr(), *_NONE * 4, 0, 0)
     if plan.bounds is None:
@@ -169,7 +174,7 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     if _elsewhere(at):
         with torch.cuda.device(at):
             return attention_backward(dout, q, k, v, out, lse, plan, scale)
-    dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+    dq, dk, dv = _fresh(q), _fresh(k), _fresh(v)
     block = N.normpre_attention.from_buffer_copy(_ARGS.pack(
         *args, *_heads(out), lse.data_ptr(), *_heads(dout), *_heads(dq), *_heads(dk), *_heads(dv), 0, 0))
     bounds = plan.bounds
@@ -297,7 +302,7 @@ def qk_norm_rope_forward(q: torch.Tensor, k: torch.Tensor, positions: torch.Tens
     if _elsewhere(at):
         with torch.cuda.device(at):
             return qk_norm_rope_forward(q, k, positions, rotary, norm=norm, q_weight=q_weight, k_weight=k_weight, eps=eps)
-    q_out, k_out = q.new_empty(q.shape), k.new_empty(k.shape)
+    q_out, k_out = _fresh(q), _fresh(k)
     block = _ROPE.pack(*args, *_heads(q), *_heads(k), *_heads(q_out), *_heads(k_out), *_NONE * 2, 0, 0, 0, 0)
     N.normpre_qk_rope_forward(N.normpre_qk_rope.from_buffer_copy(block), _stream(at))
     return q_out, k_out
@@ -319,7 +324,7 @@ def qk_norm_rope_backward(dq_out: torch.Tensor, dk_out: torch.Tensor, q: torch.T
         with torch.cuda.device(at):
             return qk_norm_rope_backward(dq_out, dk_out, q, k, positions, rotary, norm=norm, q_weight=q_weight,
                                          k_weight=k_weight, eps=eps)
-    dq, dk = q.new_empty(q.shape), k.new_empty(k.shape)
+    dq, dk = _fresh(q), _fresh(k)
     dwq = dwk = None
     ends = (0, 0, 0, 0)
     if q_weight is not None or k_weight is not None:
