@@ -782,37 +782,54 @@ __device__ Odd odd_rows(const AttnOperand& o, const Where& w, int head, int from
 template <class T, int DP, bool VEC>
 __device__ __forceinline__ bool faithful(const AttnArgs& a) { return kTerms<T> == 1 && (!VEC || a.dim == DP); }
 
-// The query passes: the highest of the wave's rows, from row qw on, that x (v, or
-// k) spoils although it does not see the place, or INT_MAX: all of them.  Rows before
-// `done` were multiplied.
+// The query passes: the wave's rows, from row qw on, that x (v, or k) spoils although they do
+// not see the place: those up to `top` (INT_MAX: all of them) and, WIN, from `low` on, whose
+// windows begin behind it.  Rows before `done` were multiplied.
+struct SpoiledQueries {
+    int top, low;
+    template <bool WIN>
+    __device__ __forceinline__ bool has(int qi) const { return qi <= top || (WIN && qi >= low); }
+};
 template <class T, bool WIN>
-__device__ int spoiled_queries(const AttnArgs& a, const Where& w, const AttnOperand& x, int qw, int done, int lane,
-                               const KeyWalk& walk, int bn) {
+__device__ SpoiledQueries spoiled_queries(const AttnArgs& a, const Where& w, const AttnOperand& x, int qw, int done, int lane,
+                                          const KeyWalk& walk, int bn) {
+    int low = INT32_MAX;
     if constexpr (WIN) {                             // the far end of the windows, and copies of the last of the first keys
-        if (odd_rows<T>(x, w, w.kv, (walk.near + walk.skip) * bn, min(qw + 32 - min(a.window, qw + 32), w.len), a.dim, lane).any ||
-            (walk.near > 0 && odd_rows<T>(x, w, w.kv, min(a.sinks, walk.near * bn) - 1, min(a.sinks, walk.near * bn), a.dim, lane).inf))
-            return INT32_MAX;
+        const Odd far = odd_rows<T>(x, w, w.kv, max((walk.near + walk.skip) * bn, a.sinks),
+                                    min(qw + 32 - min(a.window, qw + 32), w.len), a.dim, lane);
+        if (far.any) low = (int)min((uint32_t)far.first + (uint32_t)a.window, (uint32_t)INT32_MAX);
+        const int few = min(a.sinks, walk.near * bn);
+        if (walk.near > 0 && odd_rows<T>(x, w, w.kv, few - 1, few, a.dim, lane).inf) low = 0;
     }
     const Odd o = odd_rows<T>(x, w, w.kv, a.causal ? qw : w.len - 1, min(done, w.len), a.dim, lane);
-    return a.causal ? o.last : done > w.len && o.inf ? INT32_MAX : -1;
+    return {a.causal ? o.last : done > w.len && o.inf ? INT32_MAX : -1, low};
 }
 
-// dk and dv: the keys above the one that this returns, of 32 from row kw on, are spoiled
-// by queries that do not see them; INT_MAX: none, -1: all.
+// dk and dv: the keys, of 32 from row kw on, that queries spoil which do not see them: those
+// above `above` (INT_MAX: none, -1: all) and, WIN, up to `below`, whose windows' queries end
+// before them.  WIN: not the first `lost` of them, which are NaN by the formula, and no key that every
+// later query sees by what is behind its window.
+struct SpoiledKeys {
+    int above, below = -1, lost = 0;
+    template <bool WIN>
+    __device__ __forceinline__ bool has(const AttnArgs& a, int ki) const {
+        return ki > above || (WIN && ki >= lost && ki <= below && ki >= a.sinks);
+    }
+};
 template <class T, bool WIN>
-__device__ int spoiled_keys(const AttnArgs& a, const Where& w, int kw, bool right, int lane) {
+__device__ SpoiledKeys spoiled_keys(const AttnArgs& a, const Where& w, int kw, bool right, int lane) {
     const int group = a.heads / a.kv_heads;
     // A query that every key of the wave sees and that has no log-sum-exp: all NaN.
     const int sure = a.causal ? min(kw + 31, w.len - 1) : 0, last = WIN ? kw + min(a.window, w.len - kw) : w.len;
-    bool lost = false, lost_first = false;           // WIN: of a query that the first keys see too, of one behind the windows
+    bool lost = false, lost_first = false;           // WIN: lost_first by a query behind the windows, which the first keys see
     for (int h = w.kv * group; h < (w.kv + 1) * group; ++h)
         for (int i = sure + lane; i < (WIN && kw < a.sinks ? w.len : last); i += 64) {
             const float l = a.lse[h * a.tokens + w.start + i];
             if (!WIN || i < last) lost |= l != l;
             else lost_first |= l != l;
         }
-    if (__any(lost)) return INT32_MAX;
-    if (WIN && __any(lost_first)) return a.sinks - 1;
+    if (__any(lost)) return {INT32_MAX};
+    const int first_lost = WIN && __any(lost_first) ? a.sinks : 0;
     // Queries that the tiled pass has multiplied with the wave's keys end before this one.
     const int met = !WIN || kw < a.sinks ? w.len : last + min(w.len - last, 64);
     if (!right) {
@@ -821,23 +838,22 @@ __device__ int spoiled_keys(const AttnArgs& a, const Where& w, int kw, bool righ
         for (int h = w.kv * group; h < (w.kv + 1) * group && !inf; ++h)
             inf = odd_rows<T>(a.q, w, h, a.causal ? kw : 0, met, a.dim, lane).inf ||
                   odd_rows<T>(a.dout, w, h, a.causal ? kw : 0, met, a.dim, lane).inf;
-        if (inf) return -1;
+        if (inf) return {first_lost - 1};
     }
-    if constexpr (WIN) {                             // queries past the window of the wave's first key
+    int far = -1;                                    // the last odd query past the window of the wave's first key
+    if constexpr (WIN)
         for (int h = w.kv * group; h < (w.kv + 1) * group; ++h)
-            if (odd_rows<T>(a.q, w, h, last, min(met, last + min(w.len - last, 64)), a.dim, lane).any ||
-                odd_rows<T>(a.dout, w, h, last, min(met, last + min(w.len - last, 64)), a.dim, lane).any)
-                return -1;
-    }
+            for (int x = 0; x < 2; ++x)
+                far = max(far, odd_rows<T>(x ? a.dout : a.q, w, h, last, last + min(w.len - last, 64), a.dim, lane).last);
     const bool copies = w.len % 32 != 0;
     int low = INT32_MAX;
     for (int h = w.kv * group; h < (w.kv + 1) * group; ++h)
         for (int x = 0; x < 2; ++x) {
             const AttnOperand& o = x ? a.dout : a.q;
             if (a.causal) low = min(low, odd_rows<T>(o, w, h, kw, min(kw + 32, w.len), a.dim, lane).first);
-            if (copies && odd_rows<T>(o, w, h, w.len - 1, w.len, a.dim, lane).inf) return -1;
+            if (copies && odd_rows<T>(o, w, h, w.len - 1, w.len, a.dim, lane).inf) return {first_lost - 1};
         }
-    return low;
+    return {max(low, first_lost - 1), far - a.window, first_lost};
 }
 
 // ---------------------------------------------------------------- passes ---
@@ -1067,9 +1083,9 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
         if (right) {
             bad &= ~lost;
             if (bad) {
-                const int top = odd_keys<T, WIN>(a, w, a.v, WIN ? min(sees, qw + 32 - min(a.window, qw + 32)) : 0, sees, walk, BN, lane).any
-                              ? spoiled_queries<T, WIN>(a, w, a.v, qw, ((a.causal ? min(end, qw + 32) : end) + BN - 1) / BN * BN, lane, walk, BN) : INT32_MAX;
-                bad &= bad_rows(qi <= top);
+                const SpoiledQueries spoiled = odd_keys<T, WIN>(a, w, a.v, WIN ? min(sees, qw + 32 - min(a.window, qw + 32)) : 0, sees, walk, BN, lane).any
+                              ? spoiled_queries<T, WIN>(a, w, a.v, qw, ((a.causal ? min(end, qw + 32) : end) + BN - 1) / BN * BN, lane, walk, BN) : SpoiledQueries{INT32_MAX, 0};
+                bad &= bad_rows(spoiled.has<WIN>(qi));
             }
         }
     }
@@ -1233,7 +1249,10 @@ __global__ void __launch_bounds__(64 * WR * TEAMS, (query_waves<T, DP, WR, TEAMS
             right = !odd_rows<T>(a.q, w, head, qw, min(qw + 32, w.len), a.dim, lane).inf &&
                     !odd_rows<T>(a.dout, w, head, qw, min(qw + 32, w.len), a.dim, lane).inf &&
                     !odd_keys<T, WIN>(a, w, a.k, 0, end, walk, BN, lane).inf && !odd_keys<T, WIN>(a, w, a.v, 0, end, walk, BN, lane).inf;
-        if (right) bad &= bad_rows(qi <= spoiled_queries<T, WIN>(a, w, a.k, qw, ((a.causal ? min(end, qw + 32) : end) + 31) / 32 * 32, lane, walk, BN));
+        if (right) {
+            const SpoiledQueries spoiled = spoiled_queries<T, WIN>(a, w, a.k, qw, ((a.causal ? min(end, qw + 32) : end) + 31) / 32 * 32, lane, walk, BN);
+            bad &= bad_rows(spoiled.has<WIN>(qi));
+        }
     }
     store_rows<T, DP, VEC>(mine, row_of<T>(a.dq, w, qw, head), a.dq.tok, g,
                            a.scale, a.dim, live_rows(qw, w.len) & ~bad, lane);
@@ -1447,24 +1466,29 @@ __global__ void __launch_bounds__(kThreads, (HELD ? 2 : kTerms<T> == 3 ? 1 : wav
     store_rows<T, DP, VEC>(mine, row_of<T>(a.dv, w, kw, kv), a.dv.tok, gv, 1.f, a.dim, keep, lane);
 }
 
+template <bool WIN> constexpr int kOddWaves = WIN ? 4 : 1;
+
 // Rows of dk and dv that attn_dkv_kernel found not finite: a wave for 32 of them.  In a
 // launch of its own (2 us), since in the kernel above their addresses would take scalar
 // registers that it has not: kept in vector registers, they slow it by a fifth
 // (packed 16418 tokens, 16/8 heads of 128, forward and backward 1097 us / 1235).
+// WIN: four waves for the 32 rows, whose windows' far end may make many of them odd.
 template <class T, int DP, bool VEC, bool WIN>
-__global__ void __launch_bounds__(kThreads) attn_odd_keys_kernel(AttnArgs a) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+__global__ void __launch_bounds__(kThreads * kOddWaves<WIN>) attn_odd_keys_kernel(AttnArgs a) {
+    const int lane = threadIdx.x & 63, all = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wave = all / kOddWaves<WIN>, part = all % kOddWaves<WIN>;
     const AttnTile tile = a.tiles[a.num_tiles + blockIdx.x / a.kv_heads];
     const int kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads;
     int kw;
     if (!locate(a, tile, wave * 32, kw)) return;
     uint32_t bad = a.odd[blockIdx.x * 4 + wave];
+    if (WIN) bad &= 0x11111111u << part;
     if (!bad) return;
     const Where w{tile.start, tile.len, kv * group, kv};
-    const int above = spoiled_keys<T, WIN>(a, w, kw, faithful<T, DP, VEC>(a), lane);
+    const SpoiledKeys spoiled = spoiled_keys<T, WIN>(a, w, kw, faithful<T, DP, VEC>(a), lane);
     for (; bad; bad &= bad - 1) {
         const int ki = kw + __builtin_ctz(bad);
-        if (ki > above) dkv_row<T, WIN>(a, w, ki, lane);
+        if (spoiled.has<WIN>(a, ki)) dkv_row<T, WIN>(a, w, ki, lane);
     }
 }
 
@@ -1531,8 +1555,8 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a) {
     // Rows that are not finite, of this wave: one by one.
     const uint64_t bad = __ballot(live && !(t == 0.f));
     constexpr uint64_t row_lanes = LR == 16 ? 0xffffull : 0xffffffffull;
-    const int above = bad ? spoiled_keys<T, WIN>(a, w, (ki - lane / LR) / 32 * 32, faithful<T, DP, true>(a), lane) : 0;
-    const bool redo = (bad >> (lane / LR * LR) & row_lanes) && ki > above;
+    const SpoiledKeys spoiled = bad ? spoiled_keys<T, WIN>(a, w, (ki - lane / LR) / 32 * 32, faithful<T, DP, true>(a), lane) : SpoiledKeys{0};
+    const bool redo = (bad >> (lane / LR * LR) & row_lanes) && spoiled.has<WIN>(a, ki);
     if (live && !redo) {
         T *dk = row_of<T>(a.dk, w, ki, kv), *dv = row_of<T>(a.dv, w, ki, kv);
 #pragma unroll
@@ -1543,7 +1567,7 @@ __global__ void __launch_bounds__(kThreads) attn_join_kernel(AttnArgs a) {
             }
     }
     for (int k = 0; k < 64 / LR; ++k)
-        if ((bad >> (k * LR) & row_lanes) && ki - lane / LR + k > above) dkv_row<T, WIN>(a, w, ki - lane / LR + k, lane);
+        if ((bad >> (k * LR) & row_lanes) && spoiled.has<WIN>(a, ki - lane / LR + k)) dkv_row<T, WIN>(a, w, ki - lane / LR + k, lane);
 }
 
 // -------------------------------------------------------------- launches ---

@@ -53,7 +53,7 @@ hipError_t run(const AttnArgs& a, bool backward, hipStream_t s) {
     if (e != hipSuccess) return e;
     const unsigned tiles = (unsigned)a.num_tiles * a.kv_heads, sinks = (unsigned)a.sink_tiles * a.kv_heads;
     if (a.splits == 1) {
-        attn_odd_keys_kernel<T, DP, VEC, true><<<tiles, kThreads, 0, s>>>(a);
+        attn_odd_keys_kernel<T, DP, VEC, true><<<tiles, kThreads * kOddWaves<true>, 0, s>>>(a);
         if (sinks) attn_join_kernel<T, DP, true><<<dim3(sinks, DP / 8), kThreads, 0, s>>>(a);
     } else attn_join_kernel<T, DP, true><<<dim3(tiles, DP / 8), kThreads, 0, s>>>(a);
     return hipGetLastError();
