@@ -807,13 +807,17 @@ __device__ SpoiledQueries spoiled_queries(const AttnArgs& a, const Where& w, con
 
 // dk and dv: the keys, of 32 from row kw on, that queries spoil which do not see them: those
 // above `above` (INT_MAX: none, -1: all) and, WIN, up to `below`, whose windows' queries end
-// before them.  WIN: not the first `lost` of them, which are NaN by the formula, and no key that every
-// later query sees by what is behind its window.
+// before them.  WIN: not the first `lost` of them, which are NaN by the formula.  Keys that every later query
+// sees (sinks) are spoiled by none behind their windows; `sinks`: but by infinities in dout near the windows' end,
+// where the two parts of their sums, up to it and past it, each mask queries of the other: 0 * inf is NaN,
+// the formula's dv infinite.  (An infinity in q makes the row's log-sum-exp and delta NaN, and these dk by
+// the formula; places masked in dv meet dout alone.)
 struct SpoiledKeys {
     int above, below = -1, lost = 0;
+    bool sinks = false;
     template <bool WIN>
     __device__ __forceinline__ bool has(const AttnArgs& a, int ki) const {
-        return ki > above || (WIN && ki >= lost && ki <= below && ki >= a.sinks);
+        return ki > above || (WIN && ki >= lost && (ki < a.sinks ? sinks : ki <= below));
     }
 };
 template <class T, bool WIN>
@@ -841,10 +845,13 @@ __device__ SpoiledKeys spoiled_keys(const AttnArgs& a, const Where& w, int kw, b
         if (inf) return {first_lost - 1};
     }
     int far = -1;                                    // the last odd query past the window of the wave's first key
+    bool sinks = false;
     if constexpr (WIN)
-        for (int h = w.kv * group; h < (w.kv + 1) * group; ++h)
-            for (int x = 0; x < 2; ++x)
-                far = max(far, odd_rows<T>(x ? a.dout : a.q, w, h, last, last + min(w.len - last, 64), a.dim, lane).last);
+        for (int h = w.kv * group; h < (w.kv + 1) * group; ++h) {
+            const int end = last + min(w.len - last, 64);
+            for (int x = 0; x < 2; ++x) far = max(far, odd_rows<T>(x ? a.dout : a.q, w, h, last, end, a.dim, lane).last);
+            if (kw < a.sinks && !sinks) sinks = odd_rows<T>(a.dout, w, h, max(kw, last - 31), end, a.dim, lane).inf;
+        }
     const bool copies = w.len % 32 != 0;
     int low = INT32_MAX;
     for (int h = w.kv * group; h < (w.kv + 1) * group; ++h)
@@ -853,7 +860,7 @@ __device__ SpoiledKeys spoiled_keys(const AttnArgs& a, const Where& w, int kw, b
             if (a.causal) low = min(low, odd_rows<T>(o, w, h, kw, min(kw + 32, w.len), a.dim, lane).first);
             if (copies && odd_rows<T>(o, w, h, w.len - 1, w.len, a.dim, lane).inf) return {first_lost - 1};
         }
-    return {max(low, first_lost - 1), far - a.window, first_lost};
+    return {max(low, first_lost - 1), far - a.window, first_lost, sinks};
 }
 
 // ---------------------------------------------------------------- passes ---
