@@ -218,22 +218,25 @@ class Rotary:
     64 bits); the first 2 * len(freqs) features of a head turn, the others stay.
     Angles (position * frequency) are exact to 2^-52 of their size, for up to 2^51.
     axes: the axis of positions that each pair turns by (default: all by the
-    first).  adjacent: pair i is features (2i, 2i + 1); else (i, i + len(freqs)).
+    first); num_axes: how many axes positions have, where there are more than the
+    highest of these.  adjacent: pair i is features (2i, 2i + 1); else (i, i + len(freqs)).
     """
 
     def __init__(self, freqs: Sequence[float], axes: Sequence[int] | None = None, adjacent: bool = False,
-                 device="cuda"):
+                 device="cuda", num_axes: int | None = None):
         freqs = [float(f) for f in freqs]
         if not all(map(math.isfinite, freqs)):
             raise ValueError("a frequency is not finite")
-        self.pairs, self.adjacent, self.num_axes = len(freqs), bool(adjacent), 1
-        if axes is not None:
-            axes = [int(a) for a in axes]
-            if len(axes) != len(freqs) or any(a < 0 for a in axes):
-                raise ValueError("axes names an axis, 0 or above, for each frequency")
-            self.num_axes = max(axes, default=0) + 1
+        self.pairs, self.adjacent = len(freqs), bool(adjacent)
+        axes = [0] * len(freqs) if axes is None else [int(a) for a in axes]
+        if len(axes) != len(freqs) or any(a < 0 for a in axes):
+            raise ValueError("axes names an axis, 0 or above, for each frequency")
+        named = max(axes, default=0) + 1
+        self.num_axes = named if num_axes is None else int(num_axes)
+        if self.num_axes < named:
+            raise ValueError(f"axis {named - 1} of {num_axes}")
         self.freqs = torch.tensor(freqs, dtype=torch.float64, device=device)
-        self.axes = None if axes is None or self.num_axes == 1 else torch.tensor(axes, dtype=torch.int32, device=device)
+        self.axes = None if named == 1 else torch.tensor(axes, dtype=torch.int32, device=device)
 
     @staticmethod
     def geometric(rotated: int, base: float = 10000.0) -> list[float]:
@@ -294,7 +297,8 @@ def qk_norm_rope_forward(q: torch.Tensor, k: torch.Tensor, positions: torch.Tens
                          k_weight: torch.Tensor | None = None, eps: float = 1e-6):
     """(q, k) with their heads normed, x / sqrt(mean x^2 + eps) times the weight
     [dim] if there is one (``norm``), and turned by ``rotary`` (None: not turned)
-    at ``positions``, int32 or int64 [tokens], or [axes, tokens] of several axes.
+    at ``positions``, int32 or int64 [tokens], or [axes, tokens] of several axes
+    (the rotary's ``num_axes``).
     q [tokens, heads, dim], k [tokens, kv_heads, dim], dim up to 256, any strides;
     weights fp32 or bf16."""
     q, k, positions = _rows(q), _rows(k), _positions(positions)
