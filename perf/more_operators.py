@@ -214,7 +214,7 @@ def prepare(case, seed):
         freqs, axes = _pairs(case)
         if own:
             from paper_2609_36692_amd import train_ops
-            s["rotary"] = train_ops.Rotary(freqs, axes=axes, adjacent=case["adjacent"], device=DEVICE)
+            s["rotary"] = train_ops.Rotary(freqs, axes=axes, adjacent=case["adjacent"], device=DEVICE, num_axes=case["axes"])
         else:
             s["freqs"] = torch.tensor(freqs, dtype=torch.float64, device=DEVICE)
             s["axis"] = torch.tensor(axes, device=DEVICE)
