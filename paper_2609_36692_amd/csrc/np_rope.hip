@@ -253,6 +253,7 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kernel(RopeArgs a, int share
             auto row = [&](const AttnOperand& x) { return static_cast<T*>(x.p) + token * x.tok + hh * x.head; };
             float x[2][E];
             float r = 1.f;
+            int size = 0;
             if (!BACK || a.norm) {
                 at.load(row(a.x[o]), on, x[0], x[1]);
                 if (a.norm) {
@@ -264,11 +265,16 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kernel(RopeArgs a, int share
                     const double mean = group_sum<L>(sum) * a.inv_dim + a.eps;
                     double q = __builtin_amdgcn_rsq(mean);
                     q *= 1.5 - 0.5 * mean * q * q;
+                    // Rows are brought near 1 by a power of two, so that 1 / rms is a normal fp32 number also for
+                    // subnormal rows with eps 0 and at the range's end: exact but for features that round
+                    // to 0 in the result (the same time: 112 us for 16384 tokens, 16/8 heads of 128).
+                    size = -(__builtin_amdgcn_frexp_exp(mean) >> 1);
+                    q = __builtin_amdgcn_ldexp(q, -size);
                     r = !on || mean == INFINITY ? 0.f : (float)q;    // a row that is not there: 0, also where eps is
 #pragma unroll
                     for (int e = 0; e < E; ++e)
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) x[m][e] *= r;
+                        for (int m = 0; m < 2; ++m) x[m][e] = __builtin_amdgcn_ldexpf(x[m][e], size) * r;
                 }
             }
             float y[2][E];
@@ -301,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 4) rope_kernel(RopeArgs a, int share
 #pragma unroll
                     for (int e = 0; e < E; ++e)
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) y[m][e] = r * (y[m][e] - x[m][e] * mean);
+                        for (int m = 0; m < 2; ++m) y[m][e] = __builtin_amdgcn_ldexpf(r * (y[m][e] - x[m][e] * mean), size);
                 }
             }
             at.store(row(a.y[o]), on, y[0], y[1]);
