@@ -738,7 +738,7 @@ def clip_grads(grads: Iterable[torch.Tensor] | torch.Tensor, max_norm: float,
     at, block = _grad_entries(sources, targets)
     if _elsewhere(at):
         with torch.cuda.device(at):
-            return clip_grads(grads, max_norm, out)
+            return clip_grads(grads, max_norm, None if out is None else outs)    # out may be used up
     norm, work = _grad_workspace(grads[0])
     N.normpre_grad_clip(len(grads), block.buffer_info()[0], float(max_norm), norm.data_ptr(), work.data_ptr(),
                         work.numel(), _stream(at))
