@@ -721,9 +721,10 @@ def clip_grads(grads: Iterable[torch.Tensor] | torch.Tensor, max_norm: float,
     """Scales the gradients by max_norm / norm where their norm (``grad_norm``, which
     is returned) exceeds max_norm: in place, or into ``out``, tensors of the same
     shapes, bf16 or fp32, which are written in any case (bf16 gradients for an
-    optimizer that takes fp32 ones).  Does not wait for the GPU.  NaN or infinite
-    gradients follow the formula: a norm of NaN makes every gradient NaN, an
-    infinite one 0 or, where it was infinite, NaN."""
+    optimizer that takes fp32 ones).  Autograd takes either for a write in place,
+    whatever the norm.  Does not wait for the GPU.  NaN or infinite gradients follow
+    the formula: a norm of NaN makes every gradient NaN, an infinite one 0 or, where it
+    was infinite, NaN."""
     grads = _grad_list(grads)
     if not max_norm >= 0:
         raise ValueError(f"max_norm is {max_norm}")
@@ -742,6 +743,7 @@ def clip_grads(grads: Iterable[torch.Tensor] | torch.Tensor, max_norm: float,
     norm, work = _grad_workspace(grads[0])
     N.normpre_grad_clip(len(grads), block.buffer_info()[0], float(max_norm), norm.data_ptr(), work.data_ptr(),
                         work.numel(), _stream(at))
+    torch.autograd.graph.increment_version(outs)     # a backward pass that kept them has to notice
     with torch.no_grad():
         for o, t in back:
             o.copy_(t)

@@ -1,5 +1,5 @@
 """Calls of clip_grads in the ways that a program makes them: outputs from a generator on another
-device than the current one."""
+device than the current one, and gradients that a graph still holds."""
 import contextlib
 from array import array
 
@@ -46,3 +46,35 @@ def test_outputs_from_a_generator(monkeypatch):
     for g, o in zip(grads, outs):
         # One rounding of the factor's product, and 2^-40 for the factor.
         assert float((o.double() * (900.0 + 704.0) ** 0.5 / g.double() - 1.0).abs().max()) <= 2.0 ** -24 + 2.0 ** -40
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("limit", [0.1, 1e9])        # scaled, and left as they are
+def test_writes_are_seen_by_autograd(limit):
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    dev = torch.device("cuda:0")
+    grads = [torch.ones(5, device=dev), torch.ones(4, 6, device=dev)[:, ::2], torch.ones(3, 4, device=dev, dtype=torch.bfloat16).t()]
+    outs = [torch.zeros(5, device=dev), torch.zeros(4, 3, device=dev), torch.zeros(8, 3, device=dev)[::2]]
+    before = [x._version for x in grads + outs]
+    T.grad_norm(grads)
+    assert [x._version for x in grads + outs] == before
+    T.clip_grads(grads, limit, out=outs)
+    assert [x._version for x in grads] == before[:3] and all(x._version > v for x, v in zip(outs, before[3:]))
+    T.clip_grads(grads, limit)
+    assert all(x._version > v for x, v in zip(grads, before))
+    with torch.inference_mode():                     # tensors without a version
+        x = torch.full((7,), 2.0, device=dev)
+        T.clip_grads([x], limit)
+
+
+@pytest.mark.gpu
+def test_a_gradient_that_was_kept_and_clipped_is_refused():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    w = torch.tensor([1.0, 2.0, 3.0], device="cuda:0", requires_grad=True)
+    g, = torch.autograd.grad((w ** 3).sum(), w, create_graph=True)
+    penalty = (g * g).sum()                          # keeps g
+    T.clip_grads([g], 0.5)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        penalty.backward()
