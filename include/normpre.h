@@ -643,9 +643,9 @@ int normpre_checkpoint_weight_grad(int dtype, int layout, int accumulate, int64_
  * The backward call takes the gradients of q_out and k_out in their place (and q and
  * k where norm is 1) and writes dq, dk and, where wanted, the weights' gradients,
  * summed over tokens and heads (zero for tokens = 0).
- * Angles are reduced in 64 bits: at position p they are off by p freqs[i] 2^-52
- * (for p freqs[i] up to 2^51).
- * Squares are summed in 64 bits, the rest is fp32, rounded once.
+ * Angles are reduced in 64 bits: at position p they are off by p freqs[i] 2^-51 at
+ * most (for p freqs[i] up to 2^51), and their cos and sin, fp32 from there on, by
+ * another 5 2^-24.  Squares are summed in 64 bits, the rest is fp32, rounded once.
  */
 typedef struct normpre_qk_rope {
     int32_t dtype;              /* NORMPRE_DTYPE_*, of every operand             */

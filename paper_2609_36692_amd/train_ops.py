@@ -216,7 +216,8 @@ class Rotary:
 
     freqs: radians a step of each turning pair of features (finite numbers, kept in
     64 bits); the first 2 * len(freqs) features of a head turn, the others stay.
-    Angles (position * frequency) are exact to 2^-52 of their size, for up to 2^51.
+    Angles (position * frequency) are off by 2^-51 of their size at most, for up to 2^51,
+    and their cos and sin by another 5 2^-24 (fp32).
     axes: the axis of positions that each pair turns by (default: all by the
     first); num_axes: how many axes positions have, where there are more than the
     highest of these.  adjacent: pair i is features (2i, 2i + 1); else (i, i + len(freqs)).
