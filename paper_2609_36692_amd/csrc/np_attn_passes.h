@@ -900,8 +900,9 @@ __device__ __forceinline__ bool locate(const AttnArgs& a, const AttnTile& t, int
     return tile_row(t, a.tokens, within, row0);
 }
 
-// WIN: tiles of the first keys alone end behind the last of them, so that no key that
-// nobody sees is multiplied.
+// WIN: tiles of the first keys alone end behind the last of them: the rows behind it are copies of that one
+// and masked.  (The forward pass multiplies them all the same, the dq pass leaves out blocks of 32 rows
+// without a first key.)
 template <bool WIN, class S>
 __device__ __forceinline__ void walk_rows(S& keys, const AttnArgs& a, const KeyWalk& walk, int bn) {
     if constexpr (WIN)

@@ -7,12 +7,18 @@
 // and masks them on both sides.
 //
 // Measured (bf16, 16/8 heads of 128, window 1024, 4 first tokens; flops of the visible
-// pairs): forward, 16964 tokens, 187-200 us (675-720 TFLOP/s); packed 15932 tokens: forward 165 us
-// (700), dq 228 (760), dk/dv 357 (650).  Matrix instructions take 31 to 38% of the cycles, vector ones
-// 41 to 56%.  What is lost against long causal rows (940-1000): the masked 11% of the pairs,
-// each block's start and end over 19 tiles instead of a hundred, and the last round of
-// blocks (2160 on 512 places; dk/dv: 1112, 2.2 rounds that take three).
-// 4 x 1024 tokens, fp32, 12 heads of 64, window 256: forward 40 us, dq 55, dk/dv 91.
+// pairs): forward, 16964 tokens, 191-202 us (667-705 TFLOP/s); packed 15932 tokens: forward 165-178 us,
+// dq 226-245, dk/dv 356-386, together 727-753 us (540-558).  Matrix instructions take 31 to 38% of the cycles,
+// vector ones 41 to 56%.  What is lost against long causal rows (940-1000): the masked 11% of the pairs,
+// each block's start and end over 19 tiles instead of a hundred, the last round of
+// blocks (2160 on 512 places; dk/dv: 1112, 2.2 rounds that take three), and the masks' registers: forward 256
+// at heads of 128 and 179 at heads of 64, where it has 208 and 124 without a window (of 64: two waves per SIMD
+// instead of four), and dk/dv with v in LDS spills 8.
+// 16 x 1024 tokens, bf16, 12 heads of 64, window 256: forward 38-41 us (300 TFLOP/s), dq 46, dk/dv 60; with 4 first
+// tokens 40-44, 47, 74.
+// 4 x 1024 tokens, fp32, 12 heads of 64, window 256: forward 40 us, dq 56, dk/dv 91: 384 blocks, so that half of
+// the CUs have two and the others one, each a chain of up to 12 tiles that pass through registers and are split there;
+// the pipes are 18 to 30% busy.  Forward and dq have two waves per SIMD (224 and 256 registers), dk/dv (337) one.
 #include "np_attn_passes.h"
 
 namespace np {
@@ -30,7 +36,8 @@ hipError_t run(const AttnArgs& a, bool backward, hipStream_t s) {
     //     39.9 49.2
     //   fp32, (4, 1) and (2, 2), 64, 500: 256: 47.6 40.1, 320: 52.5 61.1; 128, 500: 128: 86.6
     //     52.6, 192: 92.7 100, 256: 96.8 103
-    // Rows that do not start on 16 bytes take (4, 1), as without a window.
+    // The rule goes by blocks and head size alone; with a window of 1500 it takes (4, 1) at 320 blocks, a third
+    // slower than (2, 2).  Rows that do not start on 16 bytes take (4, 1), as without a window.
     const int64_t blocks = (int64_t)a.num_tiles * a.heads;
     if constexpr (!VEC) query_pass<T, DP, VEC, 4, 1, true>(a, backward, s);
     else if (blocks <= (DP == 64 ? 256 : 128)) query_pass<T, DP, VEC, 2, 2, true>(a, backward, s);
@@ -44,7 +51,7 @@ hipError_t run(const AttnArgs& a, bool backward, hipStream_t s) {
     // once there are more of them than CUs.  Backward us with them there / in registers
     // (16/8 heads; blocks x shares): window 300: 64 x 1 111 / 103, 128 x 2 92 / 112, 256 x 1 155 / 180,
     // 512 x 1 256 / 283, 1024 x 1 442 / 567; window 1000: 128 x 2 180 / 164, 512 x 1 393 / 421, 1024 x 1
-    // 718 / 834.
+    // 718 / 834.  By blocks x shares alone: at 128 x 2 and a window of 1000 it takes the slower one.
     constexpr bool can_hold = VEC && sizeof(T) == 2 && DP == 128;
     if (can_hold && (int64_t)a.num_tiles * a.kv_heads * a.splits >= 256)
         attn_dkv_kernel<T, DP, VEC, can_hold, true><<<keys, kThreads, 0, s>>>(a);

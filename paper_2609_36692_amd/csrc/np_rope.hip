@@ -6,17 +6,25 @@
 //   dw_d = sum over rows g_d x_d r,  h_d = g_d w_d,  dx_d = r (h_d - x_d r mean_d(h_d x_d r)).
 //
 // Bound by memory (forward: each head read and written once; backward: x and dy read, dx
-// written): 16384 tokens, 16/8 heads of 128, bf16 37 us forward (201 MB), 65 backward (302 MB), where a
-// copy's rate of 4.76 TB/s would take 42 and 63.  A group of L lanes has one token and takes
-// heads of it in turn, each lane E pairs, so that an angle serves several heads and is not
-// read from a table: position * f in 64 bits (in 32 the angle of position 10^6 is
-// off by 0.06), reduced to a quarter turn, then polynomials.  Queries and keys go to blocks of
-// their own: weights and their gradients of one operand leave registers for four waves a
-// SIMD (both in one: 75 us backward).  A lane's pairs are whole
-// 16-byte chunks of the two halves of a row (or of its adjacent pairs), so a rotation needs
-// no other lane, and the mean of squares log2 L exchanges.  Squares are summed in 64 bits,
-// so rows of very large and very small values keep their norm; the rest is fp32 and rounded
-// once.
+// written): 16384 tokens, 16/8 heads of 128, bf16 38-45 us forward (201 MB; less where the last-level
+// cache holds a part), 64 backward and 5 for the weights' sums (302 MB), where a copy's rate of
+// 4.76 TB/s would take 42 and 63; fp32 85 forward (403 MB), 207 with the backward pass (1007 MB), a copy 85 and 211.
+//
+// A group of L lanes has one token and takes heads of it in turn, each lane E pairs, so that
+// an angle serves several heads and is not read from a table: position * f in 64 bits (in 32 the
+// angle of position 10^6 is off by 0.06), reduced to a quarter turn, then polynomials.
+// Queries and keys go to blocks of their own: with weights and their gradients of one operand
+// registers do for four waves a SIMD, but for 14 to 16 that the backward pass of bf16
+// spills (both operands in one block: 75 us backward).  A lane's pairs are whole 16-byte
+// chunks of the two halves of a row (or of its adjacent pairs), so a rotation needs no other
+// lane, and the mean of squares log2 L exchanges.  Where they are not, lanes go feature by feature,
+// at up to four times a copy's time: us forward and both passes of 16384 tokens, bf16, (a copy's): 41 pairs
+// of 16/8 heads of 128 98 288 (42 106), 36 of 16/16 of 72 110 266 (32 79), 10 of 80 119 264 (35
+// 88), 25 of 51 81 200 (22 56), and in whole chunks 40 of 80 42 106 (35 88); fp32, 41 of 16/8 of
+// 128 97 227 (85 211).
+//
+// Squares are summed in 64 bits and a row is brought near 1 by a power of two, so rows at
+// either end of fp32's range keep their norm; the rest is fp32 and rounded once.
 // Weight gradients are summed per lane over its rows, then over the block, then over blocks
 // in their order (in 64 bits): the same bits every time, no atomics.
 #include "np_rope.h"
